@@ -390,3 +390,278 @@ def _marshal_splitkv(entry, dt, q, k, v, n_split, o, lse, workspace, causal, sca
     if rc != ATTN_OK:
         raise AttnError(rc)
     return o, lse
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# Rotary positions, the paged cache and attention over it (include/attn_rope.h, include/attn_cache.h)
+
+ATTN_CACHE_16BIT = 0
+ATTN_CACHE_E4M3 = 1
+
+_pointer, _int, _int64, _float = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_float
+for _name, _args in (("attn_rope", [_pointer] * 8 + [_int] * 8 + [_pointer]),
+                     ("attn_cache_write", [_pointer] * 10 + [_int] * 8 + [_pointer]),
+                     ("attn_cache_read", [_pointer] * 10 + [_int] * 8 + [_pointer]),
+                     ("attn_paged_fwd", [_pointer] * 11 + [_int, _pointer, _int64, _int] + [_int] * 9 + [_float, _pointer])):
+    for _suffix in ("", "_f16"):
+        getattr(_lib, _name + _suffix).restype = _int
+        getattr(_lib, _name + _suffix).argtypes = _args
+_lib.attn_paged_fwd_workspace_bytes.restype = _int64
+_lib.attn_paged_fwd_workspace_bytes.argtypes = [_int] * 5
+
+
+def _strides(*dims):
+    """A C array of the strides of (tensor, dimension) pairs; a dimension of one element has none."""
+    return (_int64 * len(dims))(*(t.stride(d) if t is not None and t.shape[d] > 1 else 0 for t, d in dims))
+
+
+def _check_rows(t, dt, dims, name, device):
+    """Rows of contiguous elements, any strides between them."""
+    if t.dtype != dt or not t.is_cuda or t.dim() != dims or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise TypeError("%s must be a %d-D %s tensor on the GPU whose last dimension is contiguous" % (name, dims, dt))
+    if t.device != device:
+        raise ValueError("%s is on another device" % name)
+
+
+def _check_output(t, name):
+    """Two rows of an output must not share memory: sorted by stride, every dimension steps over the ones below it."""
+    reach = 1
+    for stride, size in sorted((t.stride(d), t.shape[d]) for d in range(t.dim()) if t.shape[d] > 1):
+        if stride < reach:
+            raise ValueError("rows of %s overlap" % name)
+        reach = stride * (size - 1) + reach
+
+
+def _check_array(t, dtype, shape, name, device):
+    if t.dtype != dtype or not t.is_cuda or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise TypeError("%s must be a contiguous %s GPU tensor of shape %s" % (name, dtype, tuple(shape)))
+    if t.device != device:
+        raise ValueError("%s is on another device" % name)
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
+
+
+def attn_rope(q, k, pos, freq, sections, q_out=None, k_out=None, interleaved=False, inverse=False, stream=None):
+    """attn_rope on torch device tensors (include/attn_rope.h): q and k turned by the positions of their tokens.
+
+    q [B,H_q,S,D], k [B,H_kv,S,D] (or None): bf16 on the GPU, any strides with D contiguous elements, so slices of a
+    projection's rows are fine (rows[:, :H_q].transpose(0, 1)[None]).  pos int32 [n_axes,B,S], freq fp64 [pairs], radians
+    per unit of position; sections: how many pairs follow each axis (sum = pairs; 2 * pairs of a head's D elements are
+    turned, the others are copied).  q_out and k_out are allocated when not given (contiguous); they may be q and k.
+    inverse=True turns back: with the gradients of the outputs in place of q and k it gives the gradients of the inputs.
+    Asynchronous on `stream`.  Returns (q_out, k_out).
+    """
+    import torch
+    return _marshal_rope(_lib.attn_rope, torch.bfloat16, q, k, pos, freq, sections, q_out, k_out, interleaved, inverse, stream)
+
+
+def attn_rope_f16(q, k, pos, freq, sections, q_out=None, k_out=None, interleaved=False, inverse=False, stream=None):
+    """attn_rope_f16 on torch device tensors: as attn_rope, with fp16 tensors."""
+    import torch
+    return _marshal_rope(_lib.attn_rope_f16, torch.float16, q, k, pos, freq, sections, q_out, k_out, interleaved, inverse, stream)
+
+
+def _marshal_rope(entry, dt, q, k, pos, freq, sections, q_out, k_out, interleaved, inverse, stream):
+    import torch
+
+    _check_rows(q, dt, 4, "q", q.device)
+    B, H_q, S, D = q.shape
+    H_kv = 0
+    if k is not None:
+        _check_rows(k, dt, 4, "k", q.device)
+        H_kv = k.shape[1]
+        if k.shape[0] != B or k.shape[2] != S or k.shape[3] != D:
+            raise ValueError("q, k shapes do not agree")
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    sections = [int(n) for n in sections]
+    _check_array(pos, torch.int32, (len(sections), B, S), "pos", q.device)
+    _check_array(freq, torch.float64, (sum(sections),), "freq", q.device)
+    if q_out is None:
+        q_out = _allocate(lambda: torch.empty(q.shape, dtype=dt, device=q.device), q.device, stream)
+    if k_out is None and k is not None:
+        k_out = _allocate(lambda: torch.empty(k.shape, dtype=dt, device=q.device), q.device, stream)
+    for t, like, name in ((q_out, q, "q_out"), (k_out, k, "k_out")):
+        if t is None:
+            continue
+        _check_rows(t, dt, 4, name, q.device)
+        if t.shape != like.shape:
+            raise ValueError("%s is not shaped like its input" % name)
+        _check_output(t, name)
+    if stream is None:
+        stream = torch.cuda.current_stream(q.device)
+    strides = _strides(*((t, d) for t in (q, q_out, k, k_out) for d in range(3)))
+    with torch.cuda.device(q.device):
+        rc = entry(q.data_ptr(), q_out.data_ptr(), _address(k), _address(k_out), strides, pos.data_ptr(), freq.data_ptr(),
+                   (_int * len(sections))(*sections), len(sections), B, H_q, H_kv, S, D, int(bool(interleaved)),
+                   int(bool(inverse)), stream.cuda_stream)
+    if rc != ATTN_OK:
+        raise AttnError(rc)
+    return q_out, k_out
+
+
+def _check_cache(dt, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale, device):
+    """The cache's tensors; returns (kind, n_pages, H_kv, page_size, D, B, table_width)."""
+    import torch
+
+    if k_pages.dim() != 4:
+        raise TypeError("k_pages must be [n_pages, H_kv, page_size, D]")
+    kind = ATTN_CACHE_E4M3 if k_pages.dtype == torch.float8_e4m3fn else ATTN_CACHE_16BIT
+    pages_dt = torch.float8_e4m3fn if kind == ATTN_CACHE_E4M3 else dt
+    _check_array(k_pages, pages_dt, k_pages.shape, "k_pages", device)
+    _check_array(v_pages, pages_dt, k_pages.shape, "v_pages", device)
+    if kind == ATTN_CACHE_E4M3:
+        if k_scale is None or v_scale is None:
+            raise TypeError("an e4m3 cache needs k_scale and v_scale")
+        _check_array(k_scale, torch.uint8, k_pages.shape[:3], "k_scale", device)
+        _check_array(v_scale, torch.uint8, k_pages.shape[:3], "v_scale", device)
+    elif k_scale is not None or v_scale is not None:
+        raise TypeError("a 16-bit cache has no scales")
+    if page_table.dim() != 2:
+        raise TypeError("page_table must be [B, table_width]")
+    B = page_table.shape[0]
+    _check_array(page_table, torch.int32, page_table.shape, "page_table", device)
+    _check_array(start, torch.int32, (B + 1,), "start", device)
+    _check_array(kv_len, torch.int32, (B,), "kv_len", device)
+    n_pages, H_kv, page_size, D = k_pages.shape
+    return kind, n_pages, H_kv, page_size, D, B, page_table.shape[1]
+
+
+def attn_cache_write(k, v, k_pages, v_pages, page_table, start, kv_len, k_scale=None, v_scale=None, stream=None):
+    """attn_cache_write on torch device tensors (include/attn_cache.h): new rows of K and V into their pages.
+
+    k, v [T,H_kv,D] bf16, any strides with D contiguous elements.  k_pages, v_pages [n_pages,H_kv,page_size,D]: bf16, or
+    float8_e4m3fn with k_scale, v_scale uint8 [n_pages,H_kv,page_size].  page_table int32 [B,table_width], start int32 [B+1],
+    kv_len int32 [B]: rows start[b] .. start[b+1]-1 become the last positions below kv_len[b] of sequence b.
+    Asynchronous on `stream`.  Returns (k_pages, v_pages).
+    """
+    import torch
+    _marshal_rows(_lib.attn_cache_write, torch.bfloat16, k, v, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale,
+                  stream)
+    return k_pages, v_pages
+
+
+def attn_cache_write_f16(k, v, k_pages, v_pages, page_table, start, kv_len, k_scale=None, v_scale=None, stream=None):
+    """attn_cache_write_f16 on torch device tensors: as attn_cache_write, with fp16 rows (and fp16 or e4m3 pages)."""
+    import torch
+    _marshal_rows(_lib.attn_cache_write_f16, torch.float16, k, v, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale,
+                  stream)
+    return k_pages, v_pages
+
+
+def attn_cache_read(k_pages, v_pages, page_table, start, kv_len, n_rows, k_scale=None, v_scale=None, k=None, v=None,
+                    stream=None):
+    """attn_cache_read on torch device tensors (include/attn_cache.h): the last positions below kv_len[b] of sequence b into
+    rows start[b] .. start[b+1]-1 of k and v, [n_rows,H_kv,D] bf16, allocated when not given (any strides with D contiguous
+    elements: [H_kv,n_rows,D] tensors transposed are what attn_fwd takes).  Rows of no sequence are left as they were.  The
+    cache's arguments are those of attn_cache_write.  Asynchronous on `stream`.  Returns (k, v).
+    """
+    import torch
+    return _read(_lib.attn_cache_read, torch.bfloat16, k_pages, v_pages, page_table, start, kv_len, n_rows, k_scale, v_scale, k,
+                 v, stream)
+
+
+def attn_cache_read_f16(k_pages, v_pages, page_table, start, kv_len, n_rows, k_scale=None, v_scale=None, k=None, v=None,
+                        stream=None):
+    """attn_cache_read_f16 on torch device tensors: as attn_cache_read, with fp16 rows."""
+    import torch
+    return _read(_lib.attn_cache_read_f16, torch.float16, k_pages, v_pages, page_table, start, kv_len, n_rows, k_scale, v_scale,
+                 k, v, stream)
+
+
+def _read(entry, dt, k_pages, v_pages, page_table, start, kv_len, n_rows, k_scale, v_scale, k, v, stream):
+    import torch
+
+    shape = (int(n_rows), k_pages.shape[1], k_pages.shape[3])
+    make = lambda: torch.empty(shape, dtype=dt, device=k_pages.device)
+    k = _allocate(make, k_pages.device, stream) if k is None else k
+    v = _allocate(make, k_pages.device, stream) if v is None else v
+    for t, name in ((k, "k"), (v, "v")):
+        if tuple(t.shape) != shape:
+            raise ValueError("%s must be [n_rows, H_kv, D]" % name)
+        _check_output(t, name)
+    _marshal_rows(entry, dt, k, v, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale, stream)
+    return k, v
+
+
+def _marshal_rows(entry, dt, k, v, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale, stream):
+    import torch
+
+    _check_rows(k, dt, 3, "k", k.device)
+    _check_rows(v, dt, 3, "v", k.device)
+    kind, n_pages, H_kv, page_size, D, B, width = _check_cache(dt, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale,
+                                                               k.device)
+    if k.shape != v.shape or tuple(k.shape[1:]) != (H_kv, D):
+        raise ValueError("k, v must be [T, H_kv, D] with the cache's heads")
+    if stream is None:
+        stream = torch.cuda.current_stream(k.device)
+    with torch.cuda.device(k.device):
+        rc = entry(k.data_ptr(), v.data_ptr(), _strides((k, 0), (k, 1), (v, 0), (v, 1)), k_pages.data_ptr(), v_pages.data_ptr(),
+                   _address(k_scale), _address(v_scale), page_table.data_ptr(), start.data_ptr(), kv_len.data_ptr(), kind,
+                   k.shape[0], B, H_kv, D, n_pages, page_size, width, stream.cuda_stream)
+    if rc != ATTN_OK:
+        raise AttnError(rc)
+
+
+def attn_paged_fwd_workspace_bytes(T, B, H_q, H_kv, D):
+    return int(_lib.attn_paged_fwd_workspace_bytes(T, B, H_q, H_kv, D))
+
+
+def attn_paged_fwd(q, k_pages, v_pages, page_table, start, kv_len, k_scale=None, v_scale=None, o=None, lse=None, workspace=None,
+                   causal=True, scale=None, max_q=None, stream=None):
+    """attn_paged_fwd on torch device tensors (include/attn_cache.h): the new tokens' queries against the cache.
+
+    q [T,H_q,D] bf16, any strides with D contiguous elements; H_q a multiple of the cache's H_kv.  The cache's arguments are
+    those of attn_cache_write, which has put the same rows' keys and values there.  o (bf16 [T,H_q,D]) and lse (fp32 [T,H_q])
+    are allocated when not given; rows of no sequence are left as they were.  workspace: a contiguous GPU tensor of at least
+    attn_paged_fwd_workspace_bytes(...) bytes (allocated when not given); calls that overlap in time need one each.
+    causal: row i of n_b sees the keys up to its own position, otherwise all kv_len[b] of them.  max_q: the largest n_b (or
+    an upper bound; T when not given), which chooses the kernels.  Asynchronous on `stream`.  Returns (o, lse).
+    """
+    import torch
+    return _marshal_paged(_lib.attn_paged_fwd, torch.bfloat16, q, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale,
+                          o, lse, workspace, causal, scale, max_q, stream)
+
+
+def attn_paged_fwd_f16(q, k_pages, v_pages, page_table, start, kv_len, k_scale=None, v_scale=None, o=None, lse=None,
+                       workspace=None, causal=True, scale=None, max_q=None, stream=None):
+    """attn_paged_fwd_f16 on torch device tensors: as attn_paged_fwd, with fp16 q and o (and fp16 or e4m3 pages)."""
+    import torch
+    return _marshal_paged(_lib.attn_paged_fwd_f16, torch.float16, q, k_pages, v_pages, page_table, start, kv_len, k_scale,
+                          v_scale, o, lse, workspace, causal, scale, max_q, stream)
+
+
+def _marshal_paged(entry, dt, q, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale, o, lse, workspace, causal, scale,
+                   max_q, stream):
+    import torch
+
+    _check_rows(q, dt, 3, "q", q.device)
+    T, H_q, D = q.shape
+    kind, n_pages, H_kv, page_size, D_cache, B, width = _check_cache(dt, k_pages, v_pages, page_table, start, kv_len, k_scale,
+                                                                     v_scale, q.device)
+    if D != D_cache or H_kv < 1 or H_q % H_kv:
+        raise ValueError("q's heads do not fit the cache's")
+    need = attn_paged_fwd_workspace_bytes(T, B, H_q, H_kv, D)
+    o = _allocate(lambda: torch.empty((T, H_q, D), dtype=dt, device=q.device), q.device, stream) if o is None else o
+    if lse is None:
+        lse = _allocate(lambda: torch.empty((T, H_q), dtype=torch.float32, device=q.device), q.device, stream)
+    if workspace is None:
+        workspace = _allocate(lambda: torch.empty((max(need, 16),), dtype=torch.uint8, device=q.device), q.device, stream,
+                              returned=False)
+    _check_array(o, dt, (T, H_q, D), "o", q.device)
+    _check_array(lse, torch.float32, (T, H_q), "lse", q.device)
+    _check_array(workspace, workspace.dtype, workspace.shape, "workspace", q.device)
+    if scale is None:
+        scale = 1.0 / float(D) ** 0.5
+    if stream is None:
+        stream = torch.cuda.current_stream(q.device)
+    with torch.cuda.device(q.device):
+        rc = entry(q.data_ptr(), _strides((q, 0), (q, 1)), o.data_ptr(), lse.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+                   _address(k_scale), _address(v_scale), page_table.data_ptr(), start.data_ptr(), kv_len.data_ptr(), kind,
+                   workspace.data_ptr(), workspace.numel() * workspace.element_size(), T if max_q is None else int(max_q),
+                   T, B, H_q, H_kv, D, n_pages, page_size, width, int(bool(causal)), float(scale), stream.cuda_stream)
+    if rc != ATTN_OK:
+        raise AttnError(rc)
+    return o, lse

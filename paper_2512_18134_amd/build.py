@@ -15,10 +15,12 @@ import os
 import subprocess
 import sys
 import sysconfig
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SOURCES = [os.path.join(HERE, "csrc", "attn_fwd.hip"), os.path.join(HERE, "csrc", "attn_bwd.hip")]
+SOURCES = [os.path.join(HERE, "csrc", name) for name in ("attn_fwd.hip", "attn_bwd.hip", "attn_rope.hip", "attn_cache.hip",
+                                                         "attn_paged.hip")]
 LIB_PATH = os.path.join(HERE, "libmi355attn.so")
 MARSHAL_SOURCE = os.path.join(HERE, "csrc", "marshal.cpp")
 MARSHAL_PATH = os.path.join(HERE, "_marshal.so")
@@ -65,7 +67,20 @@ def _hipcc():
 
 
 def _compile(lib_path, extra, verbose):
-    return _run_compiler([_hipcc()] + HIPCC_FLAGS + extra, SOURCES, [], lib_path, verbose)
+    """Every source to an object, side by side, then the library."""
+    flags = [f for f in HIPCC_FLAGS if f != "-shared"] + extra
+    objects = ["%s.%s.%d.o" % (lib_path, os.path.basename(src), os.getpid()) for src in SOURCES]
+    try:
+        with ThreadPoolExecutor(max_workers=4) as pool:
+            jobs = [pool.submit(_run_compiler, [_hipcc()] + flags + ["-c"], [src], [], obj, verbose)
+                    for src, obj in zip(SOURCES, objects)]
+            for job in jobs:
+                job.result()
+        return _run_compiler([_hipcc(), "--offload-arch=gfx950", "-fPIC", "-shared"], objects, [], lib_path, verbose)
+    finally:
+        for obj in objects:
+            if os.path.exists(obj):
+                os.remove(obj)
 
 
 def _compile_marshal(verbose):

@@ -1,0 +1,157 @@
+"""How a call over the paged cache is cut into units (csrc/attn_paged_plan.h), on the host: the device code runs as 64
+coroutines (wave_host).  Every row tile and every key of every sequence belongs to exactly one unit, the units fit the launch and
+the workspace, and whatever the arrays of lengths hold, nothing points outside."""
+import ctypes
+import os
+import random
+import subprocess
+
+import numpy as np
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+CSRC = os.path.join(os.path.dirname(HERE), "paper_2512_18134_amd", "csrc")
+FIELDS = ("b", "h", "tile", "range", "n_ranges", "n_tiles", "row0", "n_rows", "n", "kv", "key0", "key1", "slot0", "slot")
+ALL = 0x7fffffff
+
+
+@pytest.fixture(scope="module")
+def lib(tmp_path_factory):
+    so = str(tmp_path_factory.mktemp("plan") / "plan.so")
+    subprocess.run(["/opt/rocm/bin/amdclang++", "-x", "c++", "-std=c++17", "-O1", "-fPIC", "-shared",
+                    "-I" + os.path.join(HERE, "wave_host"), "-I" + CSRC, "-o", so,
+                    os.path.join(HERE, "wave_host", "paged_plan.cpp")], check=True)
+    return ctypes.CDLL(so)
+
+
+def ints(a):
+    return np.ascontiguousarray(a, dtype=np.int32)
+
+
+def ptr(a):
+    return a.ctypes.data_as(ctypes.c_void_p)
+
+
+def plan(lib, start, kv_len, T, H_kv, G, BM, width, page_log2=4, above=0, upto=ALL, target=512, min_range=2, n_slots=None):
+    B = len(kv_len)
+    n_slots = 2 * target + 64 if n_slots is None else n_slots
+    n_wg = (T * G // BM + min(B, T)) * H_kv + target + 64        # the launch's own bound
+    start, kv_len = ints(start), ints(kv_len)
+    table = np.zeros((B, width), np.int32)
+    units = np.zeros((n_wg, 14), np.int32)
+    notes = np.full((T + 2, 4), -77, np.int32)                    # a guard row on either side
+    n = lib.plan_batch(ptr(table), ptr(start), ptr(kv_len), T, B, H_kv, 1, page_log2, width, G, BM, above, upto, target,
+                       min_range, n_slots, n_wg, ptr(units), ctypes.c_void_p(notes.ctypes.data + 16))
+    assert n >= 0
+    assert (notes[0] == -77).all() and (notes[-1] == -77).all()
+    return [dict(zip(FIELDS, map(int, u))) for u in units[:n]], notes[1:-1], n_wg, n_slots
+
+
+CASES = [
+    dict(news=[1], kvs=[1], H=1, G=1, BM=16),
+    dict(news=[1], kvs=[1000], H=16, G=1, BM=16),
+    dict(news=[1] * 64, kvs=[17 * i + 1 for i in range(64)], H=2, G=4, BM=16),
+    dict(news=[1] * 65, kvs=[13 * i + 1 for i in range(65)], H=2, G=3, BM=16),
+    dict(news=[0, 5, 0, 7, 1, 0], kvs=[0, 900, 30, 7, 5000, 0], H=3, G=5, BM=32),
+    dict(news=[40, 1, 300], kvs=[40, 20000, 2300], H=2, G=3, BM=64),
+    dict(news=[3, 2], kvs=[0, 1], H=2, G=1, BM=16),                    # rows below position 0
+    dict(news=[1] * 200, kvs=[131072] + [40] * 199, H=1, G=8, BM=16),  # one long sequence among short ones
+    dict(news=[700], kvs=[131072], H=1, G=4, BM=256),
+    dict(news=[0, 0], kvs=[5, 6], H=4, G=2, BM=16),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "B%d_H%d_G%d_BM%d" % (len(c["news"]), c["H"], c["G"], c["BM"]))
+@pytest.mark.parametrize("front, behind", [(0, 0), (3, 4)])
+def test_units_cover_every_row_and_key_once(lib, case, front, behind):
+    news, kvs, H, G, BM = (case[k] for k in ("news", "kvs", "H", "G", "BM"))
+    start = front + np.concatenate([[0], np.cumsum(news)])
+    T = max(1, int(start[-1]) + behind)
+    width = max(1, -(-max(kvs) // 16))
+    units, notes, n_wg, n_slots = plan(lib, start, kvs, T, H, G, BM, width)
+    seen, slots = {}, set()
+    for u in units:
+        b = u["b"]
+        assert u["n"] == news[b] and u["kv"] == kvs[b] and u["row0"] == start[b] and u["n_rows"] == news[b] * G
+        assert u["n_tiles"] == -(-news[b] * G // BM) and 0 <= u["tile"] < u["n_tiles"] and 0 <= u["h"] < H
+        key = (b, u["h"], u["tile"])
+        assert (u["key0"], u["key1"]) not in seen.get(key, [])
+        seen.setdefault(key, []).append((u["key0"], u["key1"]))
+        if u["n_ranges"] > 1:
+            assert 0 <= u["slot"] < n_slots and u["slot"] not in slots
+            assert u["slot"] == u["slot0"] + (u["range"] * H + u["h"]) * u["n_tiles"] + u["tile"]     # where the merge looks
+            slots.add(u["slot"])
+    want = {(b, h, t) for b in range(len(news)) for h in range(H) for t in range(-(-news[b] * G // BM))}
+    assert set(seen) == want
+    for (b, _, _), ranges in seen.items():
+        ranges.sort()
+        assert ranges[0][0] == 0 and ranges[-1][1] == kvs[b]
+        assert all(x[1] == y[0] for x, y in zip(ranges, ranges[1:]))
+        assert all(x[0] % 64 == 0 for x in ranges)
+    # notes: exactly the tokens of the batch, with their sequence's slots
+    of = {u["b"]: u for u in units}
+    for t in range(T):
+        b = int(np.searchsorted(start, t, side="right")) - 1
+        if t < start[0] or t >= start[-1]:
+            assert (notes[t] == -77).all()
+        else:
+            u = of[b]
+            first = (t - start[b]) * G if u["n_ranges"] > 1 else -1
+            assert list(notes[t]) == [u["slot0"], u["n_tiles"], u["n_ranges"], first]
+
+
+def test_two_kernels_share_a_batch(lib):
+    news, kvs = [1, 40, 2, 500], [3000, 3040, 70, 500]
+    start = np.concatenate([[0], np.cumsum(news)])
+    rows, _, _, _ = plan(lib, start, kvs, int(start[-1]), 2, 4, 64, 200, above=0, upto=64)
+    tiles, _, _, _ = plan(lib, start, kvs, int(start[-1]), 2, 4, 128, 200, above=64)
+    assert {u["b"] for u in rows} == {0, 2} and {u["b"] for u in tiles} == {1, 3}
+
+
+def test_a_long_sequence_is_shared_out(lib):
+    units, _, _, _ = plan(lib, list(range(9)), [131072] + [64] * 7, 8, 8, 4, 16, 8192)
+    longest = max(u["key1"] - u["key0"] for u in units)
+    assert longest <= 131072 * 8 // 512 + 128        # its share of 512 units, to a block
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_arrays_that_make_no_sense_stay_in_bounds(lib, seed):
+    rng = random.Random(seed)
+    B, T, H, G, BM = rng.choice([1, 5, 70, 130]), rng.choice([1, 9, 300]), 2, 3, rng.choice([16, 64, 256])
+    wild = lambda lo, hi: rng.choice([rng.randint(lo, hi), rng.randint(-2 ** 31, 2 ** 31 - 1), 2 ** 31 - 1, -2 ** 31, 0])
+    start = [wild(0, T) for _ in range(B + 1)]
+    kvs = [wild(0, 5000) for _ in range(B)]
+    units, _, _, n_slots = plan(lib, start, kvs, T, H, G, BM, 64, target=64)
+    for u in units:
+        assert 0 <= u["b"] < B and 0 <= u["h"] < H and 0 <= u["tile"] < u["n_tiles"] and u["n"] > 0
+        assert 0 <= u["row0"] and u["row0"] + u["n"] <= T and u["n_rows"] == u["n"] * G
+        assert 0 <= u["key0"] <= u["key1"] <= u["kv"] <= 64 * 16
+        assert u["n_ranges"] == 1 or 0 <= u["slot"] < n_slots
+
+
+@pytest.mark.parametrize("B", [1, 2, 63, 64, 65, 200, 5000])
+def test_sequence_of_a_row(lib, B):
+    rng = random.Random(B)
+    news = [rng.choice([0, 0, 1, 1, 2, 9]) for _ in range(B)]
+    start = ints(2 + np.concatenate([[0], np.cumsum(news)]))
+    T = int(start[-1]) + 3
+    for t in [0, 1, 2, T - 4, T - 3, T - 1] + [rng.randrange(T) for _ in range(60)]:
+        got = lib.sequence_of(ptr(start), T, B, t)
+        inside = start[0] <= t < start[-1]
+        assert got == (int(np.searchsorted(start, t, side="right")) - 1 if inside else -1), t
+    wild = ints([rng.randint(-2 ** 31, 2 ** 31 - 1) for _ in range(B + 1)])
+    for t in range(0, T, max(1, T // 20)):
+        assert -1 <= lib.sequence_of(ptr(wild), T, B, t) < B
+
+
+@pytest.mark.parametrize("page_log2", [4, 6, 8])
+def test_pages_outside_the_pool_are_no_pages(lib, page_log2):
+    table = ints([[0, 6, 7, -1, 2 ** 31 - 1, -2 ** 31, 3]])
+    length = ctypes.c_int()
+    for kv, most in ((5, 5), (-3, 0), (2 ** 31 - 1, 7 << page_log2), (7 << page_log2, 7 << page_log2)):
+        kv_len = ints([kv])
+        for i, want in enumerate([0, 6, -1, -1, -1, -1, 3]):
+            for pos in (i << page_log2, (i + 1 << page_log2) - 1):
+                got = lib.page_of(ptr(table), ptr(kv_len), 0, 7, page_log2, 7, pos, ctypes.byref(length))
+                assert length.value == most
+                assert got == (want if pos < most else -2)
