@@ -103,7 +103,7 @@ _marshal_module = None
 
 class _NotBuilt:
     """In place of the extension module: every call is handed back."""
-    fwd = splitkv = bwd = staticmethod(lambda *args: None)
+    fwd = splitkv = bwd = rope = write = read = paged = staticmethod(lambda *args: None)
 
 
 def _native():
@@ -120,6 +120,9 @@ def _native():
                            address(_lib.attn_fwd_splitkv_workspace_bytes),
                            getattr(torch._C, "_cuda_getCurrentRawStream",
                                    lambda index: torch.cuda.current_stream(index).cuda_stream))
+        module.set_serving_entries(*(address(getattr(_lib, name + suffix))
+                                     for name in ("attn_rope", "attn_cache_write", "attn_cache_read", "attn_paged_fwd")
+                                     for suffix in ("", "_f16")), address(_lib.attn_paged_fwd_workspace_bytes))
         _marshal_module = module
     return _marshal_module
 
@@ -453,12 +456,18 @@ def attn_rope(q, k, pos, freq, sections, q_out=None, k_out=None, interleaved=Fal
     inverse=True turns back: with the gradients of the outputs in place of q and k it gives the gradients of the inputs.
     Asynchronous on `stream`.  Returns (q_out, k_out).
     """
+    r = (_marshal_module or _native()).rope(0, q, k, pos, freq, sections, q_out, k_out, interleaved, inverse, stream)
+    if r is not None:
+        return _finish(r)
     import torch
     return _marshal_rope(_lib.attn_rope, torch.bfloat16, q, k, pos, freq, sections, q_out, k_out, interleaved, inverse, stream)
 
 
 def attn_rope_f16(q, k, pos, freq, sections, q_out=None, k_out=None, interleaved=False, inverse=False, stream=None):
     """attn_rope_f16 on torch device tensors: as attn_rope, with fp16 tensors."""
+    r = (_marshal_module or _native()).rope(1, q, k, pos, freq, sections, q_out, k_out, interleaved, inverse, stream)
+    if r is not None:
+        return _finish(r)
     import torch
     return _marshal_rope(_lib.attn_rope_f16, torch.float16, q, k, pos, freq, sections, q_out, k_out, interleaved, inverse, stream)
 
@@ -537,6 +546,9 @@ def attn_cache_write(k, v, k_pages, v_pages, page_table, start, kv_len, k_scale=
     kv_len int32 [B]: rows start[b] .. start[b+1]-1 become the last positions below kv_len[b] of sequence b.
     Asynchronous on `stream`.  Returns (k_pages, v_pages).
     """
+    r = (_marshal_module or _native()).write(0, k, v, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale, stream)
+    if r is not None:
+        return _finish(r)
     import torch
     _marshal_rows(_lib.attn_cache_write, torch.bfloat16, k, v, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale,
                   stream)
@@ -545,6 +557,9 @@ def attn_cache_write(k, v, k_pages, v_pages, page_table, start, kv_len, k_scale=
 
 def attn_cache_write_f16(k, v, k_pages, v_pages, page_table, start, kv_len, k_scale=None, v_scale=None, stream=None):
     """attn_cache_write_f16 on torch device tensors: as attn_cache_write, with fp16 rows (and fp16 or e4m3 pages)."""
+    r = (_marshal_module or _native()).write(1, k, v, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale, stream)
+    if r is not None:
+        return _finish(r)
     import torch
     _marshal_rows(_lib.attn_cache_write_f16, torch.float16, k, v, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale,
                   stream)
@@ -558,6 +573,10 @@ def attn_cache_read(k_pages, v_pages, page_table, start, kv_len, n_rows, k_scale
     elements: [H_kv,n_rows,D] tensors transposed are what attn_fwd takes).  Rows of no sequence are left as they were.  The
     cache's arguments are those of attn_cache_write.  Asynchronous on `stream`.  Returns (k, v).
     """
+    r = (_marshal_module or _native()).read(0, k_pages, v_pages, page_table, start, kv_len, n_rows, k_scale, v_scale, k, v,
+                                            stream)
+    if r is not None:
+        return _finish(r)
     import torch
     return _read(_lib.attn_cache_read, torch.bfloat16, k_pages, v_pages, page_table, start, kv_len, n_rows, k_scale, v_scale, k,
                  v, stream)
@@ -566,6 +585,10 @@ def attn_cache_read(k_pages, v_pages, page_table, start, kv_len, n_rows, k_scale
 def attn_cache_read_f16(k_pages, v_pages, page_table, start, kv_len, n_rows, k_scale=None, v_scale=None, k=None, v=None,
                         stream=None):
     """attn_cache_read_f16 on torch device tensors: as attn_cache_read, with fp16 rows."""
+    r = (_marshal_module or _native()).read(1, k_pages, v_pages, page_table, start, kv_len, n_rows, k_scale, v_scale, k, v,
+                                            stream)
+    if r is not None:
+        return _finish(r)
     import torch
     return _read(_lib.attn_cache_read_f16, torch.float16, k_pages, v_pages, page_table, start, kv_len, n_rows, k_scale, v_scale,
                  k, v, stream)
@@ -620,6 +643,10 @@ def attn_paged_fwd(q, k_pages, v_pages, page_table, start, kv_len, k_scale=None,
     causal: row i of n_b sees the keys up to its own position, otherwise all kv_len[b] of them.  max_q: the largest n_b (or
     an upper bound; T when not given), which chooses the kernels.  Asynchronous on `stream`.  Returns (o, lse).
     """
+    r = (_marshal_module or _native()).paged(0, q, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale, o, lse,
+                                             workspace, causal, scale, max_q, stream)
+    if r is not None:
+        return _finish(r)
     import torch
     return _marshal_paged(_lib.attn_paged_fwd, torch.bfloat16, q, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale,
                           o, lse, workspace, causal, scale, max_q, stream)
@@ -628,6 +655,10 @@ def attn_paged_fwd(q, k_pages, v_pages, page_table, start, kv_len, k_scale=None,
 def attn_paged_fwd_f16(q, k_pages, v_pages, page_table, start, kv_len, k_scale=None, v_scale=None, o=None, lse=None,
                        workspace=None, causal=True, scale=None, max_q=None, stream=None):
     """attn_paged_fwd_f16 on torch device tensors: as attn_paged_fwd, with fp16 q and o (and fp16 or e4m3 pages)."""
+    r = (_marshal_module or _native()).paged(1, q, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale, o, lse,
+                                             workspace, causal, scale, max_q, stream)
+    if r is not None:
+        return _finish(r)
     import torch
     return _marshal_paged(_lib.attn_paged_fwd_f16, torch.float16, q, k_pages, v_pages, page_table, start, kv_len, k_scale,
                           v_scale, o, lse, workspace, causal, scale, max_q, stream)

@@ -336,3 +336,44 @@ def test_refusals():
     odd = [torch.zeros(3, 2, 48, 64, dtype=torch.bfloat16, device="cuda") for _ in "kv"]
     with pytest.raises(M.AttnError):
         M.attn_paged_fwd(q, *odd, *args[2:])
+
+
+def test_both_ways_of_the_binding_take_the_same_calls():
+    """csrc/marshal.cpp for plain calls, Python for the rest: a `causal` or `interleaved` that is no bool, a scale or an int of
+    another type sends a call the Python way."""
+    from paper_2512_18134_amd import binding as M
+    if M._native() is M._NotBuilt:
+        pytest.skip("the extension module was left out of this build")
+    same = lambda a, b: all(torch.equal(x, y) and x.dtype == y.dtype and x.shape == y.shape for x, y in zip(a, b))
+    for dt, e4m3 in (("bf16", False), ("f16", True)):
+        i = int(dt == "f16")
+        c = Cache([3, 1, 40], [300, 64, 40], 2, 64, 16, dt, e4m3, 51)
+        args, scales = c.on_gpu()
+        s = (scales["k_scale"], scales["v_scale"])
+        k, v, q = (c.rows(h).cuda() for h in (2, 2, 6))
+        native = M._native()
+        slow = lambda name, *a, **kw: getattr(M, name)(getattr(M._lib, "attn_" + kw.pop("entry") + ("_f16" if i else "")),
+                                                       R.DT[dt], *a)
+        before = [t.clone() for t in args[:2]]
+        slow("_marshal_rows", k, v, *args, *s, None, entry="cache_write")
+        one = [t.clone() for t in args[:2]]
+        for t, b in zip(args[:2], before):
+            t.copy_(b)
+        assert native.write(i, k, v, *args, *s, None)[0] is args[0]
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(one, args[:2]))
+        assert same(native.read(i, *args, c.T, *s, None, None, None), slow("_read", *args, c.T, *s, None, None, None,
+                                                                           entry="cache_read"))
+        for causal in (True, False):
+            fast = native.paged(i, q, *args, *s, None, None, None, causal, None, 40, None)
+            assert same(fast, slow("_marshal_paged", q, *args, *s, None, None, None, causal, None, 40, None, entry="paged_fwd"))
+        rq, rk = q.transpose(0, 1)[None], k.transpose(0, 1)[None]
+        pos = torch.arange(c.T, dtype=torch.int32, device="cuda")[None, None]
+        freq = torch.rand(32, dtype=torch.float64, device="cuda")
+        fast = native.rope(i, rq, rk, pos, freq, (32,), None, None, False, True, None)
+        assert same(fast, slow("_marshal_rope", rq, rk, pos, freq, (32,), None, None, False, True, None, entry="rope"))
+        # handed back: other types, overlapping outputs, another stream's allocation
+        assert native.write(i, k.float(), v, *args, *s, None) is None
+        assert native.read(i, *args, c.T, *s, k[:1].expand(c.T, 2, 64), v, None) is None
+        assert native.paged(i, q, *args, *s, None, None, None, 1, None, 40, None) is None
+        assert native.paged(i, q, *args, *s, None, None, None, True, None, None, torch.cuda.Stream()) is None
+        assert native.rope(i, rq, None, pos, freq, (32,), None, None, False, True, None) is None
