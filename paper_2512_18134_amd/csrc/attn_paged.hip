@@ -5,38 +5,40 @@
 
 #include "attn_cache.h"
 #include "attn_fwd.h"
-#include "attn_paged_rows.h"
+#include "attn_launch.h"
+#include "attn_paged_tiles.h"
 
 namespace attn {
 
-// What the chip holds at once: two workgroups of the row kernel on each of 256 compute units.
-constexpr int kRowTarget = 512;
-// A range of fewer keys than this costs more to merge than its walk by other workgroups saves.
-constexpr int kRowMinRange = 2;                        // blocks of kPlanBlock keys
+// What the chip holds at once: two workgroups of either kernel on each of 256 compute units.
+constexpr int kTarget = 512;
+// A range of fewer blocks (of kPlanBlock keys) costs more to merge than its walk by another workgroup saves.
+constexpr int kRowsMinRange = 2, kTilesMinRange = 4;
+constexpr int kSlots = 2 * kTarget + 64;
 
-constexpr long long kSlack = 64;                       // units and slots that rounding can add
-
-// 16-row tiles of a workgroup: as few as hold a sequence's rows, up to what the registers hold
-inline int row_tiles(int D, long long rows)
-{
-    return rows <= 16 ? 1 : rows <= 32 || D == 256 ? 2 : 4;
-}
+// rows of a sequence up to which the row kernel takes it
+constexpr int rows_kernel_most(int D) { return D == 256 ? 32 : 64; }
+// 16-row tiles of its workgroup: as few as hold the rows
+inline int row_tiles(int D, long long rows) { return rows <= 16 ? 1 : rows <= 32 || D == 256 ? 2 : 4; }
 
 struct Workspace {
-    long long slots, part_o, part_lse, merge, bytes;   // offsets in bytes
+    long long part_o[2], part_lse[2], merge, bytes;   // offsets in bytes
 };
 
-// Any BM the entry point may choose fits: the slots' rows are what it is laid out for.
-inline Workspace workspace_of(int T, int D)
+inline Workspace workspace_of(int T, int G, int D)
 {
-    constexpr long long kMaxRows = 64;
     Workspace w;
-    // a sequence of two ranges or more has at most twice its share of the target's units
-    w.slots = 2 * kRowTarget + kSlack;
-    w.part_o = 0;
-    w.part_lse = w.slots * kMaxRows * D * 4;
-    w.merge = w.part_lse + w.slots * kMaxRows * 4;
-    w.bytes = w.merge + (long long)T * (long long)sizeof(MergeNote);
+    long long at = 0;
+    for (int kernel = 0; kernel < 2; ++kernel) {
+        const long long rows = kernel ? (D == 256 ? 128 : 256) : rows_kernel_most(D);
+        const long long slots = kernel && (long long)T * G <= rows_kernel_most(D) ? 0 : kSlots;
+        w.part_o[kernel] = at;
+        at += slots * rows * D * 4;
+        w.part_lse[kernel] = at;
+        at += slots * rows * 4;
+    }
+    w.merge = at;
+    w.bytes = at + (long long)T * (long long)sizeof(MergeNote);
     return w;
 }
 
@@ -48,41 +50,79 @@ using attn::PagedParams;
 
 bool misaligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
-template <int D, int MT, typename E, bool E4M3>
-int launch_rows(PagedParams &p, hipStream_t st)
+// Workgroups that a kernel of tiles of BM rows may have units for: a sequence's tiles are at most one more than its rows
+// fill; the ranges' share of the target is twice the target where causal rows see half, and one more for every tile.
+long long most_units(const PagedParams &p, int BM)
 {
-    constexpr int BM = 16 * MT;
-    // sequences' tiles are at most one more than their rows fill, ranges at most one more than their share of the target
     const long long tiles = (long long)p.c.T * p.G / BM + (p.c.B < p.c.T ? p.c.B : p.c.T);
-    const long long grid = tiles * p.c.H_kv + p.target + attn::kSlack;
+    return tiles * p.c.H_kv + 2 * p.target + 64;
+}
+
+template <int D, int MT, typename E, bool E4M3>
+int launch_rows(PagedParams p, int upto, hipStream_t st)
+{
+    p.kernel = 0, p.rows_above = 0, p.rows_upto = upto;
+    p.target = attn::kTarget, p.min_range = attn::kRowsMinRange;
+    const long long grid = most_units(p, 16 * MT);
     if (grid > 0x7fffffffLL)
         return ATTN_ERR_SHAPE;
     hipLaunchKernelGGL((attn::attn_paged_rows_kernel<D, MT, E, E4M3>), dim3((unsigned)grid), dim3(256), 0, st, p);
-    if (hipGetLastError() != hipSuccess)
-        return ATTN_ERR_LAUNCH;
-    // no sequence can be longer than one range: nothing to merge
-    if (((long long)p.c.table_width << p.c.page_log2) <= (long long)p.min_range * attn::kPlanBlock)
-        return ATTN_OK;
-    const long long blocks = ((long long)p.c.T * p.H_q * (D / 4) + 255) / 256;
-    if (blocks > 0x7fffffffLL)
+    return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH;
+}
+
+template <int D, typename E, bool E4M3>
+int launch_rows(const PagedParams &p, int MT, int upto, hipStream_t st)
+{
+    if (MT == 1)
+        return launch_rows<D, 1, E, E4M3>(p, upto, st);
+    if constexpr (D != 256)
+        if (MT == 4)
+            return launch_rows<D, 4, E, E4M3>(p, upto, st);
+    return launch_rows<D, 2, E, E4M3>(p, upto, st);
+}
+
+template <int D, typename E, bool E4M3>
+int launch_tiles(PagedParams p, int above, hipStream_t st)
+{
+    typedef attn::PagedTilesTiling<D, E4M3> T;
+    p.kernel = 1, p.rows_above = above, p.rows_upto = 0x7fffffff;
+    p.target = attn::kTarget, p.min_range = attn::kTilesMinRange;
+    const long long grid = most_units(p, T::BM);
+    const void *kern = reinterpret_cast<const void *>(attn::attn_paged_tiles_kernel<D, E, E4M3>);
+    if (grid > 0x7fffffffLL)
         return ATTN_ERR_SHAPE;
-    hipLaunchKernelGGL((attn::attn_paged_merge_kernel<D, typename E::t>), dim3((unsigned)blocks), dim3(256), 0, st, p, BM);
+    if (!attn::allow_lds(kern, T::LDS_BYTES))
+        return ATTN_ERR_LAUNCH;
+    hipLaunchKernelGGL((attn::attn_paged_tiles_kernel<D, E, E4M3>), dim3((unsigned)grid), dim3(T::THREADS), T::LDS_BYTES, st, p);
     return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH;
 }
 
 template <int D, typename E, bool E4M3>
 int launch(PagedParams &p, int max_q, hipStream_t st)
 {
-    p.rows_above = 0, p.rows_upto = 0x7fffffff;
-    p.target = attn::kRowTarget, p.min_range = attn::kRowMinRange;
-    switch (attn::row_tiles(D, (long long)max_q * p.G)) {
-    case 1: return launch_rows<D, 1, E, E4M3>(p, st);
-    case 2: return launch_rows<D, 2, E, E4M3>(p, st);
-    default:
-        if constexpr (D != 256)
-            return launch_rows<D, 4, E, E4M3>(p, st);
-        return ATTN_ERR_UNSUPPORTED;
-    }
+    // Sequences of few rows and of many may be in one batch; each kernel takes its own.  One launch where max_q, or a
+    // single sequence, says that there is one kind (and then for whatever the batch holds).
+    const int most = attn::rows_kernel_most(D);
+    const long long rows = (long long)(max_q < p.c.T ? max_q : p.c.T) * p.G;
+    const bool few = rows <= most, many = !few, both = many && p.c.B > 1;
+    const int MT = attn::row_tiles(D, rows < most ? rows : most);
+    p.parts[0].BM = 16 * MT, p.parts[1].BM = attn::PagedTilesTiling<D, E4M3>::BM;
+    int rc = ATTN_OK;
+    if (few || both)
+        rc = launch_rows<D, E, E4M3>(p, MT, both ? most : 0x7fffffff, st);
+    if (rc == ATTN_OK && many)
+        rc = launch_tiles<D, E, E4M3>(p, both ? most : 0, st);
+    // no sequence can be longer than one range: nothing to merge
+    const int shortest = few ? attn::kRowsMinRange : both && attn::kRowsMinRange < attn::kTilesMinRange ? attn::kRowsMinRange
+                                                                                                         : attn::kTilesMinRange;
+    if (rc != ATTN_OK || ((long long)p.c.table_width << p.c.page_log2) <= (long long)shortest * attn::kPlanBlock)
+        return rc;
+    constexpr int kGroups = 256 / (D / 4);
+    const long long o_rows = (long long)p.c.T * p.H_q;
+    const int walkers = o_rows <= 4096 ? kGroups : 1;
+    const long long blocks = (o_rows * walkers + kGroups - 1) / kGroups;
+    hipLaunchKernelGGL((attn::attn_paged_merge_kernel<D, typename E::t>), dim3((unsigned)blocks), dim3(256), 0, st, p, walkers);
+    return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH;
 }
 
 template <typename E>
@@ -101,7 +141,7 @@ int paged_fwd(const void *q, const long long *strides, void *o, float *lse, cons
     if ((kind != ATTN_CACHE_16BIT && kind != ATTN_CACHE_E4M3) || page_size < 16 || page_size > 256 ||
         (page_size & (page_size - 1)))
         return ATTN_ERR_UNSUPPORTED;
-    if ((long long)T * H_q > 0x7fffffffLL || (long long)n_pages * H_kv > (1LL << 40) / D / page_size || H_kv > (1 << 24) ||
+    if ((long long)T * H_q > 0x3fffffffLL || (long long)n_pages * H_kv > (1LL << 40) / D / page_size || H_kv > (1 << 24) ||
         (long long)table_width * page_size > (1 << 30))
         return ATTN_ERR_SHAPE;
     for (int i = 0; i < 2; ++i) {
@@ -115,7 +155,7 @@ int paged_fwd(const void *q, const long long *strides, void *o, float *lse, cons
         return ATTN_ERR_ALIGN;
     if (!(scale > 0.f) || !(scale < INFINITY))
         return ATTN_ERR_SCALE;
-    const attn::Workspace w = attn::workspace_of(T, D);
+    const attn::Workspace w = attn::workspace_of(T, H_q / H_kv, D);
     if (workspace_bytes < w.bytes)
         return ATTN_ERR_WORKSPACE;
     PagedParams p;
@@ -128,9 +168,11 @@ int paged_fwd(const void *q, const long long *strides, void *o, float *lse, cons
     p.causal = causal != 0;
     p.c_log2 = (float)((double)scale * 1.44269504088896340736);
     unsigned char *const ws = static_cast<unsigned char *>(workspace);
-    p.n_slots = (int)w.slots;
-    p.part_o = reinterpret_cast<float *>(ws + w.part_o);
-    p.part_lse = reinterpret_cast<float *>(ws + w.part_lse);
+    for (int kernel = 0; kernel < 2; ++kernel) {
+        p.parts[kernel].o = reinterpret_cast<float *>(ws + w.part_o[kernel]);
+        p.parts[kernel].lse = reinterpret_cast<float *>(ws + w.part_lse[kernel]);
+        p.parts[kernel].slots = w.part_o[kernel] == w.part_lse[kernel] ? 0 : attn::kSlots;
+    }
     p.merge = reinterpret_cast<attn::MergeNote *>(ws + w.merge);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const bool e4m3 = kind == ATTN_CACHE_E4M3;
@@ -146,9 +188,9 @@ int paged_fwd(const void *q, const long long *strides, void *o, float *lse, cons
 extern "C" long long attn_paged_fwd_workspace_bytes(int T, int B, int H_q, int H_kv, int D)
 {
     if (T < 1 || B < 1 || H_q < 1 || H_kv < 1 || H_q % H_kv || (D != 64 && D != 128 && D != 256) ||
-        (long long)T * H_q > 0x7fffffffLL)
+        (long long)T * H_q > 0x3fffffffLL)
         return -1;
-    return attn::workspace_of(T, D).bytes;
+    return attn::workspace_of(T, H_q / H_kv, D).bytes;
 }
 
 extern "C" int attn_paged_fwd(const void *q, const long long *strides, void *o, float *lse, const void *k_pages,

@@ -10,6 +10,8 @@
 // sequence among short ones is walked by many workgroups.  A sequence of one range is finished by its unit;
 // the units of the others leave normalised fp32 rows and their log-sum-exp, which attn_paged_merge_kernel joins.
 #pragma once
+#include <type_traits>
+
 #include "attn_cache_rows.h"
 #include "attn_common.h"
 
@@ -30,14 +32,19 @@ struct PagedParams {
     float c_log2;                       // scale * log2(e)
     // units of this kernel: sequences of rows in (rows_above, rows_upto], cut for `target` units
     int rows_above, rows_upto, target, min_range;
-    int n_slots;                        // partial results that the workspace holds
-    float *part_o;                      // [n_slots][BM][D]
-    float *part_lse;                    // [n_slots][BM]
+    int kernel;                         // 0: attn_paged_rows.h, 1: attn_paged_tiles.h
+    // partial results, of either kernel
+    struct Parts {
+        float *o;                       // [slots][BM][D]
+        float *lse;                     // [slots][BM]
+        int slots, BM;
+    } parts[2];
     int4 *merge;                        // [T]: see MergeNote
 };
 
 // What the merge kernel needs to know of a token: x = first slot of its sequence, y = row tiles of the sequence,
-// z = its ranges, w = first row of the token in its sequence; w < 0 with z = 1: nothing to merge.
+// z = its ranges, w = first row of the token in its sequence * 2 + kernel.  Only sequences of several ranges have a
+// meaningful x and w.
 typedef int4 MergeNote;
 
 struct Unit {
@@ -48,23 +55,28 @@ struct Unit {
     int slot0, slot;                    // first slot of the sequence, slot of this unit (n_ranges > 1)
 };
 
-__device__ __forceinline__ int wave_sum(int x)
+// Inclusive prefix sum over the wave (the sum: lane 63), in the vector unit's own lane exchange: 16 lanes, then a row's
+// last lane to the next row and the first two rows' to the last two.  Through LDS (shuffles) the six steps of every
+// sum would take most of a microsecond of a launch that takes a few.
+template <typename T>
+__device__ __forceinline__ T wave_prefix(T x)
 {
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2)
-        x += __shfl_xor(x, m, 64);
+    auto from = [](T v, auto ctrl, auto rows) -> T {
+        return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
+    };
+    x += from(x, std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});   // row_shr 1
+    x += from(x, std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+    x += from(x, std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+    x += from(x, std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+    x += from(x, std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // row_bcast 15
+    x += from(x, std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // row_bcast 31
     return x;
 }
 
-__device__ __forceinline__ int wave_prefix(int x)   // inclusive
+template <typename T>
+__device__ __forceinline__ T wave_sum(T x)
 {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) {
-        const int y = __shfl_up(x, m, 64);
-        x += lane >= m ? y : 0;
-    }
-    return x;
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wave_prefix(x)), 63));
 }
 
 // Every wave of workgroup `wg` calls this; false: the launch has no unit for it.
@@ -90,37 +102,38 @@ __device__ __forceinline__ bool plan_unit(const PagedParams &p, int wg, Unit &u)
     };
     const bool one = p.c.B <= 64;
     Seq s = sequence(lane);
-    // work of the call, in (row tile, block, key head); more than 2^40 units of it cannot be
+    // work of the call, in (row tile, block, key head): of a causal chunk the rows see half of its own keys
     float work = 0.f;
     for (int b = 0;; b += 64) {
-        float w = (float)s.tiles * (float)s.blocks;
-#pragma unroll
-        for (int m = 1; m < 64; m *= 2)
-            w += __shfl_xor(w, m, 64);
-        work += w;
+        const float seen = (float)s.blocks - (p.causal ? (float)min(s.n, s.kv) * (0.5f / kPlanBlock) : 0.f);
+        work += wave_sum((float)s.tiles * fmaxf(seen, 1.f));
         if (b + 64 >= p.c.B)
             break;
         s = sequence(b + 64 + lane);
     }
-    // (a float is enough: the same one in every workgroup, and the margin of one block covers its rounding)
-    const float share = ceilf(work * (float)p.c.H_kv * (1.0f + 0x1p-20f) / (float)p.target);
-    const int L = max(p.min_range, (int)fminf(share, 0x1p25f));
-    // units and slots in front of every sequence
+    // (a float is enough: the same one in every workgroup, and the bounds below leave room for its rounding)
+    const float share = ceilf(work * (float)p.c.H_kv / (float)p.target);
+    int L = max(p.min_range, (int)fminf(share, 0x1p24f));
+    // units, and slots of those that are not alone in their sequence and row tile; longer ranges if the slots do not suffice
     auto ranges = [&](const Seq &x) { return x.tiles ? (x.blocks + L - 1) / L : 0; };
-    if (!one)
-        s = sequence(lane);
-    int total = 0;
-    if (one) {
-        total = wave_sum(s.tiles * ranges(s));
-    } else {
+    int total, held;
+    for (;; L *= 2) {
+        total = held = 0;
+        if (!one)
+            s = sequence(lane);
         for (int b = 0;; b += 64) {
-            total += wave_sum(s.tiles * ranges(s));
+            const int nr = ranges(s);
+            total += wave_sum(s.tiles * nr);
+            held += wave_sum(nr > 1 ? s.tiles * nr : 0);
             if (b + 64 >= p.c.B)
                 break;
             s = sequence(b + 64 + lane);
         }
-        s = sequence(lane);
+        if ((long long)held * p.c.H_kv <= p.parts[p.kernel].slots || L >= 1 << 24)
+            break;
     }
+    if (!one)
+        s = sequence(lane);
     total *= p.c.H_kv;
     if (wg >= total)
         return false;
@@ -128,8 +141,8 @@ __device__ __forceinline__ bool plan_unit(const PagedParams &p, int wg, Unit &u)
     int units0 = 0, slots0 = 0;
     for (int b = 0;; b += 64) {
         const int nr = ranges(s);
-        const int mine = s.tiles * nr * p.c.H_kv, held = nr > 1 ? mine : 0;
-        const int after = units0 + wave_prefix(mine), after_slots = slots0 + wave_prefix(held);
+        const int mine = s.tiles * nr * p.c.H_kv, kept = nr > 1 ? mine : 0;
+        const int after = units0 + wave_prefix(mine), after_slots = slots0 + wave_prefix(kept);
         const unsigned long long behind = __ballot(after > v);
         if (behind) {
             const int l = __ffsll(behind) - 1;
@@ -140,7 +153,7 @@ __device__ __forceinline__ bool plan_unit(const PagedParams &p, int wg, Unit &u)
             const int w = v - of(after - mine);
             if (w < 0 || w >= of(mine))        // starts that decrease can count more units than an int holds
                 return false;
-            u.slot0 = of(after_slots - held);
+            u.slot0 = of(after_slots - kept);
             u.slot = u.slot0 + w;
             u.tile = w % u.n_tiles;
             const int hr = w / u.n_tiles;
@@ -154,12 +167,16 @@ __device__ __forceinline__ bool plan_unit(const PagedParams &p, int wg, Unit &u)
             return false;
         s = sequence(b + 64 + lane);
     }
-    u.row0 = __builtin_amdgcn_readfirstlane(p.c.start_of(u.b));
     u.n_rows = u.n * p.G;
     u.key0 = min((long long)u.range * L * kPlanBlock, (long long)u.kv);
     u.key1 = min((long long)(u.range + 1) * L * kPlanBlock, (long long)u.kv);
+    // the same in all lanes: scalars from here on
+    auto scalar = [](int &x) { x = __builtin_amdgcn_readfirstlane(x); };
+    u.row0 = p.c.start_of(u.b);
+    scalar(u.row0), scalar(u.b), scalar(u.h), scalar(u.tile), scalar(u.range), scalar(u.key0), scalar(u.key1), scalar(u.slot0);
+    scalar(u.slot), scalar(u.n), scalar(u.kv), scalar(u.n_rows), scalar(u.n_tiles), scalar(u.n_ranges);
     // starts that decrease can count rows twice: a slot behind the workspace's last is not written
-    return u.n_ranges == 1 || (unsigned)u.slot < (unsigned)p.n_slots;
+    return u.n_ranges == 1 || (unsigned)u.slot < (unsigned)p.parts[p.kernel].slots;
 }
 
 // The first unit of every row tile tells the merge kernel about the tokens whose first row lies in the tile.
@@ -170,48 +187,54 @@ __device__ __forceinline__ void leave_note(const PagedParams &p, const Unit &u)
         return;
     const int first = (u.tile * BM + p.G - 1) / p.G, behind = min(((u.tile + 1) * BM + p.G - 1) / p.G, u.n);
     for (int i = first + threadIdx.x; i < behind; i += THREADS)
-        p.merge[u.row0 + i] = MergeNote{u.slot0, u.n_tiles, u.n_ranges, u.n_ranges > 1 ? i * p.G : -1};
+        p.merge[u.row0 + i] = MergeNote{u.slot0, u.n_tiles, u.n_ranges, i * p.G * 2 + p.kernel};
 }
 
-// Partial results -> o and lse.  A workgroup takes 256 / (D / 4) (token, query head) rows; D/4 lanes hold a row, four
-// elements each, and walk its ranges four at a time with their loads in flight together.
+// Partial results -> o and lse.  D/4 lanes hold a row (token, query head), four elements each; `walkers` such groups take
+// a row's ranges in turn, four at a time with their loads in flight together, and meet in LDS.  Few rows: a
+// workgroup to a row, for the bound is then the latency of the walk.  Many: a workgroup to as many rows as it holds, since
+// most of them will have nothing to merge.
 template <int D, typename OUT>
-__global__ __launch_bounds__(256) void attn_paged_merge_kernel(const PagedParams p, int BM)
+__global__ __launch_bounds__(256) void attn_paged_merge_kernel(const PagedParams p, int walkers)
 {
     constexpr int TPR = D / 4, U = 4;
-    const long long at = ((long long)blockIdx.x * 256 + threadIdx.x) / TPR;
-    const int sub = threadIdx.x % TPR;
-    if (at >= (long long)p.c.T * p.H_q)
-        return;
+    __shared__ f32x4 s_acc[256];
+    __shared__ f32x2 s_ml[256 / TPR];
+    const int group = threadIdx.x / TPR, sub = threadIdx.x % TPR, walker = group % walkers;
+    const long long at = (long long)blockIdx.x * (256 / TPR / walkers) + group / walkers;
     const int t = (int)(at / p.H_q), hq = (int)(at % p.H_q);
+    int n_ranges = 0, BM = 0;
+    long long slot = 0, step = 0;
+    const float *part_o = nullptr, *part_lse = nullptr;
     // a token of no sequence has no note: what lies there is old
-    if (t < p.c.start_of(0) || t >= p.c.start_of(p.c.B))
-        return;
-    const MergeNote note = p.merge[t];
-    const int n_tiles = note.y, n_ranges = note.z;
-    if (n_ranges <= 1 || note.w < 0 || n_tiles < 1)
-        return;
-    const int row = note.w + hq % p.G, h = hq / p.G;
-    const int tile = row / BM, in_tile = row % BM;
-    const long long step = (long long)p.c.H_kv * n_tiles;
-    const long long slot = note.x + (long long)h * n_tiles + tile;
-    if (note.x < 0 || tile >= n_tiles || n_ranges > p.n_slots || slot + (n_ranges - 1) * step >= p.n_slots)
-        return;
+    if (at < (long long)p.c.T * p.H_q && t >= p.c.start_of(0) && t < p.c.start_of(p.c.B)) {
+        const MergeNote note = p.merge[t];
+        const PagedParams::Parts &part = p.parts[note.w & 1];
+        const int row = (note.w >> 1) + hq % p.G, n_tiles = note.y;
+        BM = part.BM, part_o = part.o, part_lse = part.lse;
+        if (note.z > 1 && note.z <= part.slots && n_tiles >= 1 && row >= 0 && BM > 0 && row / BM < n_tiles && note.x >= 0) {
+            step = (long long)p.c.H_kv * n_tiles;
+            slot = note.x + (long long)(hq / p.G) * n_tiles + row / BM;
+            n_ranges = slot + (note.z - 1) * step < part.slots ? note.z : 0;
+            slot = slot * BM + row % BM;
+            step *= BM;
+        }
+    }
     float m = -INFINITY, sum = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < n_ranges; s0 += U) {
+    for (int s0 = walker; s0 < n_ranges; s0 += U * walkers) {
         float l[U];
         f32x4 x[U];
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            const long long k = (slot + min(s0 + i, n_ranges - 1) * step) * BM + in_tile;
-            l[i] = p.part_lse[k];
-            x[i] = *reinterpret_cast<const f32x4 *>(p.part_o + k * D + 4 * sub);
+            const long long k = slot + min(s0 + i * walkers, n_ranges - 1) * step;
+            l[i] = part_lse[k];
+            x[i] = *reinterpret_cast<const f32x4 *>(part_o + k * D + 4 * sub);
         }
         float m_new = m;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            if (s0 + i >= n_ranges)
+            if (s0 + i * walkers >= n_ranges)
                 l[i] = -INFINITY;
             m_new = fmaxf(m_new, l[i]);
         }
@@ -222,12 +245,38 @@ __global__ __launch_bounds__(256) void attn_paged_merge_kernel(const PagedParams
         acc *= keep;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
+            if (l[i] == -INFINITY)  // its row of partial results was not written
+                continue;
             const float w = expf(l[i] - m_new);
             sum += w;
             acc += w * x[i];
         }
         m = m_new;
     }
+    if (walkers > 1) {
+        s_acc[threadIdx.x] = acc;
+        if (sub == 0)
+            s_ml[group] = f32x2{m, sum};
+        __syncthreads();
+        if (walker == 0) {
+            const float m_own = m;
+            for (int j = 1; j < walkers; ++j)
+                m = fmaxf(m, s_ml[group + j][0]);
+            const float keep = m_own == -INFINITY ? 0.f : expf(m_own - m);
+            sum *= keep;
+            acc *= keep;
+            for (int j = 1; j < walkers; ++j) {
+                const f32x2 ml = s_ml[group + j];
+                if (ml[0] == -INFINITY)
+                    continue;
+                const float w = expf(ml[0] - m);
+                sum += w * ml[1];
+                acc += w * s_acc[threadIdx.x + j * TPR];
+            }
+        }
+    }
+    if (n_ranges < 1 || walker != 0)
+        return;
     acc *= sum > 0.f ? 1.f / sum : 0.f;
     typedef OUT out4 __attribute__((ext_vector_type(4)));
     *reinterpret_cast<out4 *>(static_cast<OUT *>(p.o) + at * D + 4 * sub) = __builtin_convertvector(acc, out4);

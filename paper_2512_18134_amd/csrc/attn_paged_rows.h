@@ -360,11 +360,12 @@ __global__ __launch_bounds__(256, (MT == 1 && D <= 128) || (MT == 2 && D == 64) 
             const int first = part * NV + x * NX;
             if (u.n_ranges > 1) {
                 const size_t at = (size_t)u.slot * T::BM + 16 * m + r;
+                if (sum > 0.f)
 #pragma unroll
-                for (int n = 0; n < NX / 4; ++n)
-                    *reinterpret_cast<f32x4 *>(p.part_o + at * D + first + 4 * n) = y[n];
+                    for (int n = 0; n < NX / 4; ++n)
+                        *reinterpret_cast<f32x4 *>(p.parts[0].o + at * D + first + 4 * n) = y[n];
                 if (part == 0 && x == 0)
-                    p.part_lse[at] = lse;
+                    p.parts[0].lse[at] = lse;
             } else {
                 const size_t at = (size_t)(u.row0 + row / p.G) * p.H_q + u.h * p.G + row % p.G;
                 uint32_t *dst = reinterpret_cast<uint32_t *>(static_cast<typename E::t *>(p.o) + at * D + first);

@@ -32,16 +32,16 @@ def ptr(a):
     return a.ctypes.data_as(ctypes.c_void_p)
 
 
-def plan(lib, start, kv_len, T, H_kv, G, BM, width, page_log2=4, above=0, upto=ALL, target=512, min_range=2, n_slots=None):
+def plan(lib, start, kv_len, T, H_kv, G, BM, width, page_log2=4, above=0, upto=ALL, target=512, min_range=2, n_slots=None, causal=1):
     B = len(kv_len)
     n_slots = 2 * target + 64 if n_slots is None else n_slots
-    n_wg = (T * G // BM + min(B, T)) * H_kv + target + 64        # the launch's own bound
+    n_wg = (T * G // BM + min(B, T)) * H_kv + 2 * target + 64    # the launch's own bound
     start, kv_len = ints(start), ints(kv_len)
     table = np.zeros((B, width), np.int32)
     units = np.zeros((n_wg, 14), np.int32)
     notes = np.full((T + 2, 4), -77, np.int32)                    # a guard row on either side
     n = lib.plan_batch(ptr(table), ptr(start), ptr(kv_len), T, B, H_kv, 1, page_log2, width, G, BM, above, upto, target,
-                       min_range, n_slots, n_wg, ptr(units), ctypes.c_void_p(notes.ctypes.data + 16))
+                       min_range, n_slots, causal, n_wg, ptr(units), ctypes.c_void_p(notes.ctypes.data + 16))
     assert n >= 0
     assert (notes[0] == -77).all() and (notes[-1] == -77).all()
     return [dict(zip(FIELDS, map(int, u))) for u in units[:n]], notes[1:-1], n_wg, n_slots
@@ -96,8 +96,7 @@ def test_units_cover_every_row_and_key_once(lib, case, front, behind):
             assert (notes[t] == -77).all()
         else:
             u = of[b]
-            first = (t - start[b]) * G if u["n_ranges"] > 1 else -1
-            assert list(notes[t]) == [u["slot0"], u["n_tiles"], u["n_ranges"], first]
+            assert list(notes[t]) == [u["slot0"], u["n_tiles"], u["n_ranges"], (t - start[b]) * G * 2]
 
 
 def test_two_kernels_share_a_batch(lib):
@@ -112,6 +111,15 @@ def test_a_long_sequence_is_shared_out(lib):
     units, _, _, _ = plan(lib, list(range(9)), [131072] + [64] * 7, 8, 8, 4, 16, 8192)
     longest = max(u["key1"] - u["key0"] for u in units)
     assert longest <= 131072 * 8 // 512 + 128        # its share of 512 units, to a block
+
+
+@pytest.mark.parametrize("causal", [0, 1])
+def test_few_slots_make_longer_ranges(lib, causal):
+    units, _, _, n_slots = plan(lib, [0, 900, 900, 901], [5000, 77, 800], 901, 2, 4, 64, 400, n_slots=40, causal=causal)
+    assert len({u["slot"] for u in units if u["n_ranges"] > 1}) == sum(u["n_ranges"] > 1 for u in units)
+    assert all(u["n_ranges"] == 1 or u["slot"] < 40 for u in units) and {u["b"] for u in units} == {0, 2}
+    units, _, _, _ = plan(lib, [0, 900, 900, 901], [5000, 77, 800], 901, 2, 4, 64, 400, n_slots=0, causal=causal)
+    assert all(u["n_ranges"] == 1 for u in units)
 
 
 @pytest.mark.parametrize("seed", range(12))

@@ -107,6 +107,22 @@ inline unsigned long long __ballot(bool b)
     return r;
 }
 inline int __popcll(unsigned long long x) { return __builtin_popcountll(x); }
+inline void __syncthreads() {}
 inline int __ffsll(unsigned long long x) { return __builtin_ffsll(x); }
+// the lane exchanges that a prefix sum is made of: row_shr 1 .. 8, row_bcast 15 and 31; lanes without a source keep `old`
+inline int update_dpp(int old, int x, int ctrl, int rows, int, bool)
+{
+    const uint64_t *all = static_cast<uint64_t *>(wave_host::exchange((unsigned)x));
+    const int lane = wave_host::current, row = lane / 16;
+    int from = -1;
+    if (ctrl > 0x110 && ctrl < 0x120)
+        from = lane % 16 >= ctrl - 0x110 ? lane - (ctrl - 0x110) : -1;
+    else if (ctrl == 0x142)
+        from = row > 0 ? row * 16 - 1 : -1;
+    else if (ctrl == 0x143)
+        from = row > 1 ? 31 : -1;
+    return from < 0 || !(rows >> row & 1) ? old : (int)all[from];
+}
+#define __builtin_amdgcn_update_dpp update_dpp
 #define __builtin_amdgcn_readlane(x, l) wave_host::shuffle(x, l)
 #define __builtin_amdgcn_readfirstlane(x) wave_host::shuffle(x, 0)

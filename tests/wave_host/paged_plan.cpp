@@ -24,13 +24,13 @@ void note(int)
 
 extern "C" int plan_batch(const int *table, const int *start, const int *kv_len, int T, int B, int H_kv, int n_pages,
                           int page_log2, int width, int G, int BM, int rows_above, int rows_upto, int target, int min_range,
-                          int n_slots, int n_wg, int *units, int4 *notes)
+                          int n_slots, int causal, int n_wg, int *units, int4 *notes)
 {
     p = {};
     p.c.page_table = table, p.c.start = start, p.c.kv_len = kv_len;
     p.c.T = T, p.c.B = B, p.c.H_kv = H_kv, p.c.n_pages = n_pages, p.c.page_log2 = page_log2, p.c.table_width = width;
     p.G = G, p.H_q = G * H_kv;
-    p.rows_above = rows_above, p.rows_upto = rows_upto, p.target = target, p.min_range = min_range, p.n_slots = n_slots;
+    p.rows_above = rows_above, p.rows_upto = rows_upto, p.target = target, p.min_range = min_range, p.parts[0].slots = n_slots, p.causal = causal;
     p.merge = notes;
     int n = 0;
     for (wg = 0; wg < n_wg; ++wg) {
