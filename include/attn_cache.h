@@ -107,7 +107,7 @@ int attn_cache_read_f16(void *k, void *v, const long long *strides,
  *              between calls; calls that overlap in time need one each
  *   max_q      the largest n_b, or an upper bound (T if nothing better is known): it chooses the kernels.  A wrong
  *              value costs speed, not correctness
- *   H_q        a multiple of H_kv;  scale finite and > 0;  T * H_q below 2^30
+ *   H_q        a multiple of H_kv;  scale finite and > 0;  T * H_q and H_kv * page_size * D below 2^30
  *
  * Rows of o and lse that belong to nobody are left as they were.  NaN and infinities in K and V are not checked, except
  * that places behind a sequence's last position may hold anything.  Bitwise reproducible for the same lengths

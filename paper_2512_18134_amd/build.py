@@ -51,6 +51,10 @@ def generate_sources(verbose=False, out_dir=None):
         for dtype in ("bf16", "f16"):
             out = os.path.join(out_dir, "attn_loop_%s%s.inc" % (name, "" if dtype == "bf16" else "_" + dtype))
             _run_generator([sys.executable, gen, name, out, dtype], verbose)
+    gen2 = os.path.join(HERE, "csrc", "gen_attn_paged_loop.py")
+    for name, dtype in itertools.product(("paged_d64", "paged_d128", "paged_d256"), ("bf16", "f16")):
+        out = os.path.join(out_dir, "attn_loop_%s%s.inc" % (name, "" if dtype == "bf16" else "_" + dtype))
+        _run_generator([sys.executable, gen2, name, out, dtype], verbose)
     gen3 = os.path.join(HERE, "csrc", "gen_attn_bwd_loop.py")
     for kind, d, dtype in (("kv", 128, "bf16"), ("q", 128, "bf16"), ("kv", 128, "f16"), ("q", 128, "f16"),
                            ("kv", 64, "bf16"), ("q", 64, "bf16"), ("kv", 64, "f16"), ("q", 64, "f16")):

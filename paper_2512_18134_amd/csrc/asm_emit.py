@@ -310,10 +310,11 @@ def walk(lines, take=(), loop_label=None, loop_visits=2, limit=200000):
     return out
 
 
-def run_scalar(lines, sgprs, bn, tb, bases, limit=2000000):
+def run_scalar(lines, sgprs, bn, tb, bases, limit=2000000, lanes=None):
     """Execute the scalar control flow of `lines` (labels, s_mov / s_add / s_addc / s_sub / s_min / s_lshl /
-    s_and / s_cmp_ge / s_cmp_lt / s_cbranch_scc0/1 / s_branch; vector instructions are skipped, branches on
-    vcc fall through) from the SGPR values in `sgprs` ({number: value}; unset registers read 0) and return the
+    s_lshr / s_and / s_load / s_cmp / s_cbranch_scc0/1 / s_branch; v_readlane reads lanes(register, lane, scalars), s_load
+    lanes(None, address, scalars); other vector instructions are skipped, after lanes(text, None, scalars), branches on vcc
+    fall through) from the SGPR values in `sgprs` ({number: value}; unset registers read 0) and return the
     events of the run in order: ("barrier",) and ("load", which, tile, lds_address), where `bases` =
     {"k": (base register, pointer register), "v": (...)} names the scalar pairs the direct loads go through:
     a load through a base register takes its tile from the scalar operand of the v_add_u32 that started its
@@ -358,23 +359,27 @@ def run_scalar(lines, sgprs, bn, tb, bases, limit=2000000):
             pass
         elif op == "s_barrier":
             events.append(("barrier",))
+        elif op == "v_readlane_b32" and lanes:
+            S[int(ops[0][1:])] = lanes(int(ops[1][1:]), val(ops[2]), S)
+        elif op == "s_load_dword" and lanes:
+            S[int(ops[0][1:])] = lanes(None, val(ops[2]), S)
         elif op in ("s_mov_b32", "s_add_u32", "s_add_i32", "s_addc_u32", "s_sub_i32", "s_min_i32", "s_lshl_b32",
-                    "s_and_b32"):
+                    "s_lshr_b32", "s_and_b32"):
             a = val(ops[1])
             b = val(ops[2]) if len(ops) > 2 else 0
             r = {"s_mov_b32": a, "s_add_u32": a + b, "s_add_i32": a + b, "s_addc_u32": a + b, "s_sub_i32": a - b,
-                 "s_min_i32": min(a, b), "s_lshl_b32": a << b, "s_and_b32": a & b}[op]
+                 "s_min_i32": min(a, b), "s_lshl_b32": a << b, "s_lshr_b32": a >> b, "s_and_b32": a & b}[op]
             if op != "s_mov_b32":
-                scc = int(r != 0) if op in ("s_lshl_b32", "s_and_b32", "s_min_i32") else 0
+                scc = int(r != 0) if op in ("s_lshl_b32", "s_lshr_b32", "s_and_b32", "s_min_i32") else 0
                 if op == "s_min_i32":
                     scc = int(a < b)
             if ops[0] == "m0":
                 m0 = r
             else:
                 S[int(ops[0][1:])] = r
-        elif op in ("s_cmp_ge_i32", "s_cmp_lt_i32"):
+        elif op in ("s_cmp_ge_i32", "s_cmp_lt_i32", "s_cmp_lt_u32", "s_cmp_eq_u32"):
             a, b = val(ops[0]), val(ops[1])
-            scc = int(a >= b) if op == "s_cmp_ge_i32" else int(a < b)
+            scc = int({"ge": a >= b, "lt": a < b, "eq": a == b}[op[6:8]])
         elif op == "v_add_u32" and re.fullmatch(r"s\d+", ops[1]):
             vtile[ops[0]] = val(ops[1]) // bn
         elif op.startswith("global_load_lds"):
@@ -387,4 +392,6 @@ def run_scalar(lines, sgprs, bn, tb, bases, limit=2000000):
             events.append(("load", which, tile, lds))
         elif op.startswith("s_") and op not in ("s_waitcnt", "s_nop"):
             raise AssertionError("scalar instruction not modelled: " + l)
+        elif lanes:
+            lanes(l, None, S)
     return events

@@ -6,12 +6,18 @@
 #include "attn_cache.h"
 #include "attn_fwd.h"
 #include "attn_launch.h"
+#include "attn_paged_asm.h"
 #include "attn_paged_tiles.h"
 
 namespace attn {
 
-// What the chip holds at once: two workgroups of either kernel on each of 256 compute units.
+// Workgroups that the chip holds at once: 256 compute units with two of the row kernel or the e4m3 tile kernel, or one of the
+// 16-bit tile kernel.
 constexpr int kTarget = 512;
+// cuts that a launch may choose from (PagedParams::rounds)
+constexpr int kRowsRounds = 1, kTilesRounds = 4;
+// what a unit costs besides its keys (the plan, the first loads, the exchange or the write), in blocks' time
+constexpr int kRowsOverhead = 1, kTilesOverhead = 4;
 // A range of fewer blocks (of kPlanBlock keys) costs more to merge than its walk by another workgroup saves.
 constexpr int kRowsMinRange = 2, kTilesMinRange = 4;
 constexpr int kSlots = 2 * kTarget + 64;
@@ -51,18 +57,19 @@ using attn::PagedParams;
 bool misaligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
 // Workgroups that a kernel of tiles of BM rows may have units for: a sequence's tiles are at most one more than its rows
-// fill; the ranges' share of the target is twice the target where causal rows see half, and one more for every tile.
+// fill; ranges are one for every tile and head, and the target's (twice that where rows are taken to see half).
 long long most_units(const PagedParams &p, int BM)
 {
     const long long tiles = (long long)p.c.T * p.G / BM + (p.c.B < p.c.T ? p.c.B : p.c.T);
-    return tiles * p.c.H_kv + 2 * p.target + 64;
+    return tiles * p.c.H_kv + (long long)p.target * p.rounds * (p.halve ? 2 : 1) + 64;
 }
 
 template <int D, int MT, typename E, bool E4M3>
 int launch_rows(PagedParams p, int upto, hipStream_t st)
 {
     p.kernel = 0, p.rows_above = 0, p.rows_upto = upto;
-    p.target = attn::kTarget, p.min_range = attn::kRowsMinRange;
+    p.target = attn::kTarget, p.rounds = attn::kRowsRounds, p.min_range = attn::kRowsMinRange, p.overhead = attn::kRowsOverhead;
+    p.halve = 0;
     const long long grid = most_units(p, 16 * MT);
     if (grid > 0x7fffffffLL)
         return ATTN_ERR_SHAPE;
@@ -84,16 +91,32 @@ int launch_rows(const PagedParams &p, int MT, int upto, hipStream_t st)
 template <int D, typename E, bool E4M3>
 int launch_tiles(PagedParams p, int above, hipStream_t st)
 {
-    typedef attn::PagedTilesTiling<D, E4M3> T;
     p.kernel = 1, p.rows_above = above, p.rows_upto = 0x7fffffff;
-    p.target = attn::kTarget, p.min_range = attn::kTilesMinRange;
-    const long long grid = most_units(p, T::BM);
-    const void *kern = reinterpret_cast<const void *>(attn::attn_paged_tiles_kernel<D, E, E4M3>);
+    p.rounds = attn::kTilesRounds, p.min_range = attn::kTilesMinRange, p.overhead = attn::kTilesOverhead;
+    p.halve = p.causal;
+    const void *kern;
+    int lds, threads;
+    if constexpr (E4M3) {
+        typedef attn::PagedTilesTiling<D> T;
+        p.target = attn::kTarget;                          // two of its workgroups to a compute unit
+        kern = reinterpret_cast<const void *>(attn::attn_paged_tiles_kernel<D, E>);
+        lds = T::LDS_BYTES, threads = T::THREADS;
+    } else {
+        typedef attn::PagedAsmTiling<D> T;
+        p.target = attn::kTarget / 2;
+        kern = reinterpret_cast<const void *>(attn::attn_paged_asm_kernel<D, std::is_same<E, attn::PagedF16>::value>);
+        lds = T::LDS_BYTES, threads = T::THREADS;
+    }
+    const long long grid = most_units(p, p.parts[1].BM);
     if (grid > 0x7fffffffLL)
         return ATTN_ERR_SHAPE;
-    if (!attn::allow_lds(kern, T::LDS_BYTES))
+    if (!attn::allow_lds(kern, lds))
         return ATTN_ERR_LAUNCH;
-    hipLaunchKernelGGL((attn::attn_paged_tiles_kernel<D, E, E4M3>), dim3((unsigned)grid), dim3(T::THREADS), T::LDS_BYTES, st, p);
+    if constexpr (E4M3)
+        hipLaunchKernelGGL((attn::attn_paged_tiles_kernel<D, E>), dim3((unsigned)grid), dim3(threads), lds, st, p);
+    else
+        hipLaunchKernelGGL((attn::attn_paged_asm_kernel<D, std::is_same<E, attn::PagedF16>::value>), dim3((unsigned)grid),
+                           dim3(threads), lds, st, p);
     return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH;
 }
 
@@ -106,7 +129,7 @@ int launch(PagedParams &p, int max_q, hipStream_t st)
     const long long rows = (long long)(max_q < p.c.T ? max_q : p.c.T) * p.G;
     const bool few = rows <= most, many = !few, both = many && p.c.B > 1;
     const int MT = attn::row_tiles(D, rows < most ? rows : most);
-    p.parts[0].BM = 16 * MT, p.parts[1].BM = attn::PagedTilesTiling<D, E4M3>::BM;
+    p.parts[0].BM = 16 * MT, p.parts[1].BM = E4M3 ? attn::PagedTilesTiling<D>::BM : attn::PagedAsmTiling<D>::BM;
     int rc = ATTN_OK;
     if (few || both)
         rc = launch_rows<D, E, E4M3>(p, MT, both ? most : 0x7fffffff, st);
@@ -142,7 +165,7 @@ int paged_fwd(const void *q, const long long *strides, void *o, float *lse, cons
         (page_size & (page_size - 1)))
         return ATTN_ERR_UNSUPPORTED;
     if ((long long)T * H_q > 0x3fffffffLL || (long long)n_pages * H_kv > (1LL << 40) / D / page_size || H_kv > (1 << 24) ||
-        (long long)table_width * page_size > (1 << 30))
+        (long long)table_width * page_size > (1 << 30) || (long long)H_kv * page_size >= (1 << 30) / D)
         return ATTN_ERR_SHAPE;
     for (int i = 0; i < 2; ++i) {
         const long long n = i ? H_q : T;

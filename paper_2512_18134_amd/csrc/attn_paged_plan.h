@@ -30,8 +30,10 @@ struct PagedParams {
     int H_q, G;                         // G = H_q / H_kv
     int causal;
     float c_log2;                       // scale * log2(e)
-    // units of this kernel: sequences of rows in (rows_above, rows_upto], cut for `target` units
-    int rows_above, rows_upto, target, min_range;
+    // units of this kernel: sequences of rows in (rows_above, rows_upto], cut for `target` workgroups at once that take up to
+    // `rounds` units each; what a unit costs besides its keys, in blocks
+    int rows_above, rows_upto, target, rounds, min_range, overhead;
+    int halve;                          // a chunk's rows see half of the chunk's own keys (causal)
     int kernel;                         // 0: attn_paged_rows.h, 1: attn_paged_tiles.h
     // partial results, of either kernel
     struct Parts {
@@ -51,7 +53,7 @@ struct Unit {
     int b, h, tile, range, n_ranges, n_tiles;
     int row0, n_rows;                   // start[b], rows of the sequence (tokens * G)
     int n, kv;                          // new tokens, cached positions
-    int key0, key1;                     // this range
+    int key0, key1, len;                // this range; keys of a range
     int slot0, slot;                    // first slot of the sequence, slot of this unit (n_ranges > 1)
 };
 
@@ -79,6 +81,35 @@ __device__ __forceinline__ T wave_sum(T x)
     return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wave_prefix(x)), 63));
 }
 
+// Units of one range of a sequence, H heads x n tiles: which one number w is.  Workgroups go to the 8 XCDs in turn; the tiles
+// of a head, which stream the same keys, belong to one XCD (its L2) as far as heads go evenly into XCDs, or to as many as share
+// the head.  Heavier tiles (the last ones, causal) come first and every XCD gets its share of them.
+__host__ __device__ __forceinline__ void place_in_layer(int w, int H, int n, int &h, int &tile)
+{
+    const int whole = H / kNumXcd * kNumXcd;                // heads that have an XCD to themselves
+    int t;
+    if (w < whole * n) {
+        const int x = w % kNumXcd, i = w / kNumXcd;
+        h = i / n * kNumXcd + x;
+        t = i % n;
+    } else {
+        const int rest = H - whole, share = kNumXcd % rest == 0 ? kNumXcd / rest : 1;   // XCDs of a head
+        w -= whole * n;
+        if (w < n / share * share * rest && share > 1) {
+            const int x = w % kNumXcd, i = w / kNumXcd;
+            h = x % rest;
+            t = i * share + x / rest;
+        } else {
+            const int done = share > 1 ? n / share * share : 0;
+            w -= done * rest;
+            h = w % rest;
+            t = done + w / rest;
+        }
+        h += whole;
+    }
+    tile = n - 1 - t;
+}
+
 // Every wave of workgroup `wg` calls this; false: the launch has no unit for it.
 template <int BM>
 __device__ __forceinline__ bool plan_unit(const PagedParams &p, int wg, Unit &u)
@@ -102,42 +133,58 @@ __device__ __forceinline__ bool plan_unit(const PagedParams &p, int wg, Unit &u)
     };
     const bool one = p.c.B <= 64;
     Seq s = sequence(lane);
-    // work of the call, in (row tile, block, key head): of a causal chunk the rows see half of its own keys
+    // work of the call, in (row tile, block, key head)
     float work = 0.f;
     for (int b = 0;; b += 64) {
-        const float seen = (float)s.blocks - (p.causal ? (float)min(s.n, s.kv) * (0.5f / kPlanBlock) : 0.f);
+        const float seen = (float)s.blocks - (p.halve ? (float)min(s.n, s.kv) * (0.5f / kPlanBlock) : 0.f);
         work += wave_sum((float)s.tiles * fmaxf(seen, 1.f));
         if (b + 64 >= p.c.B)
             break;
         s = sequence(b + 64 + lane);
     }
-    // (a float is enough: the same one in every workgroup, and the bounds below leave room for its rounding)
-    const float share = ceilf(work * (float)p.c.H_kv / (float)p.target);
-    int L = max(p.min_range, (int)fminf(share, 0x1p24f));
-    // units, and slots of those that are not alone in their sequence and row tile; longer ranges if the slots do not suffice
-    auto ranges = [&](const Seq &x) { return x.tiles ? (x.blocks + L - 1) / L : 0; };
+    work *= (float)p.c.H_kv;
+    // Units, and slots of those that are not alone in their sequence and row tile, for ranges of at most L blocks.  (Floats are
+    // enough above: the same ones in every workgroup, and the launch has room for their rounding.)
+    auto ranges_of = [&](const Seq &x, int L) { return x.tiles ? (x.blocks + L - 1) / L : 0; };
     int total, held;
-    for (;; L *= 2) {
+    auto count = [&](int L) {
         total = held = 0;
         if (!one)
             s = sequence(lane);
         for (int b = 0;; b += 64) {
-            const int nr = ranges(s);
+            const int nr = ranges_of(s, L);
             total += wave_sum(s.tiles * nr);
             held += wave_sum(nr > 1 ? s.tiles * nr : 0);
             if (b + 64 >= p.c.B)
                 break;
             s = sequence(b + 64 + lane);
         }
-        if ((long long)held * p.c.H_kv <= p.parts[p.kernel].slots || L >= 1 << 24)
+        return (long long)held * p.c.H_kv <= p.parts[p.kernel].slots;
+    };
+    // A number of units that just exceeds the workgroups that run at once leaves most of them idle in the last round: of the
+    // cuts for one to `rounds` units each the one that ends soonest, each unit with its share of the work and its overhead.
+    int L = 1 << 24;
+    float soonest = INFINITY;
+    for (int k = 1; k <= p.rounds; ++k) {
+        const int l = max(p.min_range, (int)fminf(ceilf(work / (float)(k * p.target)), 0x1p24f));
+        if (!count(l) && k > 1)
+            break;
+        const float units = (float)total * (float)p.c.H_kv;
+        const float ends = ceilf(units / (float)p.target) * (work / fmaxf(units, 1.f) + (float)p.overhead);
+        if (k == 1 || ends < soonest)
+            L = l, soonest = ends;
+        if (l == p.min_range)
             break;
     }
+    while (!count(L) && L < 1 << 24)                // longer ranges where the slots do not suffice
+        L *= 2;
+    auto ranges = [&](const Seq &x) { return ranges_of(x, L); };
     if (!one)
         s = sequence(lane);
     total *= p.c.H_kv;
     if (wg >= total)
         return false;
-    const int v = xcd_remap(wg, total);
+    const int v = wg;
     int units0 = 0, slots0 = 0;
     for (int b = 0;; b += 64) {
         const int nr = ranges(s);
@@ -154,11 +201,11 @@ __device__ __forceinline__ bool plan_unit(const PagedParams &p, int wg, Unit &u)
             if (w < 0 || w >= of(mine))        // starts that decrease can count more units than an int holds
                 return false;
             u.slot0 = of(after_slots - kept);
-            u.slot = u.slot0 + w;
-            u.tile = w % u.n_tiles;
-            const int hr = w / u.n_tiles;
-            u.h = hr % p.c.H_kv;
-            u.range = hr / p.c.H_kv;
+            const int layer = u.n_tiles * p.c.H_kv;
+            u.range = w / layer;
+            place_in_layer(w % layer, p.c.H_kv, u.n_tiles, u.h, u.tile);
+            u.slot = u.slot0 + (u.range * p.c.H_kv + u.h) * u.n_tiles + u.tile;
+            u.len = ((of(s.blocks) + u.n_ranges - 1) / u.n_ranges) * kPlanBlock;
             break;
         }
         units0 = __builtin_amdgcn_readlane(after, 63);
@@ -168,8 +215,8 @@ __device__ __forceinline__ bool plan_unit(const PagedParams &p, int wg, Unit &u)
         s = sequence(b + 64 + lane);
     }
     u.n_rows = u.n * p.G;
-    u.key0 = min((long long)u.range * L * kPlanBlock, (long long)u.kv);
-    u.key1 = min((long long)(u.range + 1) * L * kPlanBlock, (long long)u.kv);
+    u.key0 = min(u.range * u.len, u.kv);
+    u.key1 = min(u.key0 + u.len, u.kv);
     // the same in all lanes: scalars from here on
     auto scalar = [](int &x) { x = __builtin_amdgcn_readfirstlane(x); };
     u.row0 = p.c.start_of(u.b);

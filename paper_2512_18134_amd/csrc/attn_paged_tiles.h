@@ -14,7 +14,6 @@
 // numbers of 64 tiles.  16-bit rows go straight to LDS; e4m3 rows pass through registers, where they become 16-bit ones
 // once for all waves.
 #pragma once
-#include "attn_dma.h"
 #include "attn_paged_rows.h"
 
 namespace attn {
@@ -32,36 +31,31 @@ __device__ __forceinline__ f32x16 mfma32<PagedF16>(u32x4 a, u32x4 b, f32x16 c)
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(PagedF16::x8, a), __builtin_bit_cast(PagedF16::x8, b), c, 0, 0, 0);
 }
 
-template <int D, bool E4M3>
+template <int D>
 struct PagedTilesTiling {
     static constexpr int QB = D == 256 ? 1 : 2;             // 32-row blocks of a wave
     static constexpr int NW = 4, THREADS = NW * 64, BM = NW * QB * 32, BN = 32;
     static constexpr int ROWB = D * 2, TB = BN * ROWB;      // bytes of a tile in LDS
-    // K and V stages: tile j is read while j + 1 (.. j + STAGES - 1) arrive; two workgroups share 160 KB
-    static constexpr int STAGES = E4M3 || D == 256 ? 2 : 3;
+    static constexpr int STAGES = 2;                        // of K and V: tile j is read while j + 1 is written
     // steps of S whose part of Q waits in LDS: 128 registers of O and 64 of Q leave too few for the rest
-    static constexpr int QL = D == 64 ? 0 : D == 256 ? 2 : E4M3 ? 4 : 3;
+    static constexpr int QL = D == 64 ? 0 : D == 256 ? 2 : 4;
     static constexpr int Q_BYTES = QL * BM * 32, LDS_BYTES = 2 * STAGES * TB + Q_BYTES;
 };
 
-template <int D, typename E, bool E4M3>
+template <int D, typename E>
 __global__ __launch_bounds__(256, 2) void attn_paged_tiles_kernel(const PagedParams p)
 {
-    typedef PagedTilesTiling<D, E4M3> T;
+    typedef PagedTilesTiling<D> T;
     constexpr int QB = T::QB, ROWB = T::ROWB, TB = T::TB, BN = T::BN, ST = T::STAGES;
     constexpr int KS = D / 16, DB = D / 32;
-    constexpr int CROWB = D * (E4M3 ? 1 : 2);               // bytes of a cached row
-    // what a lane brings of a wave's eight rows: pieces of 16 bytes of memory (e4m3, D = 64: 8 bytes)
-    constexpr int PB = E4M3 && D == 64 ? 8 : 16;
+    constexpr int CROWB = D;                                // bytes of a cached row
+    // what a lane brings of a wave's eight rows: pieces of 16 bytes of memory (D = 64: 8 bytes)
+    constexpr int PB = D == 64 ? 8 : 16;
     constexpr int PPR = CROWB / PB, NP = 8 * PPR / 64;      // pieces of a row, of a lane
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
 
     Unit u;
     if (!plan_unit<T::BM>(p, blockIdx.x, u))
-        return;
-    u.tile = u.n_tiles - 1 - u.tile;                        // the tiles that see most keys come first
-    u.slot = u.slot0 + (u.range * p.c.H_kv + u.h) * u.n_tiles + u.tile;
-    if (u.n_ranges > 1 && (unsigned)u.slot >= (unsigned)p.parts[1].slots)      // (see plan_unit)
         return;
     leave_note<T::BM, T::THREADS>(p, u);
 
@@ -139,36 +133,12 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tiles_kernel(const PagedPar
             row = (size_t)__builtin_amdgcn_readfirstlane((int)(row >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)row);
             most = min(u.kv - 1 - pos, 7);
         };
-        // 16-bit: memory -> LDS, the lane that fills a physical chunk fetches the one that belongs there (swz)
-        auto bring = [&](int t_wanted) {
-            int t = t_wanted, id, most;
-            size_t row;
-            locate(t, id, row, most);
-            const unsigned char *k = static_cast<const unsigned char *>(p.k) + row * ROWB;
-            const unsigned char *v = static_cast<const unsigned char *>(p.v) + row * ROWB;
-            const uint32_t at = lds0 + (t_wanted % ST) * 2 * TB + wave * 8 * ROWB;
-#pragma unroll
-            for (int i = 0; i < NP; ++i) {
-                const int r = i * (64 / PPR) + prow, c = lane % PPR;
-                const uint32_t chunk = (uint32_t)(((c & ~15) | ((c & 15) ^ swz<D>(8 * wave + r))) * 16);
-                const uint32_t off = min(r, most) * ROWB + chunk;
-                dma16(at + i * 1024, k, off);
-                dma16(at + TB + i * 1024, v, off);
-            }
-            if (id < 0) {
-                // nothing is there: zeros for V, behind the loads (K's scores are masked)
-                wait_vmcnt<0>();
-#pragma unroll
-                for (int i = 0; i < NP; ++i)
-                    *reinterpret_cast<u32x4 *>(smem + (t_wanted % ST) * 2 * TB + TB + wave * 8 * ROWB + i * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
-            }
-        };
         // e4m3: memory -> registers, registers -> LDS
         struct Rows {
             Piece<PB> k[NP], v[NP];
             uint32_t ks[NP], vs[NP];
         };
-        [[maybe_unused]] Rows x;
+        Rows x;
         auto fetch = [&](int t) {
             int id, most;
             size_t row;
@@ -305,33 +275,17 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tiles_kernel(const PagedPar
                 }
         };
 
-        if constexpr (E4M3) {
-            advance(0);
-            fetch(0);
-            store(0);
-            fetch(1);
+        advance(0);
+        fetch(0);
+        store(0);
+        fetch(1);
 #pragma clang loop unroll(disable)
-            for (int j = 0; j < n; ++j) {
-                barrier();                                  // tile j is complete, tile j - 1 has been read
-                store(j + 1);
-                advance(j + 2);
-                fetch(j + 2);
-                tile(j);
-            }
-        } else {
-            advance(0);
-#pragma unroll
-            for (int t = 0; t < ST - 1; ++t)
-                bring(t);
-#pragma clang loop unroll(disable)
-            for (int j = 0; j < n; ++j) {
-                wait_vmcnt<(ST - 2) * 2 * NP>();            // this wave's rows of tile j have arrived
-                barrier();                                  // ... and everyone's; tile j - 1 has been read
-                advance(j + ST - 1);
-                bring(j + ST - 1);
-                tile(j);
-            }
-            wait_vmcnt<0>();                                // nothing may arrive in LDS that is somebody else's by then
+        for (int j = 0; j < n; ++j) {
+            barrier();                                      // tile j is complete, tile j - 1 has been read
+            store(j + 1);
+            advance(j + 2);
+            fetch(j + 2);
+            tile(j);
         }
     }
 

@@ -466,6 +466,14 @@ class Gen(Emitter):
             self.e("s_nop 0")
             self.e("global_load_lds_dwordx4 v%d, %s" % (t, self.sr(base, 2)))
 
+    def bump_ops(self):
+        """To the next iteration: its number, and the scalar pointers at its K and V tiles."""
+        return ["s_add_u32 s%d, s%d, %d" % (self.s_kptr, self.s_kptr, self.TB),
+                "s_addc_u32 s%d, s%d, 0" % (self.s_kptr + 1, self.s_kptr + 1),
+                "s_add_u32 s%d, s%d, %d" % (self.s_vptr, self.s_vptr, self.TB),
+                "s_addc_u32 s%d, s%d, 0" % (self.s_vptr + 1, self.s_vptr + 1),
+                "s_add_i32 s%d, s%d, 1" % (self.s_j, self.s_j)]
+
     # --------------------------------------------------------------- the loop
     def entry_reads(self, vst, pv_only):
         """State of the LDS queue where an iteration starts: the iteration before it (or the set-up code) has
@@ -517,12 +525,7 @@ class Gen(Emitter):
         # (nothing between the test above and these two branches writes SCC), pointer bumps in slot 2
         extra = {}
         if kind != "last":
-            bumps = [
-                "s_add_u32 s%d, s%d, %d" % (self.s_kptr, self.s_kptr, self.TB),
-                "s_addc_u32 s%d, s%d, 0" % (self.s_kptr + 1, self.s_kptr + 1),
-                "s_add_u32 s%d, s%d, %d" % (self.s_vptr, self.s_vptr, self.TB),
-                "s_addc_u32 s%d, s%d, 0" % (self.s_vptr + 1, self.s_vptr + 1),
-                "s_add_i32 s%d, s%d, 1" % (self.s_j, self.s_j)]
+            bumps = self.bump_ops()
             if self.LS == 0:
                 extra[0] = ["s_cbranch_scc1 %s" % L("KSLOW%s_" % tag)] + sum(self.dma_fast("k", b), []) + ["%s:" % L("KRET%s_" % tag)]
                 extra[1] = ["s_cbranch_scc1 %s" % L("VSLOW%s_" % tag)] + sum(self.dma_fast("v", (b + 2) % 4), []) + ["%s:" % L("VRET%s_" % tag)]
@@ -605,6 +608,7 @@ class Gen(Emitter):
             if kind == "loop" and b == 1:
                 self.e("s_cmp_ge_i32 s%d, s%d" % (self.s_j, self.s_nw))
                 self.e("s_cbranch_scc1 %s" % L("EXIT1_"))
+            self.special_entry(tag)
             self.e("s_cmp_lt_i32 s%d, s%d" % (self.s_j, self.s_jmask))
             self.e("s_cbranch_scc1 %s" % L("NOMASK%s_" % tag))
             # mask pre-pass: keys past the causal diagonal / past S_kv become -inf
@@ -621,6 +625,7 @@ class Gen(Emitter):
                         x = self.s_reg(S_cur, qb, sb, 0, r)
                         self.e("v_cmp_gt_i32 vcc, %d, v%d" % (const, self.THR + qb))       # key index > limit ?
                         self.e("v_cndmask_b32 v%d, v%d, v%d, vcc" % (x, x, self.NEGINF))
+            self.mask_more(tag, S_cur)
             self.e("%s:" % L("NOMASK%s_" % tag))
             if kind == "loop":
                 self.e("s_cmp_ge_i32 s%d, s%d" % (self.s_j, self.s_nm1))                   # the last tile?
@@ -654,6 +659,12 @@ class Gen(Emitter):
     def before_mask(self):
         """What an iteration's scores wait for before the mask (they are complete half an iteration before its top)."""
         return []
+
+    def special_entry(self, tag):
+        """A derived generator's work at the start of a rare iteration."""
+
+    def mask_more(self, tag, S_cur):
+        """A derived generator's keys to be masked besides those past a row's limit."""
 
     def slow_pass(self, tag, S_cur, P_new):
         """A tile row sum failed the test: exact row maxima of the (intact) scores, move the references there (alpha =
@@ -704,8 +715,6 @@ class Gen(Emitter):
         iteration, and its share of every iteration's loads (the ring stage follows from the iteration number).
         AFTERLAST: the last iteration's counter has not moved on; STANDBY: s_j = this wave's tile count."""
         L, e = self.lab, self.e
-        sh = {128: 7, 256: 8, 512: 9}[self.ROWB]
-        tb = {4096: 12, 8192: 13, 16384: 14}[self.TB]
         e("%s:" % L("AFTERLAST_"))
         e("s_add_i32 s%d, s%d, 1" % (self.s_j, self.s_j))
         e("%s:" % L("STANDBY_"))
@@ -715,6 +724,15 @@ class Gen(Emitter):
         e("s_barrier")
         e("s_cmp_ge_i32 s%d, s%d" % (self.s_j, self.s_wgnm1))        # the workgroup's last iteration has no loads
         e("s_cbranch_scc1 %s" % L("STANDBYNEXT_"))
+        self.standby_loads()
+        e("%s:" % L("STANDBYNEXT_"))
+        e("s_add_i32 s%d, s%d, 1" % (self.s_j, self.s_j))
+        e("s_branch %s" % L("STANDBY_"))
+
+    def standby_loads(self):
+        e = self.e
+        sh = {128: 7, 256: 8, 512: 9}[self.ROWB]
+        tb = {4096: 12, 8192: 13, 16384: 14}[self.TB]
         for which, ahead in (("k", 4), ("v", 2)):
             base = self.s_kbase if which == "k" else self.s_vbase
             lds = self.s_ldsk if which == "k" else self.s_ldsv
@@ -732,9 +750,13 @@ class Gen(Emitter):
                 e("v_add_u32 v%d, v%d, v%d" % (t, t, self.DCH + i))
                 e("s_nop 0")
                 e("global_load_lds_dwordx4 v%d, %s" % (t, self.sr(base, 2)))
-        e("%s:" % L("STANDBYNEXT_"))
-        e("s_add_i32 s%d, s%d, 1" % (self.s_j, self.s_j))
-        e("s_branch %s" % L("STANDBY_"))
+
+    def start_pointers(self):
+        """Scalar pointers at the tiles that the first iteration brings: K(4), V(2)."""
+        self.e("s_add_u32 s%d, s%d, %d" % (self.s_kptr, self.s_kbase, 4 * self.TB))
+        self.e("s_addc_u32 s%d, s%d, 0" % (self.s_kptr + 1, self.s_kbase + 1))
+        self.e("s_add_u32 s%d, s%d, %d" % (self.s_vptr, self.s_vbase, 2 * self.TB))
+        self.e("s_addc_u32 s%d, s%d, 0" % (self.s_vptr + 1, self.s_vbase + 1))
 
     def generate(self):
         L = self.lab
@@ -752,10 +774,7 @@ class Gen(Emitter):
         e("s_sub_i32 s%d, s%d, 4" % (self.s_tload, self.s_tfull))
         e("s_min_i32 s%d, s%d, s%d" % (self.s_special, self.s_tload, self.s_jmask))
         e("s_min_i32 s%d, s%d, s%d" % (self.s_special, self.s_special, self.s_nm1))
-        e("s_add_u32 s%d, s%d, %d" % (self.s_kptr, self.s_kbase, 4 * self.TB))
-        e("s_addc_u32 s%d, s%d, 0" % (self.s_kptr + 1, self.s_kbase + 1))
-        e("s_add_u32 s%d, s%d, %d" % (self.s_vptr, self.s_vbase, 2 * self.TB))
-        e("s_addc_u32 s%d, s%d, 0" % (self.s_vptr + 1, self.s_vbase + 1))
+        self.start_pointers()
         for st in range(4):
             e("s_add_u32 s%d, s%d, %d" % (self.s_lk + st, self.s_ldsk, st * self.TB))
             e("s_add_u32 s%d, s%d, %d" % (self.s_lv + st, self.s_ldsv, st * self.TB))
@@ -945,12 +964,7 @@ class PairedGen(Gen):
         if kind != "last":
             extra[0] = ["s_cbranch_scc1 %s" % L("KSLOW%s_" % tag)] + sum(self.dma_fast("k", b), []) + ["%s:" % L("KRET%s_" % tag)]
             extra[1] = ["s_cbranch_scc1 %s" % L("VSLOW%s_" % tag)] + sum(self.dma_fast("v", (b + 2) % 4), []) + ["%s:" % L("VRET%s_" % tag)]
-            extra[2] = [
-                "s_add_u32 s%d, s%d, %d" % (self.s_kptr, self.s_kptr, self.TB),
-                "s_addc_u32 s%d, s%d, 0" % (self.s_kptr + 1, self.s_kptr + 1),
-                "s_add_u32 s%d, s%d, %d" % (self.s_vptr, self.s_vptr, self.TB),
-                "s_addc_u32 s%d, s%d, 0" % (self.s_vptr + 1, self.s_vptr + 1),
-                "s_add_i32 s%d, s%d, 1" % (self.s_j, self.s_j)]
+            extra[2] = self.bump_ops()
         # ---- VALU program: behind the test of the tile before
         b_ops = self.first_ops(S_cur, P_new) if kind == "first" else self.pair_ops(S_cur, P_new)
         lead = 0 if kind == "first" else half

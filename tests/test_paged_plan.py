@@ -32,16 +32,16 @@ def ptr(a):
     return a.ctypes.data_as(ctypes.c_void_p)
 
 
-def plan(lib, start, kv_len, T, H_kv, G, BM, width, page_log2=4, above=0, upto=ALL, target=512, min_range=2, n_slots=None, causal=1):
+def plan(lib, start, kv_len, T, H_kv, G, BM, width, page_log2=4, above=0, upto=ALL, target=64, min_range=2, n_slots=None, causal=1, rounds=1):
     B = len(kv_len)
-    n_slots = 2 * target + 64 if n_slots is None else n_slots
-    n_wg = (T * G // BM + min(B, T)) * H_kv + 2 * target + 64    # the launch's own bound
+    n_slots = 4 * target + 64 if n_slots is None else n_slots
+    n_wg = (T * G // BM + min(B, T)) * H_kv + target * rounds * (2 if causal else 1) + 64    # the launch's own bound
     start, kv_len = ints(start), ints(kv_len)
     table = np.zeros((B, width), np.int32)
     units = np.zeros((n_wg, 14), np.int32)
     notes = np.full((T + 2, 4), -77, np.int32)                    # a guard row on either side
     n = lib.plan_batch(ptr(table), ptr(start), ptr(kv_len), T, B, H_kv, 1, page_log2, width, G, BM, above, upto, target,
-                       min_range, n_slots, causal, n_wg, ptr(units), ctypes.c_void_p(notes.ctypes.data + 16))
+                       min_range, n_slots, causal, rounds, n_wg, ptr(units), ctypes.c_void_p(notes.ctypes.data + 16))
     assert n >= 0
     assert (notes[0] == -77).all() and (notes[-1] == -77).all()
     return [dict(zip(FIELDS, map(int, u))) for u in units[:n]], notes[1:-1], n_wg, n_slots
@@ -62,13 +62,13 @@ CASES = [
 
 
 @pytest.mark.parametrize("case", CASES, ids=lambda c: "B%d_H%d_G%d_BM%d" % (len(c["news"]), c["H"], c["G"], c["BM"]))
-@pytest.mark.parametrize("front, behind", [(0, 0), (3, 4)])
-def test_units_cover_every_row_and_key_once(lib, case, front, behind):
+@pytest.mark.parametrize("front, behind, rounds, causal", [(0, 0, 1, 1), (3, 4, 4, 0), (1, 0, 3, 1)])
+def test_units_cover_every_row_and_key_once(lib, case, front, behind, rounds, causal):
     news, kvs, H, G, BM = (case[k] for k in ("news", "kvs", "H", "G", "BM"))
     start = front + np.concatenate([[0], np.cumsum(news)])
     T = max(1, int(start[-1]) + behind)
     width = max(1, -(-max(kvs) // 16))
-    units, notes, n_wg, n_slots = plan(lib, start, kvs, T, H, G, BM, width)
+    units, notes, n_wg, n_slots = plan(lib, start, kvs, T, H, G, BM, width, rounds=rounds, causal=causal)
     seen, slots = {}, set()
     for u in units:
         b = u["b"]
@@ -108,9 +108,30 @@ def test_two_kernels_share_a_batch(lib):
 
 
 def test_a_long_sequence_is_shared_out(lib):
-    units, _, _, _ = plan(lib, list(range(9)), [131072] + [64] * 7, 8, 8, 4, 16, 8192)
+    units, _, _, _ = plan(lib, list(range(9)), [131072] + [64] * 7, 8, 8, 4, 16, 8192, target=128)
     longest = max(u["key1"] - u["key0"] for u in units)
-    assert longest <= 131072 * 8 // 512 + 128        # its share of 512 units, to a block
+    assert longest <= 131072 * 8 // 128 + 128        # its share of 128 workgroups, to a block
+
+
+def test_units_fill_the_last_round(lib):
+    """Six row tiles of eight heads on 32 workgroups: one range each would be 48 units in two rounds, the second half empty."""
+    for rounds, most in ((1, 2.0), (4, 1.51)):
+        units, _, _, _ = plan(lib, [0, 24], [64 * 600], 24, 8, 4, 16, 2400, target=32, rounds=rounds, causal=0)
+        work = sum(u["key1"] - u["key0"] for u in units)
+        longest = max(u["key1"] - u["key0"] for u in units)
+        assert -(-len(units) // 32) * longest <= most * work / 32
+
+
+@pytest.mark.parametrize("H", [1, 2, 3, 4, 5, 8, 12, 16, 20])
+@pytest.mark.parametrize("n", [1, 2, 3, 7, 16])
+def test_heads_share_xcds_evenly(lib, H, n):
+    got = [[ctypes.c_int(), ctypes.c_int()] for _ in range(H * n)]
+    for w, (h, t) in enumerate(got):
+        lib.layer_place(w, H, n, ctypes.byref(h), ctypes.byref(t))
+    got = [(h.value, t.value) for h, t in got]
+    assert sorted(got) == [(h, t) for h in range(H) for t in range(n)]
+    if H % 8 == 0:
+        assert all(len({h for w, (h, _) in enumerate(got) if w % 8 == x}) == H // 8 for x in range(8))
 
 
 @pytest.mark.parametrize("causal", [0, 1])

@@ -24,13 +24,14 @@ void note(int)
 
 extern "C" int plan_batch(const int *table, const int *start, const int *kv_len, int T, int B, int H_kv, int n_pages,
                           int page_log2, int width, int G, int BM, int rows_above, int rows_upto, int target, int min_range,
-                          int n_slots, int causal, int n_wg, int *units, int4 *notes)
+                          int n_slots, int causal, int rounds, int n_wg, int *units, int4 *notes)
 {
     p = {};
     p.c.page_table = table, p.c.start = start, p.c.kv_len = kv_len;
     p.c.T = T, p.c.B = B, p.c.H_kv = H_kv, p.c.n_pages = n_pages, p.c.page_log2 = page_log2, p.c.table_width = width;
     p.G = G, p.H_q = G * H_kv;
     p.rows_above = rows_above, p.rows_upto = rows_upto, p.target = target, p.min_range = min_range, p.parts[0].slots = n_slots, p.causal = causal;
+    p.rounds = rounds, p.overhead = 2, p.halve = causal;
     p.merge = notes;
     int n = 0;
     for (wg = 0; wg < n_wg; ++wg) {
@@ -66,3 +67,5 @@ extern "C" int page_of(const int *table, const int *kv_len, int b, int n_pages, 
     *length = p.c.length_of(b);
     return pos < *length && pos >= 0 ? p.c.page_of(b, pos) : -2;
 }
+
+extern "C" void layer_place(int w, int H, int n, int *h, int *tile) { attn::place_in_layer(w, H, n, *h, *tile); }
