@@ -11,19 +11,26 @@
 
 namespace attn {
 
-// Workgroups that the chip holds at once: 256 compute units with two of the row kernel or the e4m3 tile kernel, or one of the
-// 16-bit tile kernel.
+// Workgroups that the chip holds at once: on each of 256 compute units two of the e4m3 tile kernel, one of the 16-bit one, two
+// of the row kernel where its registers let two waves share a SIMD.  (16 sequences of four drafted tokens and 512 .. 4100
+// positions, D = 256: 26.0 us cut for 512, 22.0 for 256; 16 tokens over 8000 positions, D = 128: see row_slots.)
 constexpr int kTarget = 512;
+constexpr int row_slots(int D, int MT, bool e4m3)
+{
+    return (MT == 1 && D <= 128) || (MT == 2 && (D == 64 || (D == 128 && e4m3))) ? kTarget : kTarget / 2;
+}
 // cuts that a launch may choose from (PagedParams::rounds)
 constexpr int kRowsRounds = 1, kTilesRounds = 4;
-// what a unit costs besides its keys (the plan, the first loads, the exchange or the write), in blocks' time
-constexpr int kRowsOverhead = 1, kTilesOverhead = 4;
+// what a unit costs besides its keys (the plan, the first loads, the exchange or the write), and a merge, in blocks' time
+constexpr int kRowsOverhead = 1, kTilesOverhead = 4, kRowsMerging = 1, kTilesMerging = 12;
 // A range of fewer blocks (of kPlanBlock keys) costs more to merge than its walk by another workgroup saves.
 constexpr int kRowsMinRange = 2, kTilesMinRange = 4;
+// bytes of K and V of one key head up to which a sequence is walked by one workgroup of sixteen waves
+constexpr long long kWholeBytes = 1 << 18;
 constexpr int kSlots = 2 * kTarget + 64;
 
 // rows of a sequence up to which the row kernel takes it
-constexpr int rows_kernel_most(int D) { return D == 256 ? 32 : 64; }
+constexpr int rows_kernel_most(int D) { return D == 256 ? 64 : 128; }
 // 16-row tiles of its workgroup: as few as hold the rows
 inline int row_tiles(int D, long long rows) { return rows <= 16 ? 1 : rows <= 32 || D == 256 ? 2 : 4; }
 
@@ -36,7 +43,7 @@ inline Workspace workspace_of(int T, int G, int D)
     Workspace w;
     long long at = 0;
     for (int kernel = 0; kernel < 2; ++kernel) {
-        const long long rows = kernel ? (D == 256 ? 128 : 256) : rows_kernel_most(D);
+        const long long rows = kernel ? (D == 256 ? 128 : 256) : D == 256 ? 32 : 64;
         const long long slots = kernel && (long long)T * G <= rows_kernel_most(D) ? 0 : kSlots;
         w.part_o[kernel] = at;
         at += slots * rows * D * 4;
@@ -61,19 +68,26 @@ bool misaligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_
 long long most_units(const PagedParams &p, int BM)
 {
     const long long tiles = (long long)p.c.T * p.G / BM + (p.c.B < p.c.T ? p.c.B : p.c.T);
-    return tiles * p.c.H_kv + (long long)p.target * p.rounds * (p.halve ? 2 : 1) + 64;
+    const long long blocks = (((long long)p.c.table_width << p.c.page_log2) + attn::kPlanBlock - 1) / attn::kPlanBlock;
+    const long long most_ranges = (blocks + p.min_range - 1) / p.min_range;
+    const long long units = tiles * p.c.H_kv + (long long)p.target * p.rounds * (p.halve ? 2 : 1) + 64;
+    return units < tiles * p.c.H_kv * most_ranges ? units : tiles * p.c.H_kv * most_ranges;
 }
 
-template <int D, int MT, typename E, bool E4M3>
+template <int D, int MT, typename E, bool E4M3, int NW = 4>
 int launch_rows(PagedParams p, int upto, hipStream_t st)
 {
-    p.kernel = 0, p.rows_above = 0, p.rows_upto = upto;
-    p.target = attn::kTarget, p.rounds = attn::kRowsRounds, p.min_range = attn::kRowsMinRange, p.overhead = attn::kRowsOverhead;
+    p.kernel = 0, p.slots = p.parts[0].slots, p.rows_above = 0, p.rows_upto = upto;
+    p.target = attn::row_slots(D, MT, E4M3), p.rounds = attn::kRowsRounds, p.min_range = attn::kRowsMinRange, p.overhead = attn::kRowsOverhead;
+    p.merging = attn::kRowsMerging;
     p.halve = 0;
+    if (NW > 4)
+        p.rounds = 0;                                      // whole sequences
     const long long grid = most_units(p, 16 * MT);
     if (grid > 0x7fffffffLL)
         return ATTN_ERR_SHAPE;
-    hipLaunchKernelGGL((attn::attn_paged_rows_kernel<D, MT, E, E4M3>), dim3((unsigned)grid), dim3(256), 0, st, p);
+    p.most_units = (int)grid;
+    hipLaunchKernelGGL((attn::attn_paged_rows_kernel<D, MT, E, E4M3, NW>), dim3((unsigned)grid), dim3(NW * 64), 0, st, p);
     return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH;
 }
 
@@ -91,8 +105,9 @@ int launch_rows(const PagedParams &p, int MT, int upto, hipStream_t st)
 template <int D, typename E, bool E4M3>
 int launch_tiles(PagedParams p, int above, hipStream_t st)
 {
-    p.kernel = 1, p.rows_above = above, p.rows_upto = 0x7fffffff;
+    p.kernel = 1, p.slots = p.parts[1].slots, p.rows_above = above, p.rows_upto = 0x7fffffff;
     p.rounds = attn::kTilesRounds, p.min_range = attn::kTilesMinRange, p.overhead = attn::kTilesOverhead;
+    p.merging = attn::kTilesMerging;
     p.halve = p.causal;
     const void *kern;
     int lds, threads;
@@ -107,9 +122,10 @@ int launch_tiles(PagedParams p, int above, hipStream_t st)
         kern = reinterpret_cast<const void *>(attn::attn_paged_asm_kernel<D, std::is_same<E, attn::PagedF16>::value>);
         lds = T::LDS_BYTES, threads = T::THREADS;
     }
-    const long long grid = most_units(p, p.parts[1].BM);
-    if (grid > 0x7fffffffLL)
+    const long long units = most_units(p, p.parts[1].BM), grid = units < p.target ? units : p.target;
+    if (units > 0x7fffffffLL)
         return ATTN_ERR_SHAPE;
+    p.most_units = (int)units;
     if (!attn::allow_lds(kern, lds))
         return ATTN_ERR_LAUNCH;
     if constexpr (E4M3)
@@ -131,18 +147,32 @@ int launch(PagedParams &p, int max_q, hipStream_t st)
     const int MT = attn::row_tiles(D, rows < most ? rows : most);
     p.parts[0].BM = 16 * MT, p.parts[1].BM = E4M3 ? attn::PagedTilesTiling<D>::BM : attn::PagedAsmTiling<D>::BM;
     int rc = ATTN_OK;
+    // Short sequences, and no more of them than compute units: sixteen waves walk one without a cut, and there is nothing to
+    // merge.  (The bound is what the page table can hold.)
+    if constexpr (D != 256)
+        if (few && MT == 1 && ((long long)p.c.T * p.G / 16 + (p.c.B < p.c.T ? p.c.B : p.c.T)) * p.c.H_kv <= attn::kTarget / 2 &&
+            ((long long)p.c.table_width << p.c.page_log2) * D * (E4M3 ? 2 : 4) <= attn::kWholeBytes)
+            return launch_rows<D, 1, E, E4M3, 16>(p, 0x7fffffff, st);
     if (few || both)
         rc = launch_rows<D, E, E4M3>(p, MT, both ? most : 0x7fffffff, st);
     if (rc == ATTN_OK && many)
         rc = launch_tiles<D, E, E4M3>(p, both ? most : 0, st);
     // no sequence can be longer than one range: nothing to merge
-    const int shortest = few ? attn::kRowsMinRange : both && attn::kRowsMinRange < attn::kTilesMinRange ? attn::kRowsMinRange
-                                                                                                         : attn::kTilesMinRange;
+    static_assert(attn::kRowsMinRange <= attn::kTilesMinRange, "the row kernel's ranges are the shorter ones");
+    const int shortest = few || both ? attn::kRowsMinRange : attn::kTilesMinRange;
     if (rc != ATTN_OK || ((long long)p.c.table_width << p.c.page_log2) <= (long long)shortest * attn::kPlanBlock)
         return rc;
     constexpr int kGroups = 256 / (D / 4);
     const long long o_rows = (long long)p.c.T * p.H_q;
-    const int walkers = o_rows <= 4096 ? kGroups : 1;
+    // eight ranges to a walker, of as many as a sequence may be expected to have: a launch has one for each head and row tile,
+    // and what the target leaves (twice that, for batches of uneven lengths)
+    const long long most_ranges = ((long long)p.c.table_width << p.c.page_log2) / (shortest * attn::kPlanBlock) + 1;
+    const long long tiles = (long long)p.c.T * p.G / p.parts[many].BM + 1;
+    const long long alone = (p.c.B > tiles ? p.c.B : tiles) * p.c.H_kv;
+    const long long expected = 1 + 2 * attn::kTarget / alone;
+    int walkers = 1;
+    while (walkers < kGroups && 8 * walkers < expected && 8 * walkers < most_ranges)
+        walkers *= 2;
     const long long blocks = (o_rows * walkers + kGroups - 1) / kGroups;
     hipLaunchKernelGGL((attn::attn_paged_merge_kernel<D, typename E::t>), dim3((unsigned)blocks), dim3(256), 0, st, p, walkers);
     return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH;

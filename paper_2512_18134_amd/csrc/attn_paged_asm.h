@@ -25,8 +25,9 @@ struct PagedAsmTiling {
 // eight rows of zeros: what a tile without a page is made of
 __device__ const u32x4 kPagedZeroRows[8 * 512 / 16] = {};
 
+// One unit.
 template <int D, bool F16>
-__global__ __launch_bounds__(PagedAsmTiling<D>::THREADS, 1) void attn_paged_asm_kernel(const PagedParams p)
+__device__ __forceinline__ void attn_paged_asm_unit(const PagedParams &p, const Unit &u, unsigned char *smem)
 {
     typedef typename std::conditional<F16, ElemF16, ElemBF16>::type E;
     typedef typename E::t elem_t;
@@ -37,13 +38,7 @@ __global__ __launch_bounds__(PagedAsmTiling<D>::THREADS, 1) void attn_paged_asm_
     constexpr int NLD = TB / (NW * 1024), RPG = 1024 / ROWB;  // direct loads of a wave, tile and tensor; rows of a load
     constexpr int NQP = 4 * QB * KS / 16;
     static_assert(NLD * RPG == 8, "a wave brings eight rows of a tile");
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     constexpr uint32_t KRING = 0, VRING = 4 * TB;
-
-    Unit u;
-    if (!plan_unit<T::BM>(p, blockIdx.x, u))
-        return;
-    leave_note<T::BM, T::THREADS>(p, u);
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -67,16 +62,9 @@ __global__ __launch_bounds__(PagedAsmTiling<D>::THREADS, 1) void attn_paged_asm_
     typename F32Vec<QB>::type m_ref_v = {}, l_run_v = {};
 
     if (n_tiles > 0) {
-        // ---- pages missing in the range?  (Every lane's sixteenth of a hundred loads or less; one answer for the workgroup.)
         const int *const page_tab = reinterpret_cast<const int *>(scalar64((uintptr_t)(p.c.page_table + (size_t)u.b * p.c.table_width)));
         const int kv_last = scalar(u.kv - 1), end8 = scalar(kv_last & ~7);
         const int page_log2 = scalar(p.c.page_log2), page_mask = scalar((1 << page_log2) - 1), n_pages = scalar(p.c.n_pages);
-        bool miss = false;
-#pragma unroll 4
-        for (int i = (u.key0 >> page_log2) + tid; i <= (key1 - 1) >> page_log2; i += T::THREADS)
-            miss |= (unsigned)page_tab[i] >= (unsigned)n_pages;
-        const int missing = scalar(__syncthreads_or(miss));
-
         // ---- Q: this lane's rows as MFMA B operand (rows behind the last repeat it)
         ex8 bq[QB][KS];
 #pragma unroll
@@ -95,10 +83,17 @@ __global__ __launch_bounds__(PagedAsmTiling<D>::THREADS, 1) void attn_paged_asm_
         const size_t head = ((size_t)u.h << page_log2) * ROWB;
         const uint64_t k_head = scalar64((uintptr_t)p.k + head), v_head = scalar64((uintptr_t)p.v + head);
         const uint64_t zero_rows = scalar64((uintptr_t)kPagedZeroRows);
+        const int first_id = page_tab[min(pos_base + BN * lane, end8) >> page_log2];
+        // ---- pages missing in the range?  One answer for the workgroup (its loads leave with those above)
+        bool miss = false;
+#pragma unroll 4
+        for (int i = (u.key0 >> page_log2) + tid; i <= (key1 - 1) >> page_log2; i += T::THREADS)
+            miss |= (unsigned)page_tab[i] >= (unsigned)n_pages;
+        const int missing = scalar(__syncthreads_or(miss));
+
         u32x4 page_win;
         {
-            const int pos = min(pos_base + BN * lane, end8);
-            const int id = page_tab[pos >> page_log2];
+            const int pos = min(pos_base + BN * lane, end8), id = first_id;
             const bool ok = (unsigned)id < (unsigned)n_pages;
             const size_t at = (size_t)(unsigned)id * (unsigned)page_bytes + (size_t)(pos & page_mask) * ROWB;
             const uint64_t k = ok ? k_head + at : zero_rows;
@@ -255,6 +250,27 @@ __global__ __launch_bounds__(PagedAsmTiling<D>::THREADS, 1) void attn_paged_asm_
             if (g == 0)
                 p.lse[at] = lse;
         }
+    }
+}
+
+// A workgroup takes every gridDim.x-th unit: as many workgroups as run at once, and none that only finds out that there is
+// nothing for it (2100 of those took 11 us of a call of 64 tokens over 500 positions).
+template <int D, bool F16>
+__global__ __launch_bounds__(PagedAsmTiling<D>::THREADS, 1) void attn_paged_asm_kernel(const PagedParams p)
+{
+    typedef PagedAsmTiling<D> T;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    PlanSeq seq;
+    const Plan plan = plan_call<T::BM>(p, seq);
+    for (int wg = blockIdx.x; wg < plan.total; wg += gridDim.x) {
+        const PagedParams again = params_again();
+        Unit u;
+        if (find_unit<T::BM>(again, plan, seq, wg, u)) {
+            leave_note<T::BM, T::THREADS>(again, u);
+            attn_paged_asm_unit<D, F16>(again, u, smem);
+        }
+        __syncthreads();                                      // every wave has left the rings
+        seq = plan_sequence<T::BM>(params_again(), threadIdx.x & 63);
     }
 }
 

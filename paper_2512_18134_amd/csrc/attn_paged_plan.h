@@ -31,9 +31,11 @@ struct PagedParams {
     int causal;
     float c_log2;                       // scale * log2(e)
     // units of this kernel: sequences of rows in (rows_above, rows_upto], cut for `target` workgroups at once that take up to
-    // `rounds` units each; what a unit costs besides its keys, in blocks
-    int rows_above, rows_upto, target, rounds, min_range, overhead;
+    // `rounds` units each; what a unit costs besides its keys and what a merge costs, in blocks
+    int rows_above, rows_upto, target, rounds, min_range, overhead, merging;
     int halve;                          // a chunk's rows see half of the chunk's own keys (causal)
+    int most_units;                     // no batch has more (starts that decrease may claim to)
+    int slots;                          // partial results that the workspace holds for this kernel
     int kernel;                         // 0: attn_paged_rows.h, 1: attn_paged_tiles.h
     // partial results, of either kernel
     struct Parts {
@@ -81,11 +83,33 @@ __device__ __forceinline__ T wave_sum(T x)
     return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wave_prefix(x)), 63));
 }
 
+template <typename T>
+__device__ __forceinline__ T wave_first(T x)
+{
+    return __builtin_bit_cast(T, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+}
+
+__device__ __forceinline__ int wave_max(int x)              // of numbers >= 0
+{
+    auto from = [](int v, auto ctrl, auto rows) { return __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false); };
+    x = max(x, from(x, std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{}));
+    x = max(x, from(x, std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{}));
+    x = max(x, from(x, std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{}));
+    x = max(x, from(x, std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{}));
+    x = max(x, from(x, std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{}));
+    x = max(x, from(x, std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{}));
+    return __builtin_amdgcn_readlane(x, 63);
+}
+
 // Units of one range of a sequence, H heads x n tiles: which one number w is.  Workgroups go to the 8 XCDs in turn; the tiles
 // of a head, which stream the same keys, belong to one XCD (its L2) as far as heads go evenly into XCDs, or to as many as share
 // the head.  Heavier tiles (the last ones, causal) come first and every XCD gets its share of them.
 __host__ __device__ __forceinline__ void place_in_layer(int w, int H, int n, int &h, int &tile)
 {
+    if (n == 1) {
+        h = w, tile = 0;
+        return;
+    }
     const int whole = H / kNumXcd * kNumXcd;                // heads that have an XCD to themselves
     int t;
     if (w < whole * n) {
@@ -110,120 +134,156 @@ __host__ __device__ __forceinline__ void place_in_layer(int w, int H, int n, int
     tile = n - 1 - t;
 }
 
-// Every wave of workgroup `wg` calls this; false: the launch has no unit for it.
+// Rows and positions of a sequence as a kernel of BM-row tiles sees them.
+struct PlanSeq {
+    int tiles, blocks, n, kv, start;
+};
+
 template <int BM>
-__device__ __forceinline__ bool plan_unit(const PagedParams &p, int wg, Unit &u)
+__device__ __forceinline__ PlanSeq plan_sequence(const PagedParams &p, int b)
 {
-    const int lane = threadIdx.x & 63;
-    struct Seq {
-        int tiles, blocks, n, kv;
-    };
-    auto sequence = [&](int b) -> Seq {
-        Seq s = {0, 0, 0, 0};
-        if (b < p.c.B) {
-            s.n = p.c.rows_of(b);
-            s.kv = p.c.length_of(b);
-            const long long rows = (long long)s.n * p.G;
-            if (rows > p.rows_above && rows <= p.rows_upto) {
-                s.tiles = (int)((rows + BM - 1) / BM);
-                s.blocks = s.kv > 0 ? (s.kv - 1) / kPlanBlock + 1 : 1;
-            }
+    PlanSeq s = {0, 0, 0, 0, 0};
+    if (b < p.c.B) {
+        s.start = p.c.start_of(b);
+        s.n = max(p.c.start_of(b + 1) - s.start, 0);
+        s.kv = p.c.length_of(b);
+        const long long rows = (long long)s.n * p.G;
+        if (rows > p.rows_above && rows <= p.rows_upto) {
+            s.tiles = (int)((rows + BM - 1) / BM);
+            s.blocks = s.kv > 0 ? (s.kv - 1) / kPlanBlock + 1 : 1;
         }
-        return s;
+    }
+    return s;
+}
+
+// The cut of a call: units, and 1 / (blocks of a range), 0 for whole sequences.
+struct Plan {
+    int total;
+    float per_block;
+
+    // (to the rounding of a product, the same one everywhere)
+    __device__ __forceinline__ int ranges(const PlanSeq &s) const
+    {
+        return s.tiles ? max(1, (int)ceilf((float)s.blocks * per_block)) : 0;
+    }
+};
+
+// Every wave of a workgroup calls this.  s: plan_sequence of this lane, for find_unit.
+template <int BM>
+__device__ __forceinline__ Plan plan_call(const PagedParams &p, PlanSeq &s)
+{
+    const int lane = threadIdx.x & 63, B = p.c.B;
+    Plan plan;
+    // f(s) for every 64 sequences; up to 64 of them stay in their registers from one pass to the next
+    s = plan_sequence<BM>(p, lane);
+    auto pass = [&](auto f) {
+        f();
+        if (B > 64) {
+            for (int b = 64; b < B; b += 64) {
+                s = plan_sequence<BM>(p, b + lane);
+                f();
+            }
+            s = plan_sequence<BM>(p, lane);
+        }
     };
-    const bool one = p.c.B <= 64;
-    Seq s = sequence(lane);
+    auto sum = [&](auto x) { return B == 1 ? wave_first(x) : wave_sum(x); };
     // work of the call, in (row tile, block, key head)
     float work = 0.f;
-    for (int b = 0;; b += 64) {
+    int tiles = 0, most = 0;
+    pass([&] {
         const float seen = (float)s.blocks - (p.halve ? (float)min(s.n, s.kv) * (0.5f / kPlanBlock) : 0.f);
-        work += wave_sum((float)s.tiles * fmaxf(seen, 1.f));
-        if (b + 64 >= p.c.B)
-            break;
-        s = sequence(b + 64 + lane);
-    }
+        work += sum((float)s.tiles * fmaxf(seen, 1.f));
+        tiles += sum(s.tiles);
+        most = max(most, B == 1 ? wave_first(s.blocks) : wave_max(s.blocks));
+    });
     work *= (float)p.c.H_kv;
-    // Units, and slots of those that are not alone in their sequence and row tile, for ranges of at most L blocks.  (Floats are
-    // enough above: the same ones in every workgroup, and the launch has room for their rounding.)
-    auto ranges_of = [&](const Seq &x, int L) { return x.tiles ? (x.blocks + L - 1) / L : 0; };
-    int total, held;
+    int total, held;                            // units of a key head, and slots of those that share their rows with others
     auto count = [&](int L) {
+        plan.per_block = (1.f - 0x1p-22f) / (float)L;
         total = held = 0;
-        if (!one)
-            s = sequence(lane);
-        for (int b = 0;; b += 64) {
-            const int nr = ranges_of(s, L);
-            total += wave_sum(s.tiles * nr);
-            held += wave_sum(nr > 1 ? s.tiles * nr : 0);
-            if (b + 64 >= p.c.B)
-                break;
-            s = sequence(b + 64 + lane);
-        }
-        return (long long)held * p.c.H_kv <= p.parts[p.kernel].slots;
+        pass([&] {
+            const int nr = plan.ranges(s);
+            total += sum(s.tiles * nr);
+            held += sum(nr > 1 ? s.tiles * nr : 0);
+        });
+        return (long long)held * p.c.H_kv <= p.slots;
     };
-    // A number of units that just exceeds the workgroups that run at once leaves most of them idle in the last round: of the
-    // cuts for one to `rounds` units each the one that ends soonest, each unit with its share of the work and its overhead.
-    int L = 1 << 24;
-    float soonest = INFINITY;
+    // Whole sequences, or a cut into as many units as workgroups run at once, or a few times that many (a number that just
+    // exceeds them leaves most idle in the last round): what ends soonest, each unit with its share of the work and its
+    // overhead, none sooner than the longest, and a cut with the merge behind it.
+    auto ends = [&](int n, int longest) {
+        const float units = (float)n * (float)p.c.H_kv;
+        return fmaxf(ceilf(units / (float)p.target) * (work / fmaxf(units, 1.f) + (float)p.overhead), (float)(longest + p.overhead));
+    };
+    float soonest = ends(tiles, most);
+    int L = 0;                                  // whole sequences
     for (int k = 1; k <= p.rounds; ++k) {
         const int l = max(p.min_range, (int)fminf(ceilf(work / (float)(k * p.target)), 0x1p24f));
-        if (!count(l) && k > 1)
+        if (l >= most)
+            continue;
+        if (!count(l))
             break;
-        const float units = (float)total * (float)p.c.H_kv;
-        const float ends = ceilf(units / (float)p.target) * (work / fmaxf(units, 1.f) + (float)p.overhead);
-        if (k == 1 || ends < soonest)
-            L = l, soonest = ends;
+        const float e = ends(total, l) + (float)p.merging;
+        if (e < soonest)
+            L = l, soonest = e;
         if (l == p.min_range)
             break;
     }
-    while (!count(L) && L < 1 << 24)                // longer ranges where the slots do not suffice
-        L *= 2;
-    auto ranges = [&](const Seq &x) { return ranges_of(x, L); };
-    if (!one)
-        s = sequence(lane);
-    total *= p.c.H_kv;
-    if (wg >= total)
+    if (L == 0)
+        plan.per_block = 0.f, total = tiles;
+    else if (p.rounds > 1)
+        count(L);
+    plan.total = __builtin_amdgcn_readfirstlane(min(total * p.c.H_kv, p.most_units));
+    plan.per_block = wave_first(plan.per_block);
+    return plan;
+}
+
+// Unit `wg` of the call (every wave of a workgroup calls this); false: there is none.  s: plan_sequence of this lane.
+template <int BM>
+__device__ __forceinline__ bool find_unit(const PagedParams &p, const Plan &plan, PlanSeq s, int wg, Unit &u)
+{
+    const int lane = threadIdx.x & 63, B = p.c.B;
+    if (wg >= plan.total)
         return false;
-    const int v = wg;
     int units0 = 0, slots0 = 0;
     for (int b = 0;; b += 64) {
-        const int nr = ranges(s);
+        const int nr = plan.ranges(s);
         const int mine = s.tiles * nr * p.c.H_kv, kept = nr > 1 ? mine : 0;
-        const int after = units0 + wave_prefix(mine), after_slots = slots0 + wave_prefix(kept);
-        const unsigned long long behind = __ballot(after > v);
+        const int after = units0 + (B == 1 ? mine : wave_prefix(mine)), after_slots = slots0 + (B == 1 ? kept : wave_prefix(kept));
+        const unsigned long long behind = __ballot(after > wg);
         if (behind) {
             const int l = __ffsll(behind) - 1;
             auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
             u.b = b + l;
-            u.n = of(s.n), u.kv = of(s.kv);
+            u.n = of(s.n), u.kv = of(s.kv), u.row0 = of(s.start);
             u.n_tiles = of(s.tiles), u.n_ranges = of(nr);
-            const int w = v - of(after - mine);
+            const int w = wg - of(after - mine);
             if (w < 0 || w >= of(mine))        // starts that decrease can count more units than an int holds
                 return false;
             u.slot0 = of(after_slots - kept);
             const int layer = u.n_tiles * p.c.H_kv;
-            u.range = w / layer;
-            place_in_layer(w % layer, p.c.H_kv, u.n_tiles, u.h, u.tile);
+            u.range = u.n_ranges == 1 ? 0 : w / layer;
+            place_in_layer(w - u.range * layer, p.c.H_kv, u.n_tiles, u.h, u.tile);
             u.slot = u.slot0 + (u.range * p.c.H_kv + u.h) * u.n_tiles + u.tile;
-            u.len = ((of(s.blocks) + u.n_ranges - 1) / u.n_ranges) * kPlanBlock;
+            const int blocks = of(s.blocks);
+            u.len = (u.n_ranges == 1 ? blocks : (blocks + u.n_ranges - 1) / u.n_ranges) * kPlanBlock;
             break;
         }
+        if (b + 64 >= B)
+            return false;
         units0 = __builtin_amdgcn_readlane(after, 63);
         slots0 = __builtin_amdgcn_readlane(after_slots, 63);
-        if (b + 64 >= p.c.B)
-            return false;
-        s = sequence(b + 64 + lane);
+        s = plan_sequence<BM>(p, b + 64 + lane);
     }
     u.n_rows = u.n * p.G;
     u.key0 = min(u.range * u.len, u.kv);
     u.key1 = min(u.key0 + u.len, u.kv);
     // the same in all lanes: scalars from here on
     auto scalar = [](int &x) { x = __builtin_amdgcn_readfirstlane(x); };
-    u.row0 = p.c.start_of(u.b);
     scalar(u.row0), scalar(u.b), scalar(u.h), scalar(u.tile), scalar(u.range), scalar(u.key0), scalar(u.key1), scalar(u.slot0);
     scalar(u.slot), scalar(u.n), scalar(u.kv), scalar(u.n_rows), scalar(u.n_tiles), scalar(u.n_ranges);
     // starts that decrease can count rows twice: a slot behind the workspace's last is not written
-    return u.n_ranges == 1 || (unsigned)u.slot < (unsigned)p.parts[p.kernel].slots;
+    return u.n_ranges == 1 || (unsigned)u.slot < (unsigned)p.slots;
 }
 
 // The first unit of every row tile tells the merge kernel about the tokens whose first row lies in the tile.
@@ -238,13 +298,13 @@ __device__ __forceinline__ void leave_note(const PagedParams &p, const Unit &u)
 }
 
 // Partial results -> o and lse.  D/4 lanes hold a row (token, query head), four elements each; `walkers` such groups take
-// a row's ranges in turn, four at a time with their loads in flight together, and meet in LDS.  Few rows: a
+// a row's ranges in turn, eight at a time with their loads in flight together, and meet in LDS.  Few rows: a
 // workgroup to a row, for the bound is then the latency of the walk.  Many: a workgroup to as many rows as it holds, since
 // most of them will have nothing to merge.
 template <int D, typename OUT>
 __global__ __launch_bounds__(256) void attn_paged_merge_kernel(const PagedParams p, int walkers)
 {
-    constexpr int TPR = D / 4, U = 4;
+    constexpr int TPR = D / 4, U = 8;
     __shared__ f32x4 s_acc[256];
     __shared__ f32x2 s_ml[256 / TPR];
     const int group = threadIdx.x / TPR, sub = threadIdx.x % TPR, walker = group % walkers;
@@ -253,9 +313,10 @@ __global__ __launch_bounds__(256) void attn_paged_merge_kernel(const PagedParams
     int n_ranges = 0, BM = 0;
     long long slot = 0, step = 0;
     const float *part_o = nullptr, *part_lse = nullptr;
+    const bool exists = at < (long long)p.c.T * p.H_q;
+    const MergeNote note = p.merge[exists ? t : 0];
     // a token of no sequence has no note: what lies there is old
-    if (at < (long long)p.c.T * p.H_q && t >= p.c.start_of(0) && t < p.c.start_of(p.c.B)) {
-        const MergeNote note = p.merge[t];
+    if (exists && t >= p.c.start_of(0) && t < p.c.start_of(p.c.B)) {
         const PagedParams::Parts &part = p.parts[note.w & 1];
         const int row = (note.w >> 1) + hq % p.G, n_tiles = note.y;
         BM = part.BM, part_o = part.o, part_lse = part.lse;
@@ -305,21 +366,22 @@ __global__ __launch_bounds__(256) void attn_paged_merge_kernel(const PagedParams
         if (sub == 0)
             s_ml[group] = f32x2{m, sum};
         __syncthreads();
-        if (walker == 0) {
-            const float m_own = m;
-            for (int j = 1; j < walkers; ++j)
-                m = fmaxf(m, s_ml[group + j][0]);
-            const float keep = m_own == -INFINITY ? 0.f : expf(m_own - m);
-            sum *= keep;
-            acc *= keep;
-            for (int j = 1; j < walkers; ++j) {
-                const f32x2 ml = s_ml[group + j];
-                if (ml[0] == -INFINITY)
-                    continue;
-                const float w = expf(ml[0] - m);
-                sum += w * ml[1];
-                acc += w * s_acc[threadIdx.x + j * TPR];
+        for (int d = walkers / 2; d > 0; d /= 2) {
+            if (walker < d) {
+                const f32x2 ml = s_ml[group + d];
+                const float m_new = fmaxf(m, ml[0]);
+                const float a = m == -INFINITY ? 0.f : expf(m - m_new), b = ml[0] == -INFINITY ? 0.f : expf(ml[0] - m_new);
+                acc = a * acc + b * s_acc[threadIdx.x + d * TPR];
+                sum = a * sum + b * ml[1];
+                m = m_new;
+                if (d > 1) {
+                    s_acc[threadIdx.x] = acc;
+                    if (sub == 0)
+                        s_ml[group] = f32x2{m, sum};
+                }
             }
+            if (d > 1)
+                __syncthreads();
         }
     }
     if (n_ranges < 1 || walker != 0)

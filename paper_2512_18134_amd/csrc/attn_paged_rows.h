@@ -61,6 +61,16 @@ struct PagedF16 {
     }
 };
 
+// The launch's parameters, read anew from where the launch put them (p is the kernel's only argument): what a loop over units
+// keeps of them across a unit takes registers that the unit needs.
+__device__ __forceinline__ PagedParams params_again()
+{
+    typedef __attribute__((address_space(4))) const PagedParams Arguments;
+    Arguments *args = (Arguments *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(args));
+    return *(const PagedParams *)args;
+}
+
 // 2^(s - 127) of an e4m3 row's exponent byte
 __device__ __forceinline__ float unit_of(uint32_t s) { return __builtin_bit_cast(float, s << 23); }
 
@@ -84,19 +94,22 @@ struct Piece {   // BYTES of memory in dwords
     }
 };
 
-template <int D, int MT>
+template <int D, int MT, int NW>
 struct PagedRowsTiling {
-    static constexpr int BM = 16 * MT, THREADS = 256;
+    static constexpr int BM = 16 * MT, THREADS = NW * 64;
     static constexpr int XP = D == 256 ? 2 : 1;             // parts in which a row's elements meet (64 KB of LDS hold a part)
     static constexpr int ROWF = D / XP + 4;                 // floats of a row of the exchange, padded
     static constexpr int XCH_FLOATS = 4 * 16 * ROWF, ML_FLOATS = 4 * 16 * 2;
 };
 
-// E4M3: the pool's kind.  MT: 16-row column tiles.
-template <int D, int MT, typename E, bool E4M3>
-__global__ __launch_bounds__(256, (MT == 1 && D <= 128) || (MT == 2 && D == 64) ? 2 : 1) void attn_paged_rows_kernel(const PagedParams p)
+// E4M3: the pool's kind.  MT: 16-row column tiles.  NW: waves; 4, or 16 for units that must take whole sequences soon (see
+// attn_paged.hip).
+template <int D, int MT, typename E, bool E4M3, int NW>
+__global__ __launch_bounds__(NW * 64, NW == 4 && ((MT == 1 && D <= 128) || (MT == 2 && D == 64)) ? 2 : 1)
+    void attn_paged_rows_kernel(const PagedParams p)
 {
-    typedef PagedRowsTiling<D, MT> T;
+    typedef PagedRowsTiling<D, MT, NW> T;
+    static_assert(NW == 4 || (NW == 16 && MT == 1 && D <= 128), "the exchange holds four waves at a time");
     constexpr int EB = E4M3 ? 1 : 2;                        // bytes of a cached element
     constexpr int ROWB = D * EB;
     constexpr int KL = ROWB / 64;                           // 16-byte loads of a lane's share of a key
@@ -104,9 +117,12 @@ __global__ __launch_bounds__(256, (MT == 1 && D <= 128) || (MT == 2 && D == 64) 
     constexpr int NV = D / 16;                              // elements of a lane's share of a value row, products of O^T
     __shared__ __attribute__((aligned(16))) float xch[T::XCH_FLOATS];
     __shared__ float ml[T::ML_FLOATS];
+    [[maybe_unused]] __shared__ float xml[NW > 4 ? 512 : 1];   // reference and row sum of four waves' lanes
 
     Unit u;
-    if (!plan_unit<T::BM>(p, blockIdx.x, u))
+    PlanSeq seq;
+    const Plan plan = plan_call<T::BM>(p, seq);
+    if (!find_unit<T::BM>(p, plan, seq, blockIdx.x, u))
         return;
     leave_note<T::BM, T::THREADS>(p, u);
 
@@ -163,7 +179,9 @@ __global__ __launch_bounds__(256, (MT == 1 && D <= 128) || (MT == 2 && D == 64) 
         for (int t = 0; t < 2; ++t)
             id[t] = __builtin_amdgcn_readfirstlane(p.c.page_of(u.b, min(u.key0 + 32 * s + 16 * t, u.kv - 1)));
     };
-    auto load = [&](Step &x, int s, const int id[2]) {
+    // D = 256, two tiles of rows: the accumulators and Q leave registers for the keys or the values, not for both
+    constexpr bool LATE_V = D == 256 && MT == 2;
+    auto load_k = [&](Step &x, int s, const int id[2]) {
         x.bad = (id[0] | id[1]) < 0;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -171,23 +189,27 @@ __global__ __launch_bounds__(256, (MT == 1 && D <= 128) || (MT == 2 && D == 64) 
             const int j = min(u.key0 + 32 * s + 16 * t, (u.kv - 1) & ~15);
             const size_t row = p.c.page_row(max(id[t], 0), u.h) + (j & page_mask);
             const unsigned char *k = static_cast<const unsigned char *>(p.k) + row * ROWB;
-            const unsigned char *v = static_cast<const unsigned char *>(p.v) + row * ROWB;
 #pragma unroll
             for (int i = 0; i < KL; ++i)
                 x.k[t][i].load(k + c * ROWB + g * 16 + i * 64);
+            if (E4M3)
+                x.ks[t] = p.k_scale[row + c];
+        }
+    };
+    auto load_v = [&](Step &x, int s, const int id[2]) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int j = min(u.key0 + 32 * s + 16 * t, (u.kv - 1) & ~15);
+            const size_t row = p.c.page_row(max(id[t], 0), u.h) + (j & page_mask);
+            const unsigned char *v = static_cast<const unsigned char *>(p.v) + row * ROWB;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 x.v[t][i].load(v + (4 * g + i) * ROWB + c * NV * EB);
-            if (E4M3) {
-                x.ks[t] = p.k_scale[row + c];
+            if (E4M3)
                 x.vs[t] = *reinterpret_cast<const uint32_t *>(p.v_scale + row + 4 * g);
-            }
         }
-    };
-
-    auto work = [&](Step &x, int s) {
+        // places that hold no key of this sequence: P is 0 there, but 0 x NaN is not
         const int j0 = u.key0 + 32 * s;
-        // values of places that hold no key of this sequence: P is 0 there, but 0 x NaN is not
         if (x.bad || j0 + 32 > u.kv) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -201,6 +223,12 @@ __global__ __launch_bounds__(256, (MT == 1 && D <= 128) || (MT == 2 && D == 64) 
                             x.vs[t] &= ~(0xffu << (8 * i));   // (an exponent byte of 255 would be infinity)
                     }
         }
+    };
+
+    auto work = [&](Step &x, int s, const int id[2]) {
+        const int j0 = u.key0 + 32 * s;
+        if constexpr (!LATE_V)
+            load_v(x, s, id);
         f32x4 sc[MT][2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -233,6 +261,8 @@ __global__ __launch_bounds__(256, (MT == 1 && D <= 128) || (MT == 2 && D == 64) 
                         if (!x.ok[t] || j0 + 16 * t + 4 * g + i > last[m])
                             sc[m][t][i] = -INFINITY;
         }
+        if constexpr (LATE_V)
+            load_v(x, s, id);
         u32x4 pt[MT];
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
@@ -301,10 +331,37 @@ __global__ __launch_bounds__(256, (MT == 1 && D <= 128) || (MT == 2 && D == 64) 
     if (wave < n_steps) {
         int id[2];
         Step x;
-        for (int s = wave; s < n_steps; s += 4) {
+        for (int s = wave; s < n_steps; s += NW) {
             pages_of(s, id);
-            load(x, s, id);
-            work(x, s);
+            load_k(x, s, id);
+            work(x, s, id);
+        }
+    }
+
+    // ---- more waves than four: the last four hand their results to the four before them, lane by lane, until four are left
+    if constexpr (NW > 4) {
+        static_assert(T::XCH_FLOATS >= 4 * NV * 4 * 64 , "four waves' accumulators");
+#pragma unroll
+        for (int left = NW - 4; left >= 4; left -= 4) {
+            f32x4 *const lanes = reinterpret_cast<f32x4 *>(xch) + (wave & 3) * NV * 64 + lane;
+            float *const stats = xml + (wave & 3) * 128 + lane;
+            if (wave >= left && wave < left + 4) {
+#pragma unroll
+                for (int n = 0; n < NV; ++n)
+                    lanes[n * 64] = o[0][n];
+                stats[0] = mc[0], stats[64] = l[0];
+            }
+            __syncthreads();
+            if (wave >= left - 4 && wave < left) {
+                const float m_other = stats[0], m_new = fmaxf(mc[0], m_other);
+                const float a = __builtin_amdgcn_exp2f(mc[0] - m_new), b = __builtin_amdgcn_exp2f(m_other - m_new);
+                l[0] = l[0] * a + stats[64] * b;
+                mc[0] = m_new;
+#pragma unroll
+                for (int n = 0; n < NV; ++n)
+                    o[0][n] = o[0][n] * a + lanes[n * 64] * b;
+            }
+            __syncthreads();
         }
     }
 
@@ -317,12 +374,12 @@ __global__ __launch_bounds__(256, (MT == 1 && D <= 128) || (MT == 2 && D == 64) 
 #pragma unroll
         for (int x = 0; x < T::XP; ++x) {
             __syncthreads();                                // what lay there has been read
-            if (g == 0) {
+            if (wave < 4 && g == 0) {
                 ml[(wave * 16 + c) * 2] = mc[m];
                 ml[(wave * 16 + c) * 2 + 1] = l[m];
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < 4 && wave < 4; ++i) {
                 float *dst = xch + (wave * 16 + c) * T::ROWF + (4 * g + i) * NX;
 #pragma unroll
                 for (int n = 0; n < NX; n += 4) {
@@ -334,7 +391,7 @@ __global__ __launch_bounds__(256, (MT == 1 && D <= 128) || (MT == 2 && D == 64) 
             // 16 threads of a row, NX elements each
             const int r = threadIdx.x >> 4, part = threadIdx.x & 15;
             const int row = tile_row + 16 * m + r;
-            if (row >= u.n_rows)
+            if (r >= 16 || row >= u.n_rows)
                 continue;
             float top = ml[r * 2];
 #pragma unroll

@@ -38,12 +38,13 @@ struct PagedTilesTiling {
     static constexpr int ROWB = D * 2, TB = BN * ROWB;      // bytes of a tile in LDS
     static constexpr int STAGES = 2;                        // of K and V: tile j is read while j + 1 is written
     // steps of S whose part of Q waits in LDS: 128 registers of O and 64 of Q leave too few for the rest
-    static constexpr int QL = D == 64 ? 0 : D == 256 ? 2 : 4;
+    static constexpr int QL = D == 64 ? 0 : D == 256 ? 4 : 5;
     static constexpr int Q_BYTES = QL * BM * 32, LDS_BYTES = 2 * STAGES * TB + Q_BYTES;
 };
 
+// One unit.
 template <int D, typename E>
-__global__ __launch_bounds__(256, 2) void attn_paged_tiles_kernel(const PagedParams p)
+__device__ __forceinline__ void attn_paged_tiles_unit(const PagedParams &p, const Unit &u, unsigned char *smem)
 {
     typedef PagedTilesTiling<D> T;
     constexpr int QB = T::QB, ROWB = T::ROWB, TB = T::TB, BN = T::BN, ST = T::STAGES;
@@ -52,12 +53,6 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tiles_kernel(const PagedPar
     // what a lane brings of a wave's eight rows: pieces of 16 bytes of memory (D = 64: 8 bytes)
     constexpr int PB = D == 64 ? 8 : 16;
     constexpr int PPR = CROWB / PB, NP = 8 * PPR / 64;      // pieces of a row, of a lane
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-
-    Unit u;
-    if (!plan_unit<T::BM>(p, blockIdx.x, u))
-        return;
-    leave_note<T::BM, T::THREADS>(p, u);
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lq = lane & 31, g = lane >> 5;
@@ -109,15 +104,19 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tiles_kernel(const PagedPar
         // ahead), then of this wave's eight rows, and which tiles have a page missing (scalar).
         const int *const table = p.c.page_table + (size_t)u.b * p.c.table_width;
         auto ask = [&](int t0, int half) -> int { return table[min(u.key0 + BN * (t0 + lane) + 16 * half, u.kv - 1) >> p.c.page_log2]; };
-        int next0 = ask(0, 0), next1 = ask(0, 1), win = 0, win_first = -64;
+        constexpr bool AHEAD = D != 256;                    // (D = 256 has no registers for it)
+        int next0 = AHEAD ? ask(0, 0) : 0, next1 = AHEAD ? ask(0, 1) : 0, win = 0, win_first = -64;
         unsigned long long missing = 0, missing_before = 0;
         auto advance = [&](int t) {                         // before tile t is located for the first time
             if ((t & 63) == 0 && t < n) {
+                if constexpr (!AHEAD)
+                    next0 = ask(t, 0), next1 = ask(t, 1);
                 win = wave < 2 ? next0 : next1;
                 win_first = t;
                 missing_before = missing;
                 missing = __ballot((unsigned)next0 >= (unsigned)p.c.n_pages || (unsigned)next1 >= (unsigned)p.c.n_pages);
-                next0 = ask(t + 64, 0), next1 = ask(t + 64, 1);
+                if constexpr (AHEAD)
+                    next0 = ask(t + 64, 0), next1 = ask(t + 64, 1);
             }
         };
         auto any_missing = [&](int t) -> bool { return (t >= win_first ? missing : missing_before) >> (t & 63) & 1; };
@@ -204,6 +203,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tiles_kernel(const PagedPar
             return __builtin_bit_cast(u32x4, y);
         };
 
+        // D = 256: the next rows are asked for once S has left its registers, otherwise first of all
+        constexpr bool LATE = D == 256;
         auto tile = [&](int j) {
             const uint32_t base = lds0 + (j % ST) * 2 * TB;
             // the offsets of the later steps are made anew in every tile: kept across tiles they take registers from O and Q
@@ -264,6 +265,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tiles_kernel(const PagedPar
                     }
                 l[b] += sum + sum2;
             }
+            if constexpr (LATE)
+                fetch(j + 2);
 #pragma unroll
             for (int kc = 0; kc < 2; ++kc)
 #pragma unroll
@@ -284,7 +287,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tiles_kernel(const PagedPar
             barrier();                                      // tile j is complete, tile j - 1 has been read
             store(j + 1);
             advance(j + 2);
-            fetch(j + 2);
+            if constexpr (!LATE)
+                fetch(j + 2);
             tile(j);
         }
     }
@@ -321,6 +325,26 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tiles_kernel(const PagedPar
             if (g == 0)
                 p.lse[at] = lse;
         }
+    }
+}
+
+// A workgroup takes every gridDim.x-th unit (attn_paged_asm.h).
+template <int D, typename E>
+__global__ __launch_bounds__(256, 2) void attn_paged_tiles_kernel(const PagedParams p)
+{
+    typedef PagedTilesTiling<D> T;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    PlanSeq seq;
+    const Plan plan = plan_call<T::BM>(p, seq);
+    for (int wg = blockIdx.x; wg < plan.total; wg += gridDim.x) {
+        const PagedParams again = params_again();
+        Unit u;
+        if (find_unit<T::BM>(again, plan, seq, wg, u)) {
+            leave_note<T::BM, T::THREADS>(again, u);
+            attn_paged_tiles_unit<D, E>(again, u, smem);
+        }
+        __syncthreads();                                    // every wave has read its last tile
+        seq = plan_sequence<T::BM>(params_again(), threadIdx.x & 63);
     }
 }
 

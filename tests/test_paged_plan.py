@@ -136,9 +136,10 @@ def test_heads_share_xcds_evenly(lib, H, n):
 
 @pytest.mark.parametrize("causal", [0, 1])
 def test_few_slots_make_longer_ranges(lib, causal):
-    units, _, _, n_slots = plan(lib, [0, 900, 900, 901], [5000, 77, 800], 901, 2, 4, 64, 400, n_slots=40, causal=causal)
+    units, _, _, n_slots = plan(lib, [0, 900, 900, 901], [5000, 77, 800], 901, 2, 4, 64, 400, n_slots=230, rounds=4,
+                                target=128, causal=causal)
     assert len({u["slot"] for u in units if u["n_ranges"] > 1}) == sum(u["n_ranges"] > 1 for u in units)
-    assert all(u["n_ranges"] == 1 or u["slot"] < 40 for u in units) and {u["b"] for u in units} == {0, 2}
+    assert all(u["n_ranges"] == 1 or u["slot"] < 230 for u in units) and {u["b"] for u in units} == {0, 2}
     units, _, _, _ = plan(lib, [0, 900, 900, 901], [5000, 77, 800], 901, 2, 4, 64, 400, n_slots=0, causal=causal)
     assert all(u["n_ranges"] == 1 for u in units)
 

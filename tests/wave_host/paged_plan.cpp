@@ -11,7 +11,9 @@ template <int BM>
 void plan(int)
 {
     attn::Unit u = {};
-    const bool f = attn::plan_unit<BM>(p, wg, u);
+    attn::PlanSeq seq;
+    const attn::Plan cut = attn::plan_call<BM>(p, seq);
+    const bool f = attn::find_unit<BM>(p, cut, seq, wg, u);
     unit = u, found = f;
 }
 
@@ -30,8 +32,8 @@ extern "C" int plan_batch(const int *table, const int *start, const int *kv_len,
     p.c.page_table = table, p.c.start = start, p.c.kv_len = kv_len;
     p.c.T = T, p.c.B = B, p.c.H_kv = H_kv, p.c.n_pages = n_pages, p.c.page_log2 = page_log2, p.c.table_width = width;
     p.G = G, p.H_q = G * H_kv;
-    p.rows_above = rows_above, p.rows_upto = rows_upto, p.target = target, p.min_range = min_range, p.parts[0].slots = n_slots, p.causal = causal;
-    p.rounds = rounds, p.overhead = 2, p.halve = causal;
+    p.rows_above = rows_above, p.rows_upto = rows_upto, p.target = target, p.min_range = min_range, p.slots = n_slots, p.causal = causal;
+    p.rounds = rounds, p.overhead = 2, p.merging = 1, p.most_units = n_wg, p.halve = causal;
     p.merge = notes;
     int n = 0;
     for (wg = 0; wg < n_wg; ++wg) {
