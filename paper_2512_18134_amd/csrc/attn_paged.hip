@@ -122,7 +122,7 @@ int launch_tiles(PagedParams p, int above, hipStream_t st)
         kern = reinterpret_cast<const void *>(attn::attn_paged_asm_kernel<D, std::is_same<E, attn::PagedF16>::value>);
         lds = T::LDS_BYTES, threads = T::THREADS;
     }
-    const long long units = most_units(p, p.parts[1].BM), grid = units < p.target ? units : p.target;
+    const long long units = most_units(p, p.parts[1].BM), grid = units < p.target ? units : p.target;   // (a multiple of 8 if less)
     if (units > 0x7fffffffLL)
         return ATTN_ERR_SHAPE;
     p.most_units = (int)units;
@@ -218,6 +218,12 @@ int paged_fwd(const void *q, const long long *strides, void *o, float *lse, cons
     p.q = q, p.o = o, p.lse = lse, p.k = k_pages, p.v = v_pages, p.k_scale = k_scale, p.v_scale = v_scale;
     p.q_st = strides[0], p.q_sh = strides[1];
     p.H_q = H_q, p.G = H_q / H_kv;
+    // see token_of
+    int log_g = 0;
+    while ((1LL << log_g) < p.G)
+        ++log_g;
+    p.g_mul = p.G == 1 ? 0 : (uint32_t)(((1ULL << (31 + log_g)) + p.G - 1) / p.G);
+    p.g_shift = p.G == 1 ? 0 : log_g - 1;
     p.causal = causal != 0;
     p.c_log2 = (float)((double)scale * 1.44269504088896340736);
     unsigned char *const ws = static_cast<unsigned char *>(workspace);

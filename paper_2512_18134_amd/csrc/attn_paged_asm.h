@@ -49,7 +49,7 @@ __device__ __forceinline__ void attn_paged_asm_unit(const PagedParams &p, const 
     const int tile_row = u.tile * T::BM, first_pos = u.kv - u.n;
     auto scalar = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
     auto scalar64 = [&](uint64_t x) { return (uint64_t)(uint32_t)scalar((int)(x >> 32)) << 32 | (uint32_t)scalar((int)x); };
-    auto sees = [&](int row) { return p.causal ? first_pos + min(row, u.n_rows - 1) / p.G : u.kv - 1; };   // last visible key
+    auto sees = [&](int row) { return p.causal ? first_pos + p.token_of(min(row, u.n_rows - 1)) : u.kv - 1; };   // last visible key
     const int key1 = scalar(min(u.key1, sees(tile_row + T::BM - 1) + 1));
     const int n_tiles = scalar(key1 > u.key0 ? (key1 - u.key0 + BN - 1) / BN : 0);
 
@@ -70,7 +70,7 @@ __device__ __forceinline__ void attn_paged_asm_unit(const PagedParams &p, const 
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
             const int row = min(tile_row + (wave * QB + qb) * 32 + lq, u.n_rows - 1);
-            const int i = row / p.G, hq = u.h * p.G + row % p.G;
+            const int i = p.token_of(row), hq = u.h * p.G + row - i * p.G;
             const elem_t *src = static_cast<const elem_t *>(p.q) + (long long)(u.row0 + i) * p.q_st + (long long)hq * p.q_sh + 8 * g;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
@@ -237,7 +237,8 @@ __device__ __forceinline__ void attn_paged_asm_unit(const PagedParams &p, const 
             if (g == 0)
                 p.parts[1].lse[at] = lse;
         } else {
-            const size_t at = (size_t)(u.row0 + row / p.G) * p.H_q + u.h * p.G + row % p.G;
+            const int i = p.token_of(row);
+            const size_t at = (size_t)(u.row0 + i) * p.H_q + u.h * p.G + row - i * p.G;
             elem_t *dst = static_cast<elem_t *>(p.o) + at * D;
 #pragma unroll
             for (int db = 0; db < DB; ++db)
@@ -262,10 +263,10 @@ __global__ __launch_bounds__(PagedAsmTiling<D>::THREADS, 1) void attn_paged_asm_
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     PlanSeq seq;
     const Plan plan = plan_call<T::BM>(p, seq);
-    for (int wg = blockIdx.x; wg < plan.total; wg += gridDim.x) {
+    for (int k = 0; k * (int)gridDim.x < plan.total; ++k) {
         const PagedParams again = params_again();
         Unit u;
-        if (find_unit<T::BM>(again, plan, seq, wg, u)) {
+        if (find_unit<T::BM>(again, plan, seq, unit_of_pass(gridDim.x, k), u)) {
             leave_note<T::BM, T::THREADS>(again, u);
             attn_paged_asm_unit<D, F16>(again, u, smem);
         }

@@ -28,6 +28,7 @@ struct PagedParams {
     const unsigned char *k_scale, *v_scale;
     long long q_st, q_sh;               // strides of q in elements
     int H_q, G;                         // G = H_q / H_kv
+    uint32_t g_mul, g_shift;            // row / G without a division (token_of)
     int causal;
     float c_log2;                       // scale * log2(e)
     // units of this kernel: sequences of rows in (rows_above, rows_upto], cut for `target` workgroups at once that take up to
@@ -44,7 +45,24 @@ struct PagedParams {
         int slots, BM;
     } parts[2];
     int4 *merge;                        // [T]: see MergeNote
+
+    // token of a row of the sequence, row >= 0: row / G = row * ceil(2^(31 + s) / G) / 2^(31 + s), s = ceil(log2 G), exact
+    // below 2^31
+    __device__ __forceinline__ int token_of(int row) const
+    {
+        return G == 1 ? row : (int)((uint32_t)(((uint64_t)(uint32_t)row * g_mul) >> 32) >> g_shift);
+    }
 };
+
+// a / b for a >= 0, b > 0.  The compiler's division is a chain of some 30 instructions, and the plan has a dozen of them in a row;
+// below 2^22 a reciprocal's quotient is off by one at most.
+__device__ __forceinline__ int quotient(int a, int b)
+{
+    if (a >= 1 << 22)
+        return a / b;
+    const int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b)), r = a - q * b;
+    return q + (r >= b) - (r < 0);
+}
 
 // What the merge kernel needs to know of a token: x = first slot of its sequence, y = row tiles of the sequence,
 // z = its ranges, w = first row of the token in its sequence * 2 + kernel.  Only sequences of several ranges have a
@@ -113,21 +131,24 @@ __host__ __device__ __forceinline__ void place_in_layer(int w, int H, int n, int
     const int whole = H / kNumXcd * kNumXcd;                // heads that have an XCD to themselves
     int t;
     if (w < whole * n) {
-        const int x = w % kNumXcd, i = w / kNumXcd;
-        h = i / n * kNumXcd + x;
-        t = i % n;
+        const int x = w % kNumXcd, i = w / kNumXcd, k = quotient(i, n);
+        h = k * kNumXcd + x;
+        t = i - k * n;
     } else {
-        const int rest = H - whole, share = kNumXcd % rest == 0 ? kNumXcd / rest : 1;   // XCDs of a head
+        const int rest = H - whole;
+        const int log_rest = rest == 4 ? 2 : rest == 2 ? 1 : 0, log_share = 3 - log_rest;     // XCDs of a head
+        const bool shared = rest <= 2 || rest == 4;
         w -= whole * n;
-        if (w < n / share * share * rest && share > 1) {
+        const int done = shared ? n >> log_share << log_share : 0;      // tiles dealt out to the XCDs of their head
+        if (w < done * rest) {
             const int x = w % kNumXcd, i = w / kNumXcd;
-            h = x % rest;
-            t = i * share + x / rest;
+            h = x & (rest - 1);
+            t = (i << log_share) + (x >> log_rest);
         } else {
-            const int done = share > 1 ? n / share * share : 0;
             w -= done * rest;
-            h = w % rest;
-            t = done + w / rest;
+            const int k = quotient(w, rest);
+            h = w - k * rest;
+            t = done + k;
         }
         h += whole;
     }
@@ -167,6 +188,14 @@ struct Plan {
         return s.tiles ? max(1, (int)ceilf((float)s.blocks * per_block)) : 0;
     }
 };
+
+// Unit that a workgroup of a launch of `slots` (fewer than units: a multiple of the XCD count) takes in pass k: odd passes
+// run through an XCD's workgroups in reverse, so that who had the heaviest tile of one pass gets the lightest of the next.
+__device__ __forceinline__ int unit_of_pass(int slots, int k)
+{
+    const int wg = blockIdx.x, x = wg % kNumXcd, m = wg / kNumXcd;
+    return k * slots + (k & 1 ? (slots / kNumXcd - 1 - m) * kNumXcd + x : wg);
+}
 
 // Every wave of a workgroup calls this.  s: plan_sequence of this lane, for find_unit.
 template <int BM>
@@ -262,11 +291,11 @@ __device__ __forceinline__ bool find_unit(const PagedParams &p, const Plan &plan
                 return false;
             u.slot0 = of(after_slots - kept);
             const int layer = u.n_tiles * p.c.H_kv;
-            u.range = u.n_ranges == 1 ? 0 : w / layer;
+            u.range = u.n_ranges == 1 ? 0 : quotient(w, layer);
             place_in_layer(w - u.range * layer, p.c.H_kv, u.n_tiles, u.h, u.tile);
             u.slot = u.slot0 + (u.range * p.c.H_kv + u.h) * u.n_tiles + u.tile;
             const int blocks = of(s.blocks);
-            u.len = (u.n_ranges == 1 ? blocks : (blocks + u.n_ranges - 1) / u.n_ranges) * kPlanBlock;
+            u.len = (u.n_ranges == 1 ? blocks : quotient(blocks + u.n_ranges - 1, u.n_ranges)) * kPlanBlock;
             break;
         }
         if (b + 64 >= B)
@@ -292,7 +321,7 @@ __device__ __forceinline__ void leave_note(const PagedParams &p, const Unit &u)
 {
     if (u.range != 0 || u.h != 0 || !p.merge)
         return;
-    const int first = (u.tile * BM + p.G - 1) / p.G, behind = min(((u.tile + 1) * BM + p.G - 1) / p.G, u.n);
+    const int first = p.token_of(u.tile * BM + p.G - 1), behind = min(p.token_of((u.tile + 1) * BM + p.G - 1), u.n);
     for (int i = first + threadIdx.x; i < behind; i += THREADS)
         p.merge[u.row0 + i] = MergeNote{u.slot0, u.n_tiles, u.n_ranges, i * p.G * 2 + p.kernel};
 }

@@ -137,7 +137,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 && ((MT == 1 && D <= 128) || (MT =
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
         const int row = min(tile_row + 16 * m + c, u.n_rows - 1);      // rows behind the last repeat it
-        const int i = row / p.G, hq = u.h * p.G + row % p.G;
+        const int i = p.token_of(row), hq = u.h * p.G + row - i * p.G;
         last[m] = p.causal ? first_pos + i : u.kv - 1;
         const typename E::t *src = static_cast<const typename E::t *>(p.q) + (long long)(u.row0 + i) * p.q_st + (long long)hq * p.q_sh;
 #pragma unroll
@@ -148,7 +148,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 && ((MT == 1 && D <= 128) || (MT =
         }
     }
     // keys that no row of the tile sees are not walked; from `open` on some row does not see a key
-    const int low = tile_row / p.G, high = min(tile_row + T::BM - 1, u.n_rows - 1) / p.G;
+    const int low = p.token_of(tile_row), high = p.token_of(min(tile_row + T::BM - 1, u.n_rows - 1));
     const int key1 = p.causal ? min(u.key1, first_pos + high + 1) : u.key1;
     const int open = p.causal ? min(first_pos + low + 1, u.kv) : u.kv;
     const int n_steps = key1 > u.key0 ? (key1 - u.key0 + 31) / 32 : 0;
@@ -424,7 +424,8 @@ __global__ __launch_bounds__(NW * 64, NW == 4 && ((MT == 1 && D <= 128) || (MT =
                 if (part == 0 && x == 0)
                     p.parts[0].lse[at] = lse;
             } else {
-                const size_t at = (size_t)(u.row0 + row / p.G) * p.H_q + u.h * p.G + row % p.G;
+                const int i = p.token_of(row);
+                const size_t at = (size_t)(u.row0 + i) * p.H_q + u.h * p.G + row - i * p.G;
                 uint32_t *dst = reinterpret_cast<uint32_t *>(static_cast<typename E::t *>(p.o) + at * D + first);
 #pragma unroll
                 for (int n = 0; n < NX / 4; ++n)

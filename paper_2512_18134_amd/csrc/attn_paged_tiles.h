@@ -66,7 +66,7 @@ __device__ __forceinline__ void attn_paged_tiles_unit(const PagedParams &p, cons
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
         const int row = min(tile_row + (wave * QB + b) * 32 + lq, u.n_rows - 1);    // rows behind the last repeat it
-        const int i = row / p.G, hq = u.h * p.G + row % p.G;
+        const int i = p.token_of(row), hq = u.h * p.G + row - i * p.G;
         last[b] = p.causal ? first_pos + i : u.kv - 1;
         const typename E::t *src = static_cast<const typename E::t *>(p.q) + (long long)(u.row0 + i) * p.q_st + (long long)hq * p.q_sh;
 #pragma unroll
@@ -78,7 +78,7 @@ __device__ __forceinline__ void attn_paged_tiles_unit(const PagedParams &p, cons
                 q_lds[(b * T::QL + s - (KS - T::QL)) * 64] = x;    // read by this lane alone
         }
     }
-    const int low = tile_row / p.G, high = min(tile_row + T::BM - 1, u.n_rows - 1) / p.G;
+    const int low = p.token_of(tile_row), high = p.token_of(min(tile_row + T::BM - 1, u.n_rows - 1));
     const int key1 = __builtin_amdgcn_readfirstlane(p.causal ? min(u.key1, first_pos + high + 1) : u.key1);
     // from here on some row does not see a key
     const int open = __builtin_amdgcn_readfirstlane(p.causal ? min(first_pos + low + 1, u.kv) : u.kv);
@@ -121,7 +121,6 @@ __device__ __forceinline__ void attn_paged_tiles_unit(const PagedParams &p, cons
         };
         auto any_missing = [&](int t) -> bool { return (t >= win_first ? missing : missing_before) >> (t & 63) & 1; };
         const int page_mask = (1 << p.c.page_log2) - 1;
-        const int prow = lane / PPR;                        // row of this lane's first piece
         // tile t (tiles behind the last repeat it): page of the wave's rows, their first row in the cache, last row of eight
         auto locate = [&](int &t, int &id, size_t &row, int &most) {
             t = min(t, n - 1);
@@ -138,7 +137,14 @@ __device__ __forceinline__ void attn_paged_tiles_unit(const PagedParams &p, cons
             uint32_t ks[NP], vs[NP];
         };
         Rows x;
+        // (D = 256: places made anew in every tile, as the operands' are below; it has no registers to keep them in)
+        auto anew = [](int x) {
+            if constexpr (D == 256)
+                asm volatile("" : "+v"(x));
+            return x;
+        };
         auto fetch = [&](int t) {
+            const int ln = anew(lane), prow = ln / PPR;     // row of this lane's first piece
             int id, most;
             size_t row;
             locate(t, id, row, most);
@@ -146,7 +152,7 @@ __device__ __forceinline__ void attn_paged_tiles_unit(const PagedParams &p, cons
             const unsigned char *v = static_cast<const unsigned char *>(p.v) + row * CROWB;
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-                const int r = min(i * (64 / PPR) + prow, most), off = r * CROWB + (lane % PPR) * PB;
+                const int r = min(i * (64 / PPR) + prow, most), off = r * CROWB + (ln % PPR) * PB;
                 x.k[i].load(k + off);
                 x.v[i].load(v + off);
                 x.ks[i] = p.k_scale[row + r];
@@ -160,6 +166,7 @@ __device__ __forceinline__ void attn_paged_tiles_unit(const PagedParams &p, cons
             }
         };
         auto store = [&](int t) {
+            const int ln = anew(lane), prow = ln / PPR;
             unsigned char *const k = smem + (t % ST) * 2 * TB, *const v = k + TB;
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
@@ -167,7 +174,7 @@ __device__ __forceinline__ void attn_paged_tiles_unit(const PagedParams &p, cons
                 const float ku = unit_of(x.ks[i]), vu = unit_of(x.vs[i]);
 #pragma unroll
                 for (int e = 0; e < PB / 8; ++e) {
-                    const int c = (lane % PPR) * (PB / 8) + e, at = r * ROWB + (((c & ~15) | ((c & 15) ^ swz<D>(r))) * 16);
+                    const int c = (ln % PPR) * (PB / 8) + e, at = r * ROWB + (((c & ~15) | ((c & 15) ^ swz<D>(r))) * 16);
                     const uint32_t k0 = x.k[i].d[2 * e], k1 = x.k[i].d[2 * e + 1], v0 = x.v[i].d[2 * e], v1 = x.v[i].d[2 * e + 1];
                     *reinterpret_cast<u32x4 *>(k + at) =
                         u32x4{E::template from_e4m3<false>(k0, ku), E::template from_e4m3<true>(k0, ku),
@@ -314,7 +321,8 @@ __device__ __forceinline__ void attn_paged_tiles_unit(const PagedParams &p, cons
             if (g == 0)
                 p.parts[1].lse[at] = lse;
         } else {
-            const size_t at = (size_t)(u.row0 + row / p.G) * p.H_q + u.h * p.G + row % p.G;
+            const int i = p.token_of(row);
+            const size_t at = (size_t)(u.row0 + i) * p.H_q + u.h * p.G + row - i * p.G;
             typename E::t *dst = static_cast<typename E::t *>(p.o) + at * D;
 #pragma unroll
             for (int d = 0; d < DB; ++d)
@@ -336,10 +344,10 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tiles_kernel(const PagedPar
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     PlanSeq seq;
     const Plan plan = plan_call<T::BM>(p, seq);
-    for (int wg = blockIdx.x; wg < plan.total; wg += gridDim.x) {
+    for (int k = 0; k * (int)gridDim.x < plan.total; ++k) {
         const PagedParams again = params_again();
         Unit u;
-        if (find_unit<T::BM>(again, plan, seq, wg, u)) {
+        if (find_unit<T::BM>(again, plan, seq, unit_of_pass(gridDim.x, k), u)) {
             leave_note<T::BM, T::THREADS>(again, u);
             attn_paged_tiles_unit<D, E>(again, u, smem);
         }

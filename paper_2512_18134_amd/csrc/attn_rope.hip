@@ -36,7 +36,8 @@ struct Vec8 {
 
 // A wave holds 64 >> lanes_log2 neighbouring tokens; of a token's head lane c turns the pairs 8c .. 8c+7 (two 16-byte
 // loads) and copies chunks c, c + lanes, ... of the elements behind R.
-template <typename T, bool INTERLEAVED>
+// PAST: stored past the caches, where the outputs would not stay in them until they are read (see rope below).
+template <typename T, bool INTERLEAVED, bool PAST>
 __global__ __launch_bounds__(256) void attn_rope_kernel(const RopeParams p)
 {
     typedef typename Vec8<T>::type t8;
@@ -108,8 +109,14 @@ __global__ __launch_bounds__(256) void attn_rope_kernel(const RopeParams p)
                 }
             }
             if (head + j < head_end) {
-                *reinterpret_cast<t8 *>(out[j] + first) = __builtin_convertvector(a, t8);      // to nearest even
-                *reinterpret_cast<t8 *>(out[j] + second) = __builtin_convertvector(d, t8);
+                const t8 ya = __builtin_convertvector(a, t8), yd = __builtin_convertvector(d, t8);      // to nearest even
+                if (PAST) {
+                    __builtin_nontemporal_store(ya, reinterpret_cast<t8 *>(out[j] + first));
+                    __builtin_nontemporal_store(yd, reinterpret_cast<t8 *>(out[j] + second));
+                } else {
+                    *reinterpret_cast<t8 *>(out[j] + first) = ya;
+                    *reinterpret_cast<t8 *>(out[j] + second) = yd;
+                }
             }
         }
     }
@@ -182,10 +189,18 @@ int rope(const void *q, void *q_out, const void *k, void *k_out, const long long
     if (blocks > 0x7fffffffLL)
         return ATTN_ERR_SHAPE;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (interleaved)
-        hipLaunchKernelGGL((attn::attn_rope_kernel<T, true>), dim3((unsigned)blocks), dim3(256), 0, st, p);
+    // Outputs that the 256 MB of the last-level cache do not hold next to the inputs are stored past the caches: forward and back
+    // of 4 x 32 heads of 4096 tokens, D = 128, 110 us through them, 93 past them; 16 heads of 16384, D = 64 (34 MB), 15.0 and 16.0.
+    const bool past = tokens * heads * D * 2 > (64LL << 20);
+    const dim3 grid((unsigned)blocks), threads(256);
+    if (interleaved && past)
+        hipLaunchKernelGGL((attn::attn_rope_kernel<T, true, true>), grid, threads, 0, st, p);
+    else if (interleaved)
+        hipLaunchKernelGGL((attn::attn_rope_kernel<T, true, false>), grid, threads, 0, st, p);
+    else if (past)
+        hipLaunchKernelGGL((attn::attn_rope_kernel<T, false, true>), grid, threads, 0, st, p);
     else
-        hipLaunchKernelGGL((attn::attn_rope_kernel<T, false>), dim3((unsigned)blocks), dim3(256), 0, st, p);
+        hipLaunchKernelGGL((attn::attn_rope_kernel<T, false, false>), grid, threads, 0, st, p);
     return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH;
 }
 

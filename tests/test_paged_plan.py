@@ -185,3 +185,16 @@ def test_pages_outside_the_pool_are_no_pages(lib, page_log2):
                 got = lib.page_of(ptr(table), ptr(kv_len), 0, 7, page_log2, 7, pos, ctypes.byref(length))
                 assert length.value == most
                 assert got == (want if pos < most else -2)
+
+
+def test_divisions_without_a_division(lib):
+    rng = random.Random(1)
+    for G in list(range(1, 70)) + [96, 100, 127, 128, 129, 1000, 65537, 2 ** 20 + 7, 2 ** 29 + 1]:
+        for k in [0, 1, 5, 1000, (2 ** 31 - 1) // G] + [rng.randrange(2 ** 31 // G) for _ in range(5)]:
+            for row in (k * G - 1, k * G, k * G + 1):
+                if 0 <= row < 2 ** 31:
+                    assert lib.row_over(row, G) == row // G, (row, G)
+    for _ in range(3000):
+        b = rng.choice([1, 2, 3, 7, 8, rng.randrange(1, 5000), rng.randrange(1, 2 ** 22)])
+        a = rng.choice([0, b - 1, b, b * rng.randrange(1, 50), rng.randrange(2 ** 22), 2 ** 22 - 1, 2 ** 22, 2 ** 31 - 1])
+        assert lib.over(a, b) == a // b, (a, b)

@@ -124,5 +124,7 @@ inline int update_dpp(int old, int x, int ctrl, int rows, int, bool)
     return from < 0 || !(rows >> row & 1) ? old : (int)all[from];
 }
 #define __builtin_amdgcn_update_dpp update_dpp
+inline float rcpf(float x) { return 1.f / x; }
+#define __builtin_amdgcn_rcpf rcpf
 #define __builtin_amdgcn_readlane(x, l) wave_host::shuffle(x, l)
 #define __builtin_amdgcn_readfirstlane(x) wave_host::shuffle(x, 0)

@@ -35,6 +35,11 @@ extern "C" int plan_batch(const int *table, const int *start, const int *kv_len,
     p.rows_above = rows_above, p.rows_upto = rows_upto, p.target = target, p.min_range = min_range, p.slots = n_slots, p.causal = causal;
     p.rounds = rounds, p.overhead = 2, p.merging = 1, p.most_units = n_wg, p.halve = causal;
     p.merge = notes;
+    int log_g = 0;
+    while ((1LL << log_g) < G)
+        ++log_g;
+    p.g_mul = G == 1 ? 0 : (uint32_t)(((1ULL << (31 + log_g)) + G - 1) / G);
+    p.g_shift = G == 1 ? 0 : log_g - 1;
     int n = 0;
     for (wg = 0; wg < n_wg; ++wg) {
         if (!wave_host::run(BM == 16 ? plan<16> : BM == 32 ? plan<32> : BM == 64 ? plan<64> : BM == 128 ? plan<128> : plan<256>))
@@ -71,3 +76,16 @@ extern "C" int page_of(const int *table, const int *kv_len, int b, int n_pages, 
 }
 
 extern "C" void layer_place(int w, int H, int n, int *h, int *tile) { attn::place_in_layer(w, H, n, *h, *tile); }
+
+// row / G and a / b as the kernels take them
+extern "C" int row_over(int row, int G)
+{
+    int log_g = 0;
+    while ((1LL << log_g) < G)
+        ++log_g;
+    p.G = G;
+    p.g_mul = G == 1 ? 0 : (uint32_t)(((1ULL << (31 + log_g)) + G - 1) / G);
+    p.g_shift = G == 1 ? 0 : log_g - 1;
+    return p.token_of(row);
+}
+extern "C" int over(int a, int b) { return attn::quotient(a, b); }
