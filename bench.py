@@ -9,6 +9,7 @@
     python bench.py --probe-dq-atomics                  # cost of a single-pass backward's atomic dQ reduction alone
     python bench.py --timeline --config 3               # per-workgroup phase timing of one forward launch (debug build)
     python bench.py --config 3 --compare-lib old.so     # A/B against another build of the library, same process
+    python bench.py --serve 64                          # a layer's decoding step for 64 sequences: rope, cache write, paged attention
 
 A "step" is one attn_fwd call (the whole hot path) over one batch of seeded
 synthetic Q/K/V that is already resident in HBM.  Prints ONE JSON line.
@@ -364,6 +365,74 @@ def compare_lib(args, cfg, entry, qd, kd, vd, o, lse, scale, stream):
             "same_bits": bool(torch.equal(o.view(torch.int16), o2.view(torch.int16)) and torch.equal(lse, lse2))}
 
 
+def serve(args, dev):
+    """One step = one attention layer's part of a decoding step of `--serve` sequences (H_q = 32, H_kv = 8, D = 128, pages of 16
+    positions, lengths drawn up to `--serve-context`, `--serve-new` new tokens each): attn_rope, attn_cache_write and
+    attn_paged_fwd, captured once and replayed while the lengths grow in the device arrays.  Prints one JSON line."""
+    import torch
+    from paper_2512_18134_amd import binding
+
+    B, n, H_q, H_kv, D, page = args.serve, args.serve_new, 32, 8, 128, 16
+    rounds = args.warmup + args.steps
+    f16, e4m3 = (args.dtype or "bf16") == "f16", args.serve_cache == "e4m3"
+    dt = torch.float16 if f16 else torch.bfloat16
+    rope, write, attend = (getattr(binding, name + ("_f16" if f16 else ""))
+                           for name in ("attn_rope", "attn_cache_write", "attn_paged_fwd"))
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(400)
+    kv = torch.randint(args.serve_context // 8, args.serve_context + 1, (B,), generator=gen, device=dev, dtype=torch.int32)
+    width = -(-(args.serve_context + n * (rounds + 3)) // page)
+    table = torch.randperm(B * width, generator=gen, device=dev).to(torch.int32).view(B, width)
+    shape = (B * width, H_kv, page, D)
+    if e4m3:
+        pool = [torch.randint(0, 0x70, shape, generator=gen, device=dev, dtype=torch.uint8).view(torch.float8_e4m3fn) for _ in "kv"]
+        units = [torch.full(shape[:3], 118, device=dev, dtype=torch.uint8) for _ in "kv"]
+    else:
+        pool, units = [torch.randn(shape, generator=gen, device=dev, dtype=dt) for _ in "kv"], [None, None]
+    start = torch.arange(B + 1, device=dev, dtype=torch.int32) * n
+    rows = torch.randn((B * n, H_q + 2 * H_kv, D), generator=gen, device=dev, dtype=dt)
+    new = torch.arange(n, device=dev, dtype=torch.int32)
+    freq = 10000.0 ** (-torch.arange(D // 2, device=dev, dtype=torch.float64) / (D // 2))
+    turned = [torch.empty((B * n, h, D), device=dev, dtype=dt) for h in (H_q, H_kv)]
+    o, lse = torch.empty_like(turned[0]), torch.empty((B * n, H_q), device=dev)
+    ws = torch.empty(binding.attn_paged_fwd_workspace_bytes(B * n, B, H_q, H_kv, D), dtype=torch.uint8, device=dev)
+    heads = lambda x: x.transpose(0, 1)[None]
+
+    def step():
+        kv.add_(n)
+        pos = (kv[:, None] - n + new).view(1, 1, B * n)
+        rope(heads(rows[:, :H_q]), heads(rows[:, H_q:H_q + H_kv]), pos, freq, (D // 2,), *map(heads, turned))
+        write(turned[1], rows[:, H_q + H_kv:], *pool, table, start, kv, *units)
+        attend(turned[0], *pool, table, start, kv, *units, o=o, lse=lse, workspace=ws, max_q=n)
+
+    side = torch.cuda.Stream(dev)
+    side.wait_stream(torch.cuda.current_stream(dev))
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream(dev).wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    before = int(kv.sum())
+    for _ in range(args.warmup):
+        graph.replay()
+    torch.cuda.synchronize()
+    t0 = time.perf_counter()
+    for _ in range(args.steps):
+        graph.replay()
+    torch.cuda.synchronize()
+    ms = (time.perf_counter() - t0) * 1e3 / args.steps
+    keys = before + B * n * (args.warmup + (args.steps + 1) / 2)             # cached positions of a step, in the mean
+    nbytes = keys * H_kv * 2 * (D + 1 if e4m3 else 2 * D)
+    print(json.dumps({
+        "metric": "decoding steps of one attention layer, tokens/s at 1 GPU (%s rows, %s cache)" % (args.dtype or "bf16", args.serve_cache),
+        "value": B * n / ms * 1e3, "unit": "tokens/s", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup, "ms_per_step": ms,
+        "higher_is_better": True, "scaling": "weak", "vs_baseline": None, "dtype": args.dtype or "bf16", "data": "synthetic",
+        "config": {"workload": "serve_B%d_n%d_Hq%d_Hkv%d_D%d_page%d" % (B, n, H_q, H_kv, D, page), "cached_positions": keys,
+                   "cache": args.serve_cache},
+        "roofline": {"bound": "hbm", "achieved": nbytes / ms / 1e9, "peak": 8.0, "unit": "TB/s", "frac": nbytes / ms / 8e9}}), flush=True)
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -391,6 +460,12 @@ def main():
                     help="time attn_fwd_splitkv with this many key ranges on the long-context shape "
                          "(B=1, H=8, S_q=256, S_kv=131072, D=128, non-causal; --long-skv changes S_kv)")
     ap.add_argument("--long-skv", type=int, default=131072)
+    ap.add_argument("--serve", type=int, default=0,
+                    help="time one attention layer's decoding step of this many sequences instead (rope, cache write, paged "
+                         "attention, replayed from a graph)")
+    ap.add_argument("--serve-context", type=int, default=8192, help="with --serve: the longest sequence")
+    ap.add_argument("--serve-new", type=int, default=1, help="with --serve: new tokens of a sequence in a step")
+    ap.add_argument("--serve-cache", choices=["16bit", "e4m3"], default="16bit", help="with --serve: elements of the cache")
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--compare-lib", default="",
                     help="also time the forward call through this other build of libmi355attn.so, interleaved "
@@ -425,6 +500,8 @@ def main():
         return probe_dq_atomics(args, dev)
     if args.timeline:
         return timeline(args, dev)
+    if args.serve:
+        return serve(args, dev)
     if args.splitkv:
         cfg = dict(name="long_B1_H8_Sq256_Skv%d_D128_full_split%d" % (args.long_skv, args.splitkv), B=1, H=8, S_q=256,
                    S_kv=args.long_skv, D=128, causal=False, seed=300, sharp=False, dtype="bf16")

@@ -699,19 +699,19 @@ extern "C" const char *attn_strerror(int status)
     case ATTN_ERR_NULL:
         return "a required pointer is NULL";
     case ATTN_ERR_SHAPE:
-        return "B, H, S_q, S_kv must be >= 1 and the tensors must not exceed 2^40 elements";
+        return "sizes must be >= 1 (B, H, S_q, S_kv ...), the tensors within 2^40 elements and the entry point's own limits";
     case ATTN_ERR_UNSUPPORTED_D:
         return "head dimension D must be 64, 128 or 256";
     case ATTN_ERR_ALIGN:
-        return "q, k, v, o must be 16-byte aligned and lse 4-byte aligned";
+        return "element tensors (q, k, v, o ...) must be 16-byte aligned, lse and int32 arrays 4-byte aligned, fp64 arrays 8-byte aligned";
     case ATTN_ERR_SCALE:
         return "scale must be finite and >= 0";
     case ATTN_ERR_LAUNCH:
         return "the HIP runtime rejected the kernel launch";
     case ATTN_ERR_UNSUPPORTED:
-        return "this entry point does not implement the requested combination (e.g. causal split-KV)";
+        return "this entry point does not implement the requested combination (e.g. causal split-KV, a page size that is no power of two)";
     case ATTN_ERR_WORKSPACE:
-        return "the workspace is too small: smaller than attn_fwd_splitkv_workspace_bytes() asks for, or the shape exceeds "
+        return "the workspace is too small: smaller than the entry point's ..._workspace_bytes() asks for, or the shape exceeds "
                "the built-in workspace of attn_bwd_noalloc (B*H*S_q <= 2^21)";
     }
     return "unknown attn_status";

@@ -221,3 +221,13 @@ def test_pages_far_behind_the_pools_start(n, e4m3):
     c = Cache([n], [kv], H, D, page, "bf16", False, 82)
     ref = R.attention(q.double(), *small, torch.tensor([[0, 1, 2]], dtype=torch.int32), c.start, c.kv_len, True, D ** -0.5)
     check_attention(c, o.cpu(), lse.cpu(), ref)
+
+
+@pytest.mark.parametrize("extra", [(), ("--serve-cache", "e4m3", "--serve-new", "3", "--dtype", "f16")], ids=["bf16", "f16_e4m3"])
+def test_bench_line_of_a_decoding_step(extra):
+    from test_bench_tools_gpu import run_bench
+    d = run_bench("--serve", "8", "--serve-context", "2000", "--steps", "5", "--warmup", "2", *extra)
+    for key in ("metric", "value", "unit", "n_gpus", "steps", "warmup", "ms_per_step", "higher_is_better", "scaling",
+                "vs_baseline", "dtype", "data", "config", "roofline"):
+        assert key in d, key
+    assert d["value"] > 0 and d["steps"] == 5 and 0 < d["roofline"]["frac"] < 1
