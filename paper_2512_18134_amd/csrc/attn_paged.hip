@@ -25,8 +25,11 @@ constexpr int kRowsRounds = 1, kTilesRounds = 4;
 constexpr int kRowsOverhead = 1, kTilesOverhead = 4, kRowsMerging = 1, kTilesMerging = 12;
 // A range of fewer blocks (of kPlanBlock keys) costs more to merge than its walk by another workgroup saves.
 constexpr int kRowsMinRange = 2, kTilesMinRange = 4;
-// bytes of K and V of one key head up to which a sequence is walked by one workgroup of sixteen waves
+// Bytes of K and V of one key head up to which a sequence is walked by one workgroup, of kWaves waves, without a cut and without
+// a merge.  One sequence of 8 key heads, D = 128, 500 keys: 9.0 us whole, 9.6 cut; 16 of them 10.0 and 13.2; of twice the
+// keys 13.6 whole, 9.9 cut.
 constexpr long long kWholeBytes = 1 << 18;
+constexpr int kWaves = 8;
 constexpr int kSlots = 2 * kTarget + 64;
 
 // rows of a sequence up to which the row kernel takes it
@@ -87,7 +90,10 @@ int launch_rows(PagedParams p, int upto, hipStream_t st)
     if (grid > 0x7fffffffLL)
         return ATTN_ERR_SHAPE;
     p.most_units = (int)grid;
-    hipLaunchKernelGGL((attn::attn_paged_rows_kernel<D, MT, E, E4M3, NW>), dim3((unsigned)grid), dim3(NW * 64), 0, st, p);
+    constexpr int lds = attn::PagedRowsTiling<D, MT, NW>::LDS_BYTES;
+    if (!attn::allow_lds(reinterpret_cast<const void *>(attn::attn_paged_rows_kernel<D, MT, E, E4M3, NW>), lds))
+        return ATTN_ERR_LAUNCH;
+    hipLaunchKernelGGL((attn::attn_paged_rows_kernel<D, MT, E, E4M3, NW>), dim3((unsigned)grid), dim3(NW * 64), lds, st, p);
     return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH;
 }
 
@@ -147,12 +153,11 @@ int launch(PagedParams &p, int max_q, hipStream_t st)
     const int MT = attn::row_tiles(D, rows < most ? rows : most);
     p.parts[0].BM = 16 * MT, p.parts[1].BM = E4M3 ? attn::PagedTilesTiling<D>::BM : attn::PagedAsmTiling<D>::BM;
     int rc = ATTN_OK;
-    // Short sequences, and no more of them than compute units: sixteen waves walk one without a cut, and there is nothing to
-    // merge.  (The bound is what the page table can hold.)
+    // Short sequences, and no more of them than compute units.  (The bound is what the page table can hold.)
     if constexpr (D != 256)
         if (few && MT == 1 && ((long long)p.c.T * p.G / 16 + (p.c.B < p.c.T ? p.c.B : p.c.T)) * p.c.H_kv <= attn::kTarget / 2 &&
             ((long long)p.c.table_width << p.c.page_log2) * D * (E4M3 ? 2 : 4) <= attn::kWholeBytes)
-            return launch_rows<D, 1, E, E4M3, 16>(p, 0x7fffffff, st);
+            return launch_rows<D, 1, E, E4M3, attn::kWaves>(p, 0x7fffffff, st);
     if (few || both)
         rc = launch_rows<D, E, E4M3>(p, MT, both ? most : 0x7fffffff, st);
     if (rc == ATTN_OK && many)

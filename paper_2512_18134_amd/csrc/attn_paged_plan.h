@@ -336,25 +336,28 @@ __global__ __launch_bounds__(256) void attn_paged_merge_kernel(const PagedParams
     constexpr int TPR = D / 4, U = 8;
     __shared__ f32x4 s_acc[256];
     __shared__ f32x2 s_ml[256 / TPR];
-    const int group = threadIdx.x / TPR, sub = threadIdx.x % TPR, walker = group % walkers;
-    const long long at = (long long)blockIdx.x * (256 / TPR / walkers) + group / walkers;
-    const int t = (int)(at / p.H_q), hq = (int)(at % p.H_q);
-    int n_ranges = 0, BM = 0;
+    const int group = threadIdx.x / TPR, sub = threadIdx.x % TPR, walker = group & (walkers - 1);
+    const int log_walkers = __builtin_ctz(walkers);            // powers of two, both, and T H_q < 2^30
+    const int at = (int)blockIdx.x * (256 / TPR >> log_walkers) + (group >> log_walkers);
+    const int t = quotient(at, p.H_q), hq = at - t * p.H_q;
+    int n_ranges = 0;
     long long slot = 0, step = 0;
     const float *part_o = nullptr, *part_lse = nullptr;
-    const bool exists = at < (long long)p.c.T * p.H_q;
+    const bool exists = at < p.c.T * p.H_q;
     const MergeNote note = p.merge[exists ? t : 0];
     // a token of no sequence has no note: what lies there is old
     if (exists && t >= p.c.start_of(0) && t < p.c.start_of(p.c.B)) {
-        const PagedParams::Parts &part = p.parts[note.w & 1];
-        const int row = (note.w >> 1) + hq % p.G, n_tiles = note.y;
-        BM = part.BM, part_o = part.o, part_lse = part.lse;
-        if (note.z > 1 && note.z <= part.slots && n_tiles >= 1 && row >= 0 && BM > 0 && row / BM < n_tiles && note.x >= 0) {
+        const bool tiles = note.w & 1;
+        const int h = quotient(hq, p.G), row = (note.w >> 1) + hq - h * p.G, n_tiles = note.y;
+        const int slots = tiles ? p.parts[1].slots : p.parts[0].slots, BM = tiles ? p.parts[1].BM : p.parts[0].BM;
+        part_o = tiles ? p.parts[1].o : p.parts[0].o, part_lse = tiles ? p.parts[1].lse : p.parts[0].lse;
+        const int log_bm = __builtin_ctz(BM);
+        if (note.z > 1 && note.z <= slots && n_tiles >= 1 && row >= 0 && row >> log_bm < n_tiles && note.x >= 0) {
             step = (long long)p.c.H_kv * n_tiles;
-            slot = note.x + (long long)(hq / p.G) * n_tiles + row / BM;
-            n_ranges = slot + (note.z - 1) * step < part.slots ? note.z : 0;
-            slot = slot * BM + row % BM;
-            step *= BM;
+            slot = note.x + (long long)h * n_tiles + (row >> log_bm);
+            n_ranges = slot + (note.z - 1) * step < slots ? note.z : 0;
+            slot = (slot << log_bm) + (row & (BM - 1));
+            step <<= log_bm;
         }
     }
     float m = -INFINITY, sum = 0.f;
@@ -417,7 +420,7 @@ __global__ __launch_bounds__(256) void attn_paged_merge_kernel(const PagedParams
         return;
     acc *= sum > 0.f ? 1.f / sum : 0.f;
     typedef OUT out4 __attribute__((ext_vector_type(4)));
-    *reinterpret_cast<out4 *>(static_cast<OUT *>(p.o) + at * D + 4 * sub) = __builtin_convertvector(acc, out4);
+    *reinterpret_cast<out4 *>(static_cast<OUT *>(p.o) + (size_t)at * D + 4 * sub) = __builtin_convertvector(acc, out4);
     if (sub == 0)
         p.lse[at] = m + logf(sum);       // -inf where there is no key
 }

@@ -2,7 +2,7 @@
 //
 // What bounds it is the cache: every key and value is read once and used for at most 16 MT rows, so the kernel is a
 // stream from memory into registers with the products along the way.  Nothing of the stream passes through LDS and no wave
-// waits for another: the four waves of a workgroup take the 32-key steps of their unit's range in turn, each
+// waits for another: the waves of a workgroup take the 32-key steps of their unit's range in turn, each
 // with a softmax of its own, and meet once at the end.
 //
 // Transposed products on v_mfma_f32_16x16x32: S^T = K Q^T, O^T = V^T P^T.  Lane l has column c = l % 16 (a row of the tile:
@@ -97,27 +97,31 @@ struct Piece {   // BYTES of memory in dwords
 template <int D, int MT, int NW>
 struct PagedRowsTiling {
     static constexpr int BM = 16 * MT, THREADS = NW * 64;
+    static constexpr int PER_SIMD = NW > 4 ? NW / 4 : (MT == 1 && D <= 128) || (MT == 2 && D == 64) ? 2 : 1;   // waves, at least
+    static constexpr int PER_CU = PER_SIMD * 4 / NW;        // workgroups
     static constexpr int XP = D == 256 ? 2 : 1;             // parts in which a row's elements meet (64 KB of LDS hold a part)
     static constexpr int ROWF = D / XP + 4;                 // floats of a row of the exchange, padded
-    static constexpr int XCH_FLOATS = 4 * 16 * ROWF, ML_FLOATS = 4 * 16 * 2;
+    static constexpr int XCH_FLOATS = NW * 16 * ROWF, ML_FLOATS = NW * 16 * 2;
+    static constexpr int LDS_BYTES = (XCH_FLOATS + ML_FLOATS) * 4;
 };
 
-// E4M3: the pool's kind.  MT: 16-row column tiles.  NW: waves; 4, or 16 for units that must take whole sequences soon (see
-// attn_paged.hip).
+// E4M3: the pool's kind.  MT: 16-row column tiles.  NW: waves; 4, or 8 where a unit is a whole short sequence (kWholeBytes in
+// attn_paged.hip).  The waves' results meet in one exchange: handed on by four waves at a time, sixteen waves took 3.5 us of
+// a launch's 9.
 template <int D, int MT, typename E, bool E4M3, int NW>
-__global__ __launch_bounds__(NW * 64, NW == 4 && ((MT == 1 && D <= 128) || (MT == 2 && D == 64)) ? 2 : 1)
+__global__ __launch_bounds__(NW * 64, (PagedRowsTiling<D, MT, NW>::PER_CU))
     void attn_paged_rows_kernel(const PagedParams p)
 {
     typedef PagedRowsTiling<D, MT, NW> T;
-    static_assert(NW == 4 || (NW == 16 && MT == 1 && D <= 128), "the exchange holds four waves at a time");
+    static_assert(NW == 4 || (MT == 1 && D <= 128), "the exchange holds all waves of 16 rows");
     constexpr int EB = E4M3 ? 1 : 2;                        // bytes of a cached element
     constexpr int ROWB = D * EB;
     constexpr int KL = ROWB / 64;                           // 16-byte loads of a lane's share of a key
     constexpr int KS = D / 32;                              // products of S^T
     constexpr int NV = D / 16;                              // elements of a lane's share of a value row, products of O^T
-    __shared__ __attribute__((aligned(16))) float xch[T::XCH_FLOATS];
-    __shared__ float ml[T::ML_FLOATS];
-    [[maybe_unused]] __shared__ float xml[NW > 4 ? 512 : 1];   // reference and row sum of four waves' lanes
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    float *const xch = reinterpret_cast<float *>(lds);
+    f32x2 *const ml = reinterpret_cast<f32x2 *>(xch + T::XCH_FLOATS);      // reference and row sum of a wave's rows
 
     Unit u;
     PlanSeq seq;
@@ -173,14 +177,23 @@ __global__ __launch_bounds__(NW * 64, NW == 4 && ((MT == 1 && D <= 128) || (MT =
         bool ok[2];
     };
     const int page_mask = (1 << p.c.page_log2) - 1;
-    // pages of the two 16-key blocks of step s (uniform; pages hold a multiple of 16 positions)
+    // Pages of the two 16-key blocks (pages hold a multiple of 16 positions) of the wave's next 32 steps, one in a lane: asked
+    // for step by step, a page's number would have to arrive before its keys could be asked for.
+    int window = 0, turn = 0;
     auto pages_of = [&](int s, int id[2]) {
+        if ((turn & 31) == 0)
+            window = p.c.page_of(u.b, min(u.key0 + 32 * (s + NW * (lane >> 1)) + 16 * (lane & 1), u.kv - 1));
 #pragma unroll
         for (int t = 0; t < 2; ++t)
-            id[t] = __builtin_amdgcn_readfirstlane(p.c.page_of(u.b, min(u.key0 + 32 * s + 16 * t, u.kv - 1)));
+            id[t] = __builtin_amdgcn_readlane(window, 2 * (turn & 31) + t);
+        ++turn;
     };
     // D = 256, two tiles of rows: the accumulators and Q leave registers for the keys or the values, not for both
     constexpr bool LATE_V = D == 256 && MT == 2;
+    // The next step's keys are on their way during a step where they are few registers (16): 8 heads of 2000 keys, D = 128, e4m3,
+    // 14.6 us without and 13.7 with them, 16 heads of 1000, D = 64, 9.2 and 9.0.  At 32 registers the second copy of the loop
+    // gains nothing: 64 sequences of up to 8191 keys, D = 128, 16 bits, 180 and 189 us, of up to 500 keys 19.4 and 20.5.
+    constexpr bool AHEAD = KL <= 2 && !LATE_V;
     auto load_k = [&](Step &x, int s, const int id[2]) {
         x.bad = (id[0] | id[1]) < 0;
 #pragma unroll
@@ -208,6 +221,8 @@ __global__ __launch_bounds__(NW * 64, NW == 4 && ((MT == 1 && D <= 128) || (MT =
             if (E4M3)
                 x.vs[t] = *reinterpret_cast<const uint32_t *>(p.v_scale + row + 4 * g);
         }
+    };
+    auto mask_v = [&](Step &x, int s) {
         // places that hold no key of this sequence: P is 0 there, but 0 x NaN is not
         const int j0 = u.key0 + 32 * s;
         if (x.bad || j0 + 32 > u.kv) {
@@ -228,7 +243,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 && ((MT == 1 && D <= 128) || (MT =
     auto work = [&](Step &x, int s, const int id[2]) {
         const int j0 = u.key0 + 32 * s;
         if constexpr (!LATE_V)
-            load_v(x, s, id);
+            mask_v(x, s);
         f32x4 sc[MT][2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -261,8 +276,10 @@ __global__ __launch_bounds__(NW * 64, NW == 4 && ((MT == 1 && D <= 128) || (MT =
                         if (!x.ok[t] || j0 + 16 * t + 4 * g + i > last[m])
                             sc[m][t][i] = -INFINITY;
         }
-        if constexpr (LATE_V)
+        if constexpr (LATE_V) {
             load_v(x, s, id);
+            mask_v(x, s);
+        }
         u32x4 pt[MT];
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
@@ -331,41 +348,43 @@ __global__ __launch_bounds__(NW * 64, NW == 4 && ((MT == 1 && D <= 128) || (MT =
     if (wave < n_steps) {
         int id[2];
         Step x;
-        for (int s = wave; s < n_steps; s += NW) {
-            pages_of(s, id);
-            load_k(x, s, id);
+        pages_of(wave, id);
+        load_k(x, wave, id);
+        if constexpr (AHEAD) {
+            Step y;
+            int s = wave;
+            auto ahead = [&](Step &now, Step &next) {
+                load_v(now, s, id);
+                if (s + NW >= n_steps)
+                    return false;
+                pages_of(s + NW, id);
+                load_k(next, s + NW, id);
+                work(now, s, id);
+                s += NW;
+                return true;
+            };
+            while (ahead(x, y)) {
+                if (!ahead(y, x)) {
+                    x = y;
+                    break;
+                }
+            }
             work(x, s, id);
+        } else {
+            for (int s = wave;;) {
+                if constexpr (!LATE_V)
+                    load_v(x, s, id);
+                work(x, s, id);
+                s += NW;
+                if (s >= n_steps)
+                    break;
+                pages_of(s, id);
+                load_k(x, s, id);
+            }
         }
     }
 
-    // ---- more waves than four: the last four hand their results to the four before them, lane by lane, until four are left
-    if constexpr (NW > 4) {
-        static_assert(T::XCH_FLOATS >= 4 * NV * 4 * 64 , "four waves' accumulators");
-#pragma unroll
-        for (int left = NW - 4; left >= 4; left -= 4) {
-            f32x4 *const lanes = reinterpret_cast<f32x4 *>(xch) + (wave & 3) * NV * 64 + lane;
-            float *const stats = xml + (wave & 3) * 128 + lane;
-            if (wave >= left && wave < left + 4) {
-#pragma unroll
-                for (int n = 0; n < NV; ++n)
-                    lanes[n * 64] = o[0][n];
-                stats[0] = mc[0], stats[64] = l[0];
-            }
-            __syncthreads();
-            if (wave >= left - 4 && wave < left) {
-                const float m_other = stats[0], m_new = fmaxf(mc[0], m_other);
-                const float a = __builtin_amdgcn_exp2f(mc[0] - m_new), b = __builtin_amdgcn_exp2f(m_other - m_new);
-                l[0] = l[0] * a + stats[64] * b;
-                mc[0] = m_new;
-#pragma unroll
-                for (int n = 0; n < NV; ++n)
-                    o[0][n] = o[0][n] * a + lanes[n * 64] * b;
-            }
-            __syncthreads();
-        }
-    }
-
-    // ---- the four waves' results meet, 16 rows at a time
+    // ---- the waves' results meet, 16 rows at a time
     constexpr int NX = NV / T::XP;
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
@@ -374,12 +393,11 @@ __global__ __launch_bounds__(NW * 64, NW == 4 && ((MT == 1 && D <= 128) || (MT =
 #pragma unroll
         for (int x = 0; x < T::XP; ++x) {
             __syncthreads();                                // what lay there has been read
-            if (wave < 4 && g == 0) {
-                ml[(wave * 16 + c) * 2] = mc[m];
-                ml[(wave * 16 + c) * 2 + 1] = l[m];
-            }
+            const bool exists = tile_row + 16 * m + c < u.n_rows;
+            if (g == 0)
+                ml[wave * 16 + c] = f32x2{mc[m], l[m]};
 #pragma unroll
-            for (int i = 0; i < 4 && wave < 4; ++i) {
+            for (int i = 0; i < 4 && exists; ++i) {
                 float *dst = xch + (wave * 16 + c) * T::ROWF + (4 * g + i) * NX;
 #pragma unroll
                 for (int n = 0; n < NX; n += 4) {
@@ -388,48 +406,42 @@ __global__ __launch_bounds__(NW * 64, NW == 4 && ((MT == 1 && D <= 128) || (MT =
                 }
             }
             __syncthreads();
-            // 16 threads of a row, NX elements each
-            const int r = threadIdx.x >> 4, part = threadIdx.x & 15;
+            // NW * 4 threads of a row, EPT elements each
+            constexpr int TPR = NW * 4, EPT = D / T::XP / TPR;
+            typedef float elements __attribute__((ext_vector_type(EPT)));
+            const int r = threadIdx.x / TPR, part = threadIdx.x % TPR;
             const int row = tile_row + 16 * m + r;
-            if (r >= 16 || row >= u.n_rows)
+            if (row >= u.n_rows)
                 continue;
-            float top = ml[r * 2];
+            float top = ml[r][0];
 #pragma unroll
-            for (int w = 1; w < 4; ++w)
-                top = fmaxf(top, ml[(w * 16 + r) * 2]);
-            float sum = 0.f, weight[4];
+            for (int w = 1; w < NW; ++w)
+                top = fmaxf(top, ml[w * 16 + r][0]);
+            float sum = 0.f;
+            elements y = {};
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                weight[w] = __builtin_amdgcn_exp2f(ml[(w * 16 + r) * 2] - top);
-                sum += weight[w] * ml[(w * 16 + r) * 2 + 1];
+            for (int w = 0; w < NW; ++w) {
+                const f32x2 stats = ml[w * 16 + r];
+                const float weight = __builtin_amdgcn_exp2f(stats[0] - top);
+                sum += weight * stats[1];
+                y += weight * *reinterpret_cast<const elements *>(xch + (w * 16 + r) * T::ROWF + part * EPT);
             }
             const float inv = sum > 0.f ? 1.f / sum : 0.f;
             const float lse = sum > 0.f ? (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f : -INFINITY;
-            f32x4 y[NX / 4];
-#pragma unroll
-            for (int n = 0; n < NX / 4; ++n) {
-                y[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int w = 0; w < 4; ++w)
-                    y[n] += weight[w] * *reinterpret_cast<const f32x4 *>(xch + (w * 16 + r) * T::ROWF + part * NX + 4 * n);
-                y[n] *= inv;
-            }
-            const int first = part * NV + x * NX;
+            y *= inv;
+            // (NX neighbouring elements of part x belong to one lane's NV)
+            const int first = part * EPT / NX * NV + x * NX + part * EPT % NX;
             if (u.n_ranges > 1) {
                 const size_t at = (size_t)u.slot * T::BM + 16 * m + r;
                 if (sum > 0.f)
-#pragma unroll
-                    for (int n = 0; n < NX / 4; ++n)
-                        *reinterpret_cast<f32x4 *>(p.parts[0].o + at * D + first + 4 * n) = y[n];
+                    *reinterpret_cast<elements *>(p.parts[0].o + at * D + first) = y;
                 if (part == 0 && x == 0)
                     p.parts[0].lse[at] = lse;
             } else {
                 const int i = p.token_of(row);
                 const size_t at = (size_t)(u.row0 + i) * p.H_q + u.h * p.G + row - i * p.G;
-                uint32_t *dst = reinterpret_cast<uint32_t *>(static_cast<typename E::t *>(p.o) + at * D + first);
-#pragma unroll
-                for (int n = 0; n < NX / 4; ++n)
-                    *reinterpret_cast<u32x2 *>(dst + 2 * n) = u32x2{E::pack(y[n][0], y[n][1]), E::pack(y[n][2], y[n][3])};
+                typedef typename E::t out __attribute__((ext_vector_type(EPT)));
+                *reinterpret_cast<out *>(static_cast<typename E::t *>(p.o) + at * D + first) = __builtin_convertvector(y, out);
                 if (part == 0 && x == 0)
                     p.lse[at] = lse;
             }
