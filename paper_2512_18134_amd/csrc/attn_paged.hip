@@ -32,16 +32,21 @@ constexpr long long kWholeBytes = 1 << 18;
 constexpr int kWaves = 8;
 constexpr int kSlots = 2 * kTarget + 64;
 
+// Sequences up to which every workgroup works the cut out for itself, 64 of them at a time; of more, a launch of its own does,
+// which takes some 3 us: 128 sequences of up to 2000 keys 102.8 us each for itself, 107.4 that way; 256 of up to 200 32.2 and
+// 28.5; 1024 213 and 103; 4096 2245 and 379.
+constexpr int kOwnCut = 128;
+
 // rows of a sequence up to which the row kernel takes it
 constexpr int rows_kernel_most(int D) { return D == 256 ? 64 : 128; }
 // 16-row tiles of its workgroup: as few as hold the rows
 inline int row_tiles(int D, long long rows) { return rows <= 16 ? 1 : rows <= 32 || D == 256 ? 2 : 4; }
 
 struct Workspace {
-    long long part_o[2], part_lse[2], merge, bytes;   // offsets in bytes
+    long long part_o[2], part_lse[2], merge, cut[2], bytes;   // offsets in bytes
 };
 
-inline Workspace workspace_of(int T, int G, int D)
+inline Workspace workspace_of(int T, int B, int G, int D)
 {
     Workspace w;
     long long at = 0;
@@ -54,7 +59,12 @@ inline Workspace workspace_of(int T, int G, int D)
         at += slots * rows * 4;
     }
     w.merge = at;
-    w.bytes = at + (long long)T * (long long)sizeof(MergeNote);
+    at += (long long)T * (long long)sizeof(MergeNote);
+    for (int kernel = 0; kernel < 2; ++kernel) {
+        w.cut[kernel] = at;
+        at += B > kOwnCut ? (B + 1LL) * (long long)sizeof(int2) : 0;
+    }
+    w.bytes = at;
     return w;
 }
 
@@ -65,6 +75,16 @@ namespace {
 using attn::PagedParams;
 
 bool misaligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
+
+// The cut of a batch of many sequences, before the kernel that takes its units.
+template <int BM>
+int launch_cut(PagedParams &p, hipStream_t st)
+{
+    p.cut = p.parts[p.kernel].cut;
+    if (p.cut)
+        hipLaunchKernelGGL((attn::attn_paged_plan_kernel<BM>), dim3(1), dim3(1024), 0, st, p);
+    return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH;
+}
 
 // Workgroups that a kernel of tiles of BM rows may have units for: a sequence's tiles are at most one more than its rows
 // fill; ranges are one for every tile and head, and the target's (twice that where rows are taken to see half).
@@ -90,6 +110,8 @@ int launch_rows(PagedParams p, int upto, hipStream_t st)
     if (grid > 0x7fffffffLL)
         return ATTN_ERR_SHAPE;
     p.most_units = (int)grid;
+    if (const int rc = launch_cut<16 * MT>(p, st))
+        return rc;
     constexpr int lds = attn::PagedRowsTiling<D, MT, NW>::LDS_BYTES;
     if (!attn::allow_lds(reinterpret_cast<const void *>(attn::attn_paged_rows_kernel<D, MT, E, E4M3, NW>), lds))
         return ATTN_ERR_LAUNCH;
@@ -134,6 +156,8 @@ int launch_tiles(PagedParams p, int above, hipStream_t st)
     p.most_units = (int)units;
     if (!attn::allow_lds(kern, lds))
         return ATTN_ERR_LAUNCH;
+    if (const int rc = launch_cut<E4M3 ? attn::PagedTilesTiling<D>::BM : attn::PagedAsmTiling<D>::BM>(p, st))
+        return rc;
     if constexpr (E4M3)
         hipLaunchKernelGGL((attn::attn_paged_tiles_kernel<D, E>), dim3((unsigned)grid), dim3(threads), lds, st, p);
     else
@@ -213,7 +237,7 @@ int paged_fwd(const void *q, const long long *strides, void *o, float *lse, cons
         return ATTN_ERR_ALIGN;
     if (!(scale > 0.f) || !(scale < INFINITY))
         return ATTN_ERR_SCALE;
-    const attn::Workspace w = attn::workspace_of(T, H_q / H_kv, D);
+    const attn::Workspace w = attn::workspace_of(T, B, H_q / H_kv, D);
     if (workspace_bytes < w.bytes)
         return ATTN_ERR_WORKSPACE;
     PagedParams p;
@@ -235,6 +259,7 @@ int paged_fwd(const void *q, const long long *strides, void *o, float *lse, cons
     for (int kernel = 0; kernel < 2; ++kernel) {
         p.parts[kernel].o = reinterpret_cast<float *>(ws + w.part_o[kernel]);
         p.parts[kernel].lse = reinterpret_cast<float *>(ws + w.part_lse[kernel]);
+        p.parts[kernel].cut = B > attn::kOwnCut ? reinterpret_cast<int2 *>(ws + w.cut[kernel]) : nullptr;
         p.parts[kernel].slots = w.part_o[kernel] == w.part_lse[kernel] ? 0 : attn::kSlots;
     }
     p.merge = reinterpret_cast<attn::MergeNote *>(ws + w.merge);
@@ -254,7 +279,7 @@ extern "C" long long attn_paged_fwd_workspace_bytes(int T, int B, int H_q, int H
     if (T < 1 || B < 1 || H_q < 1 || H_kv < 1 || H_q % H_kv || (D != 64 && D != 128 && D != 256) ||
         (long long)T * H_q > 0x3fffffffLL)
         return -1;
-    return attn::workspace_of(T, H_q / H_kv, D).bytes;
+    return attn::workspace_of(T, B, H_q / H_kv, D).bytes;
 }
 
 extern "C" int attn_paged_fwd(const void *q, const long long *strides, void *o, float *lse, const void *k_pages,

@@ -1,7 +1,8 @@
 // attn_paged_plan.h -- how a call over the paged cache is cut into units of work, and how partial results are merged.
 //
 // The host knows the number of rows and sequences, not the lengths, so the workgroups work the cut out for themselves, all of
-// them alike, from start and kv_len (a load, a sum over the wave, one more load for every 64 sequences).  A unit
+// them alike, from start and kv_len (a load, a sum over the wave, one more load for every 64 sequences); for a batch of
+// many sequences one workgroup does it before them (attn_paged_plan_kernel) and they look theirs up.  A unit
 // is (sequence, key head, tile of BM rows, range of keys).  A row is a query head of a token: the G query heads that
 // share a key head lie side by side (row = token * G + head in group), so that a key is fetched once for all of them.
 //
@@ -43,8 +44,12 @@ struct PagedParams {
         float *o;                       // [slots][BM][D]
         float *lse;                     // [slots][BM]
         int slots, BM;
+        int2 *cut;                      // see cut
     } parts[2];
     int4 *merge;                        // [T]: see MergeNote
+    // [B + 1] or NULL: the cut, worked out once for a batch of many sequences.  [0] = (units, Plan::per_block), [1 + b] = units
+    // and slots of the sequences before b
+    int2 *cut;
 
     // token of a row of the sequence, row >= 0: row / G = row * ceil(2^(31 + s) / G) / 2^(31 + s), s = ceil(log2 G), exact
     // below 2^31
@@ -197,25 +202,82 @@ __device__ __forceinline__ int unit_of_pass(int slots, int k)
     return k * slots + (k & 1 ? (slots / kNumXcd - 1 - m) * kNumXcd + x : wg);
 }
 
-// Every wave of a workgroup calls this.  s: plan_sequence of this lane, for find_unit.
-template <int BM>
-__device__ __forceinline__ Plan plan_call(const PagedParams &p, PlanSeq &s)
+// Who works a cut out together: a wave, or (GroupScope) a workgroup of sixteen.
+struct WaveScope {
+    static constexpr int kLanes = 64;
+    bool one;                           // a batch of one sequence: lane 0 has it
+    __device__ __forceinline__ int lane() const { return threadIdx.x & 63; }
+    template <typename T>
+    __device__ __forceinline__ T sum(T x) const
+    {
+        return one ? wave_first(x) : wave_sum(x);
+    }
+    __device__ __forceinline__ int most(int x) const { return one ? wave_first(x) : wave_max(x); }
+    // x of the lanes before this one, and of all
+    __device__ __forceinline__ int before(int x, int &all) const
+    {
+        const int upto = wave_prefix(x);
+        all = __builtin_amdgcn_readlane(upto, 63);
+        return upto - x;
+    }
+};
+struct GroupScope {
+    static constexpr int kLanes = 1024;
+    int *lds;                           // [16]
+    __device__ __forceinline__ int lane() const { return threadIdx.x; }
+    template <typename T, typename F>
+    __device__ __forceinline__ T join(T of_wave, F f) const
+    {
+        __syncthreads();                // what lay there has been read
+        if ((threadIdx.x & 63) == 0)
+            lds[threadIdx.x >> 6] = __builtin_bit_cast(int, of_wave);
+        __syncthreads();
+        T all = __builtin_bit_cast(T, lds[0]);
+        for (int w = 1; w < 16; ++w)
+            all = f(w, all, __builtin_bit_cast(T, lds[w]));
+        return all;
+    }
+    template <typename T>
+    __device__ __forceinline__ T sum(T x) const
+    {
+        return join(wave_sum(x), [](int, T a, T b) { return a + b; });
+    }
+    __device__ __forceinline__ int most(int x) const
+    {
+        return join(wave_max(x), [](int, int a, int b) { return max(a, b); });
+    }
+    __device__ __forceinline__ int before(int x, int &all) const
+    {
+        const int upto = wave_prefix(x), wave = threadIdx.x >> 6;
+        int first = 0;                  // of this wave
+        all = join(__builtin_amdgcn_readlane(upto, 63), [&](int w, int a, int b) {
+            first = w == wave ? a : first;
+            return a + b;
+        });
+        return first + upto - x;
+    }
+};
+
+// s: plan_sequence of this lane, for find_unit.
+template <int BM, typename Scope>
+__device__ __forceinline__ Plan plan_cut(const PagedParams &p, const Scope &scope, PlanSeq &s)
 {
-    const int lane = threadIdx.x & 63, B = p.c.B;
+    constexpr int N = Scope::kLanes;
+    const int lane = scope.lane(), B = p.c.B;
     Plan plan;
-    // f(s) for every 64 sequences; up to 64 of them stay in their registers from one pass to the next
+    // f(s) for every N sequences; up to N of them stay in their registers from one pass to the next
     s = plan_sequence<BM>(p, lane);
     auto pass = [&](auto f) {
         f();
-        if (B > 64) {
-            for (int b = 64; b < B; b += 64) {
+        if (B > N) {
+            for (int b = N; b < B; b += N) {
                 s = plan_sequence<BM>(p, b + lane);
                 f();
             }
             s = plan_sequence<BM>(p, lane);
         }
     };
-    auto sum = [&](auto x) { return B == 1 ? wave_first(x) : wave_sum(x); };
+    auto sum = [&](auto x) { return scope.sum(x); };
     // work of the call, in (row tile, block, key head)
     float work = 0.f;
     int tiles = 0, most = 0;
@@ -223,7 +285,7 @@ __device__ __forceinline__ Plan plan_call(const PagedParams &p, PlanSeq &s)
         const float seen = (float)s.blocks - (p.halve ? (float)min(s.n, s.kv) * (0.5f / kPlanBlock) : 0.f);
         work += sum((float)s.tiles * fmaxf(seen, 1.f));
         tiles += sum(s.tiles);
-        most = max(most, B == 1 ? wave_first(s.blocks) : wave_max(s.blocks));
+        most = max(most, scope.most(s.blocks));
     });
     work *= (float)p.c.H_kv;
     int total, held;                            // units of a key head, and slots of those that share their rows with others
@@ -267,6 +329,44 @@ __device__ __forceinline__ Plan plan_call(const PagedParams &p, PlanSeq &s)
     return plan;
 }
 
+// Every wave of a workgroup calls this.
+template <int BM>
+__device__ __forceinline__ Plan plan_call(const PagedParams &p, PlanSeq &s)
+{
+    if (p.cut) {
+        const int2 known = p.cut[0];
+        return Plan{__builtin_amdgcn_readfirstlane(known.x), __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(known.y))};
+    }
+    return plan_cut<BM>(p, WaveScope{p.c.B == 1}, s);
+}
+
+// The cut of a batch of many sequences, left in p.cut.
+template <int BM, typename Scope>
+__device__ __forceinline__ void leave_cut(const PagedParams &p, const Scope &scope)
+{
+    PlanSeq s;
+    const Plan plan = plan_cut<BM>(p, scope, s);
+    if (scope.lane() == 0)
+        p.cut[0] = int2{plan.total, __builtin_bit_cast(int, plan.per_block)};
+    int units = 0, slots = 0;
+    for (int b = scope.lane(); b - scope.lane() < p.c.B; b += Scope::kLanes) {
+        s = plan_sequence<BM>(p, b);
+        const int nr = plan.ranges(s), mine = s.tiles * nr * p.c.H_kv;
+        int all, all_slots;
+        const int2 before = {units + scope.before(mine, all), slots + scope.before(nr > 1 ? mine : 0, all_slots)};
+        if (b < p.c.B)
+            p.cut[1 + b] = before;
+        units += all, slots += all_slots;
+    }
+}
+
+template <int BM>
+__global__ __launch_bounds__(1024) void attn_paged_plan_kernel(const PagedParams p)
+{
+    __shared__ int lds[16];
+    leave_cut<BM>(p, GroupScope{lds});
+}
+
 // Unit `wg` of the call (every wave of a workgroup calls this); false: there is none.  s: plan_sequence of this lane.
 template <int BM>
 __device__ __forceinline__ bool find_unit(const PagedParams &p, const Plan &plan, PlanSeq s, int wg, Unit &u)
@@ -274,35 +374,62 @@ __device__ __forceinline__ bool find_unit(const PagedParams &p, const Plan &plan
     const int lane = threadIdx.x & 63, B = p.c.B;
     if (wg >= plan.total)
         return false;
-    int units0 = 0, slots0 = 0;
-    for (int b = 0;; b += 64) {
-        const int nr = plan.ranges(s);
-        const int mine = s.tiles * nr * p.c.H_kv, kept = nr > 1 ? mine : 0;
-        const int after = units0 + (B == 1 ? mine : wave_prefix(mine)), after_slots = slots0 + (B == 1 ? kept : wave_prefix(kept));
-        const unsigned long long behind = __ballot(after > wg);
-        if (behind) {
-            const int l = __ffsll(behind) - 1;
-            auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
-            u.b = b + l;
-            u.n = of(s.n), u.kv = of(s.kv), u.row0 = of(s.start);
-            u.n_tiles = of(s.tiles), u.n_ranges = of(nr);
-            const int w = wg - of(after - mine);
-            if (w < 0 || w >= of(mine))        // starts that decrease can count more units than an int holds
-                return false;
-            u.slot0 = of(after_slots - kept);
-            const int layer = u.n_tiles * p.c.H_kv;
-            u.range = u.n_ranges == 1 ? 0 : quotient(w, layer);
-            place_in_layer(w - u.range * layer, p.c.H_kv, u.n_tiles, u.h, u.tile);
-            u.slot = u.slot0 + (u.range * p.c.H_kv + u.h) * u.n_tiles + u.tile;
-            const int blocks = of(s.blocks);
-            u.len = (u.n_ranges == 1 ? blocks : quotient(blocks + u.n_ranges - 1, u.n_ranges)) * kPlanBlock;
-            break;
-        }
-        if (b + 64 >= B)
+    // the unit is number w of sequence b, which x describes
+    auto take = [&](int b, const PlanSeq &x, int nr, int w, int slot0) {
+        if (w < 0 || w >= x.tiles * nr * p.c.H_kv)     // starts that decrease can count more units than an int holds
             return false;
-        units0 = __builtin_amdgcn_readlane(after, 63);
-        slots0 = __builtin_amdgcn_readlane(after_slots, 63);
-        s = plan_sequence<BM>(p, b + 64 + lane);
+        u.b = b;
+        u.n = x.n, u.kv = x.kv, u.row0 = x.start;
+        u.n_tiles = x.tiles, u.n_ranges = nr;
+        u.slot0 = slot0;
+        const int layer = u.n_tiles * p.c.H_kv;
+        u.range = u.n_ranges == 1 ? 0 : quotient(w, layer);
+        place_in_layer(w - u.range * layer, p.c.H_kv, u.n_tiles, u.h, u.tile);
+        u.slot = u.slot0 + (u.range * p.c.H_kv + u.h) * u.n_tiles + u.tile;
+        u.len = (u.n_ranges == 1 ? x.blocks : quotient(x.blocks + u.n_ranges - 1, u.n_ranges)) * kPlanBlock;
+        return true;
+    };
+    if (p.cut) {
+        // the last sequence with no more than wg units before it: 64 of them are compared at a time
+        int lo = 0, n = B;
+        while (n > 64) {
+            const int step = (n + 63) / 64;
+            const int below = __popcll(__ballot(lane * step < n && p.cut[1 + lo + min(lane * step, n - 1)].x <= wg));
+            if (below == 0)
+                return false;
+            const int next = (below - 1) * step;
+            lo += next;
+            n = min(step, n - next);
+        }
+        const int below = __popcll(__ballot(lane < n && p.cut[1 + lo + min(lane, n - 1)].x <= wg));
+        if (below == 0)
+            return false;
+        const int b = __builtin_amdgcn_readfirstlane(lo + below - 1);
+        const int2 before = p.cut[1 + b];
+        const PlanSeq x = plan_sequence<BM>(p, b);
+        if (!take(b, x, plan.ranges(x), wg - before.x, before.y))
+            return false;
+    } else {
+        int units0 = 0, slots0 = 0;
+        for (int b = 0;; b += 64) {
+            const int nr = plan.ranges(s);
+            const int mine = s.tiles * nr * p.c.H_kv, kept = nr > 1 ? mine : 0;
+            const int after = units0 + (B == 1 ? mine : wave_prefix(mine)), after_slots = slots0 + (B == 1 ? kept : wave_prefix(kept));
+            const unsigned long long behind = __ballot(after > wg);
+            if (behind) {
+                const int l = __ffsll(behind) - 1;
+                auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+                const PlanSeq x = {of(s.tiles), of(s.blocks), of(s.n), of(s.kv), of(s.start)};
+                if (!take(b + l, x, of(nr), wg - of(after - mine), of(after_slots - kept)))
+                    return false;
+                break;
+            }
+            if (b + 64 >= B)
+                return false;
+            units0 = __builtin_amdgcn_readlane(after, 63);
+            slots0 = __builtin_amdgcn_readlane(after_slots, 63);
+            s = plan_sequence<BM>(p, b + 64 + lane);
+        }
     }
     u.n_rows = u.n * p.G;
     u.key0 = min(u.range * u.len, u.kv);

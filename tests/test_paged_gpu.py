@@ -127,6 +127,21 @@ def test_the_hint_costs_speed_only(max_q):
     check_attention(c, o, lse, ref)
 
 
+@pytest.mark.parametrize("dt, e4m3", [("bf16", False), ("f16", True)])
+@pytest.mark.parametrize("most", [3, 50])
+def test_batches_of_many_sequences(most, dt, e4m3):
+    """So many that the cut is worked out before the kernels that take its units; of few rows, or of few and of many."""
+    from paper_2512_18134_amd import binding as M
+    gen = torch.Generator().manual_seed(17)
+    news = torch.randint(0, 4, (150,), generator=gen).tolist()
+    kvs = [n + int(torch.randint(0, 60, (1,), generator=gen)) for n in news]
+    news[70], kvs[70], kvs[71], kvs[149] = most, 700, 1500, 300
+    c = Cache(news, kvs, 2, 64, 16, dt, e4m3, 18, front=1, behind=2)
+    for max_q in (most, None):
+        _, o, lse, ref = attend(M, c, 3, True, max_q)
+        check_attention(c, o, lse, ref)
+
+
 @pytest.mark.parametrize("n", [1, 70])
 def test_rows_that_see_nothing(n):
     from paper_2512_18134_amd import binding as M

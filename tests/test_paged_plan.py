@@ -32,7 +32,7 @@ def ptr(a):
     return a.ctypes.data_as(ctypes.c_void_p)
 
 
-def plan(lib, start, kv_len, T, H_kv, G, BM, width, page_log2=4, above=0, upto=ALL, target=64, min_range=2, n_slots=None, causal=1, rounds=1):
+def plan(lib, start, kv_len, T, H_kv, G, BM, width, page_log2=4, above=0, upto=ALL, target=64, min_range=2, n_slots=None, causal=1, rounds=1, before=None):
     B = len(kv_len)
     n_slots = 4 * target + 64 if n_slots is None else n_slots
     n_wg = (T * G // BM + min(B, T)) * H_kv + target * rounds * (2 if causal else 1) + 64    # the launch's own bound
@@ -40,8 +40,12 @@ def plan(lib, start, kv_len, T, H_kv, G, BM, width, page_log2=4, above=0, upto=A
     table = np.zeros((B, width), np.int32)
     units = np.zeros((n_wg, 14), np.int32)
     notes = np.full((T + 2, 4), -77, np.int32)                    # a guard row on either side
+    before = B > 128 if before is None else before               # the cut is left in a table first, as for so many sequences
+    cut = np.full((B + 3, 2), -77, np.int32)
     n = lib.plan_batch(ptr(table), ptr(start), ptr(kv_len), T, B, H_kv, 1, page_log2, width, G, BM, above, upto, target,
-                       min_range, n_slots, causal, rounds, n_wg, ptr(units), ctypes.c_void_p(notes.ctypes.data + 16))
+                       min_range, n_slots, causal, rounds, n_wg, ptr(units), ctypes.c_void_p(notes.ctypes.data + 16),
+                       ctypes.c_void_p(cut.ctypes.data + 8) if before else None)
+    assert (cut[0] == -77).all() and (cut[-1] == -77).all()
     assert n >= 0
     assert (notes[0] == -77).all() and (notes[-1] == -77).all()
     return [dict(zip(FIELDS, map(int, u))) for u in units[:n]], notes[1:-1], n_wg, n_slots
@@ -198,3 +202,30 @@ def test_divisions_without_a_division(lib):
         b = rng.choice([1, 2, 3, 7, 8, rng.randrange(1, 5000), rng.randrange(1, 2 ** 22)])
         a = rng.choice([0, b - 1, b, b * rng.randrange(1, 50), rng.randrange(2 ** 22), 2 ** 22 - 1, 2 ** 22, 2 ** 31 - 1])
         assert lib.over(a, b) == a // b, (a, b)
+
+
+@pytest.mark.parametrize("B", [1, 2, 64, 65, 130])
+@pytest.mark.parametrize("rounds", [0, 1, 4])
+def test_the_table_of_units_says_what_the_workgroups_find(lib, B, rounds):
+    """The cut worked out by every workgroup, and once before them: the same units, whatever the lengths (0 among them)."""
+    rng = random.Random(B)
+    news = [rng.choice([0, 1, 1, 3]) for _ in range(B)]
+    news[0] = 2
+    kvs = [n + rng.choice([0, 0, 5, 70, 900]) for n in news]
+    start = np.concatenate([[0], np.cumsum(news)])
+    args = (lib, start, kvs, int(start[-1]), 2, 3, 16, 64)
+    one, other = (plan(*args, target=16, rounds=rounds, before=b) for b in (False, True))
+    assert one[0] == other[0] and (one[1] == other[1]).all()
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_a_table_of_arrays_that_make_no_sense_stays_in_bounds(lib, seed):
+    rng = random.Random(100 + seed)
+    B, T, width = rng.choice([3, 129, 200]), 50, 4
+    wild = lambda: rng.choice([-2 ** 31, -1, 0, 7, 30, 50, 51, 2 ** 31 - 1])
+    units, _, n_wg, n_slots = plan(lib, [wild() for _ in range(B + 1)], [wild() for _ in range(B)], T, 2, 2, 16, width, before=True)
+    assert len(units) <= n_wg
+    for u in units:
+        assert 0 <= u["b"] < B and 0 <= u["h"] < 2 and 0 <= u["row0"] <= T and u["row0"] + u["n"] <= T
+        assert 0 <= u["key0"] <= u["key1"] <= width * 16 and 0 <= u["tile"] < u["n_tiles"]
+        assert u["n_ranges"] == 1 or 0 <= u["slot"] < n_slots

@@ -16,6 +16,9 @@
 #define __forceinline__ inline
 #define __launch_bounds__(...)
 
+struct int2 {
+    int x, y;
+};
 struct int4 {
     int x, y, z, w;
 };

@@ -18,6 +18,12 @@ void plan(int)
 }
 
 template <int BM>
+void cut(int)
+{
+    attn::leave_cut<BM>(p, attn::WaveScope{p.c.B == 1});
+}
+
+template <int BM>
 void note(int)
 {
     attn::leave_note<BM, 64>(p, unit);
@@ -26,7 +32,7 @@ void note(int)
 
 extern "C" int plan_batch(const int *table, const int *start, const int *kv_len, int T, int B, int H_kv, int n_pages,
                           int page_log2, int width, int G, int BM, int rows_above, int rows_upto, int target, int min_range,
-                          int n_slots, int causal, int rounds, int n_wg, int *units, int4 *notes)
+                          int n_slots, int causal, int rounds, int n_wg, int *units, int4 *notes, int2 *table_of_units)
 {
     p = {};
     p.c.page_table = table, p.c.start = start, p.c.kv_len = kv_len;
@@ -40,6 +46,11 @@ extern "C" int plan_batch(const int *table, const int *start, const int *kv_len,
         ++log_g;
     p.g_mul = G == 1 ? 0 : (uint32_t)(((1ULL << (31 + log_g)) + G - 1) / G);
     p.g_shift = G == 1 ? 0 : log_g - 1;
+    if (table_of_units) {
+        p.cut = table_of_units;
+        if (!wave_host::run(BM == 16 ? cut<16> : BM == 32 ? cut<32> : BM == 64 ? cut<64> : BM == 128 ? cut<128> : cut<256>))
+            return -1;
+    }
     int n = 0;
     for (wg = 0; wg < n_wg; ++wg) {
         if (!wave_host::run(BM == 16 ? plan<16> : BM == 32 ? plan<32> : BM == 64 ? plan<64> : BM == 128 ? plan<128> : plan<256>))
