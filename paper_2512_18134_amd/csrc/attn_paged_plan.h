@@ -22,6 +22,9 @@ constexpr int kPlanBlock = 64;          // keys of a block
 
 struct PagedParams {
     CacheParams c;
+    // [B + 1] or NULL: the cut, worked out once for a batch of many sequences.  [0] = (units, Plan::per_block), [1 + b] = units
+    // and slots of the sequences before b.  (Asked for first: here it is in the same line as what the plan begins with.)
+    int2 *cut;
     const void *q;
     void *o;
     float *lse;
@@ -47,9 +50,6 @@ struct PagedParams {
         int2 *cut;                      // see cut
     } parts[2];
     int4 *merge;                        // [T]: see MergeNote
-    // [B + 1] or NULL: the cut, worked out once for a batch of many sequences.  [0] = (units, Plan::per_block), [1 + b] = units
-    // and slots of the sequences before b
-    int2 *cut;
 
     // token of a row of the sequence, row >= 0: row / G = row * ceil(2^(31 + s) / G) / 2^(31 + s), s = ceil(log2 G), exact
     // below 2^31
@@ -333,7 +333,7 @@ __device__ __forceinline__ Plan plan_cut(const PagedParams &p, const Scope &scop
 template <int BM>
 __device__ __forceinline__ Plan plan_call(const PagedParams &p, PlanSeq &s)
 {
-    if (p.cut) {
+    if (__builtin_expect(p.cut != nullptr, 0)) {
         const int2 known = p.cut[0];
         return Plan{__builtin_amdgcn_readfirstlane(known.x), __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(known.y))};
     }
@@ -374,22 +374,11 @@ __device__ __forceinline__ bool find_unit(const PagedParams &p, const Plan &plan
     const int lane = threadIdx.x & 63, B = p.c.B;
     if (wg >= plan.total)
         return false;
-    // the unit is number w of sequence b, which x describes
-    auto take = [&](int b, const PlanSeq &x, int nr, int w, int slot0) {
-        if (w < 0 || w >= x.tiles * nr * p.c.H_kv)     // starts that decrease can count more units than an int holds
-            return false;
-        u.b = b;
-        u.n = x.n, u.kv = x.kv, u.row0 = x.start;
-        u.n_tiles = x.tiles, u.n_ranges = nr;
-        u.slot0 = slot0;
-        const int layer = u.n_tiles * p.c.H_kv;
-        u.range = u.n_ranges == 1 ? 0 : quotient(w, layer);
-        place_in_layer(w - u.range * layer, p.c.H_kv, u.n_tiles, u.h, u.tile);
-        u.slot = u.slot0 + (u.range * p.c.H_kv + u.h) * u.n_tiles + u.tile;
-        u.len = (u.n_ranges == 1 ? x.blocks : quotient(x.blocks + u.n_ranges - 1, u.n_ranges)) * kPlanBlock;
-        return true;
-    };
-    if (p.cut) {
+    // the unit is number w of sequence u.b, which x describes
+    PlanSeq x;
+    int nr, w;
+    auto scalar = [](int &x) { x = __builtin_amdgcn_readfirstlane(x); };
+    if (__builtin_expect(p.cut != nullptr, 0)) {
         // the last sequence with no more than wg units before it: 64 of them are compared at a time
         int lo = 0, n = B;
         while (n > 64) {
@@ -404,24 +393,25 @@ __device__ __forceinline__ bool find_unit(const PagedParams &p, const Plan &plan
         const int below = __popcll(__ballot(lane < n && p.cut[1 + lo + min(lane, n - 1)].x <= wg));
         if (below == 0)
             return false;
-        const int b = __builtin_amdgcn_readfirstlane(lo + below - 1);
-        const int2 before = p.cut[1 + b];
-        const PlanSeq x = plan_sequence<BM>(p, b);
-        if (!take(b, x, plan.ranges(x), wg - before.x, before.y))
-            return false;
+        u.b = __builtin_amdgcn_readfirstlane(lo + below - 1);
+        const int2 before = p.cut[1 + u.b];
+        x = plan_sequence<BM>(p, u.b);
+        scalar(x.tiles), scalar(x.blocks), scalar(x.n), scalar(x.kv), scalar(x.start);
+        nr = __builtin_amdgcn_readfirstlane(plan.ranges(x));
+        w = __builtin_amdgcn_readfirstlane(wg - before.x), u.slot0 = __builtin_amdgcn_readfirstlane(before.y);
     } else {
         int units0 = 0, slots0 = 0;
         for (int b = 0;; b += 64) {
-            const int nr = plan.ranges(s);
-            const int mine = s.tiles * nr * p.c.H_kv, kept = nr > 1 ? mine : 0;
+            const int ranges = plan.ranges(s);
+            const int mine = s.tiles * ranges * p.c.H_kv, kept = ranges > 1 ? mine : 0;
             const int after = units0 + (B == 1 ? mine : wave_prefix(mine)), after_slots = slots0 + (B == 1 ? kept : wave_prefix(kept));
             const unsigned long long behind = __ballot(after > wg);
             if (behind) {
                 const int l = __ffsll(behind) - 1;
-                auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
-                const PlanSeq x = {of(s.tiles), of(s.blocks), of(s.n), of(s.kv), of(s.start)};
-                if (!take(b + l, x, of(nr), wg - of(after - mine), of(after_slots - kept)))
-                    return false;
+                auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+                u.b = b + l;
+                x = PlanSeq{of(s.tiles), of(s.blocks), of(s.n), of(s.kv), of(s.start)};
+                nr = of(ranges), w = wg - of(after - mine), u.slot0 = of(after_slots - kept);
                 break;
             }
             if (b + 64 >= B)
@@ -431,11 +421,19 @@ __device__ __forceinline__ bool find_unit(const PagedParams &p, const Plan &plan
             s = plan_sequence<BM>(p, b + 64 + lane);
         }
     }
+    if (w < 0 || w >= x.tiles * nr * p.c.H_kv)             // starts that decrease can count more units than an int holds
+        return false;
+    u.n = x.n, u.kv = x.kv, u.row0 = x.start;
+    u.n_tiles = x.tiles, u.n_ranges = nr;
+    const int layer = u.n_tiles * p.c.H_kv;
+    u.range = u.n_ranges == 1 ? 0 : quotient(w, layer);
+    place_in_layer(w - u.range * layer, p.c.H_kv, u.n_tiles, u.h, u.tile);
+    u.slot = u.slot0 + (u.range * p.c.H_kv + u.h) * u.n_tiles + u.tile;
+    u.len = (u.n_ranges == 1 ? x.blocks : quotient(x.blocks + u.n_ranges - 1, u.n_ranges)) * kPlanBlock;
     u.n_rows = u.n * p.G;
     u.key0 = min(u.range * u.len, u.kv);
     u.key1 = min(u.key0 + u.len, u.kv);
     // the same in all lanes: scalars from here on
-    auto scalar = [](int &x) { x = __builtin_amdgcn_readfirstlane(x); };
     scalar(u.row0), scalar(u.b), scalar(u.h), scalar(u.tile), scalar(u.range), scalar(u.key0), scalar(u.key1), scalar(u.slot0);
     scalar(u.slot), scalar(u.n), scalar(u.kv), scalar(u.n_rows), scalar(u.n_tiles), scalar(u.n_ranges);
     // starts that decrease can count rows twice: a slot behind the workspace's last is not written
