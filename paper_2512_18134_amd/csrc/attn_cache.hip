@@ -109,7 +109,7 @@ __global__ __launch_bounds__(256) void attn_cache_token_kernel(const RowsParams 
     constexpr int LPR = D / 8;                          // lanes of a row
     const int lane = threadIdx.x & 63;
     const long long wave = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int t = (int)(wave / p.slices), piece = (int)(wave % p.slices) * 64 + lane;
+    const int t = (int)quotient(wave, p.slices), piece = (int)(wave - (long long)t * p.slices) * 64 + lane;
     if (t >= p.c.T)
         return;
     const int b = p.c.sequence_of(t);
@@ -148,7 +148,8 @@ __global__ __launch_bounds__(256) void attn_cache_run_kernel(const RowsParams p)
     constexpr int LPR = D / 8, TPI = 64 / LPR, F = kRunTokens / TPI;   // lanes of a row, tokens of an access, accesses of a row
     const int lane = threadIdx.x & 63;
     const long long wave = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int t0 = (int)(wave / p.slices) * kRunTokens, slice = (int)(wave % p.slices);
+    const long long run = quotient(wave, p.slices);
+    const int t0 = (int)run * kRunTokens, slice = (int)(wave - run * p.slices);
     if (t0 >= p.c.T)
         return;
 

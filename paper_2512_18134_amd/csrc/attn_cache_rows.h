@@ -9,6 +9,18 @@
 
 namespace attn {
 
+// a / b for a >= 0, b > 0.  The compiler's division is a chain of some 30 instructions, and the plan of attn_paged_plan.h has a dozen of them
+// in a row; below 2^22 a reciprocal's quotient is off by one at most.
+__device__ __forceinline__ int quotient(int a, int b)
+{
+    if (a >= 1 << 22)
+        return a / b;
+    const int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b)), r = a - q * b;
+    return q + (r >= b) - (r < 0);
+}
+// The same of a count that may pass 32 bits (the compiler's 64-bit division is some 100 instructions).
+__device__ __forceinline__ long long quotient(long long a, int b) { return a < 1 << 22 ? quotient((int)a, b) : a / b; }
+
 struct CacheParams {
     const int *page_table, *start, *kv_len;
     int T, B, H_kv;

@@ -59,16 +59,6 @@ struct PagedParams {
     }
 };
 
-// a / b for a >= 0, b > 0.  The compiler's division is a chain of some 30 instructions, and the plan has a dozen of them in a row;
-// below 2^22 a reciprocal's quotient is off by one at most.
-__device__ __forceinline__ int quotient(int a, int b)
-{
-    if (a >= 1 << 22)
-        return a / b;
-    const int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b)), r = a - q * b;
-    return q + (r >= b) - (r < 0);
-}
-
 // What the merge kernel needs to know of a token: x = first slot of its sequence, y = row tiles of the sequence,
 // z = its ranges, w = first row of the token in its sequence * 2 + kernel.  Only sequences of several ranges have a
 // meaningful x and w.

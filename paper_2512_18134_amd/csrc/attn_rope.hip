@@ -7,7 +7,7 @@
 
 #include <type_traits>
 
-#include "attn_common.h"
+#include "attn_cache_rows.h"   // quotient
 #include "attn_fwd.h"
 #include "attn_rope.h"
 
@@ -44,13 +44,41 @@ __global__ __launch_bounds__(256) void attn_rope_kernel(const RopeParams p)
     typedef float f8 __attribute__((ext_vector_type(8)));
     const int lane = threadIdx.x & 63;
     const long long wave = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int head0 = (int)(wave % p.head_groups) * p.heads_per_wave;
-    const long long token = (wave / p.head_groups << (6 - p.lanes_log2)) + (lane >> p.lanes_log2);
+    const long long group = quotient(wave, p.head_groups);
+    const int head0 = (int)(wave - group * p.head_groups) * p.heads_per_wave;
+    // (lanes behind the last token go along with it and store nothing: a wave of eight lanes or fewer took 4 us longer)
+    const long long own = (group << (6 - p.lanes_log2)) + (lane >> p.lanes_log2), token = own < p.tokens ? own : p.tokens - 1;
+    const bool mine = own < p.tokens;
     const int c = lane & ((1 << p.lanes_log2) - 1);
-    if (token >= p.tokens)
+    if (group << (6 - p.lanes_log2) >= p.tokens)
         return;
     const int half = p.R >> 1;
     const bool turns = 8 * c < half;
+    const long long b = p.tokens == p.S ? 0 : quotient(token, p.S), s = token - b * p.S;
+    const int head_end = min(head0 + p.heads_per_wave, p.H_all);
+    const int first = INTERLEAVED ? 16 * c : 8 * c, second = INTERLEAVED ? 16 * c + 8 : half + 8 * c;
+    // U heads at a time, all their loads before their stores (which the compiler must take for aliases), the first ones' before
+    // the sines and cosines: a small call is a chain of latencies
+    constexpr int U = 4;
+    t8 lo[U], hi[U];
+    T *out[U];
+    auto load = [&](int head) {
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int at = min(head + j, head_end - 1);
+            const int w = at >= p.H_q, h = w ? at - p.H_q : at;
+            const T *x = static_cast<const T *>(p.x[w]) + b * p.sx[w][0] + h * p.sx[w][1] + s * p.sx[w][2];
+            out[j] = static_cast<T *>(p.y[w]) + b * p.sy[w][0] + h * p.sy[w][1] + s * p.sy[w][2];
+            if (turns) {
+                lo[j] = *reinterpret_cast<const t8 *>(x + first);
+                hi[j] = *reinterpret_cast<const t8 *>(x + second);
+            }
+            if (head + j < head_end && x != out[j] && mine)
+                for (int e = p.R + 8 * c; e < p.D; e += 8 << p.lanes_log2)
+                    *reinterpret_cast<t8 *>(out[j] + e) = *reinterpret_cast<const t8 *>(x + e);
+        }
+    };
+    load(head0);
     f8 cs, sn;
     if (turns) {
 #pragma unroll
@@ -67,32 +95,9 @@ __global__ __launch_bounds__(256) void attn_rope_kernel(const RopeParams p)
             sn[i] = p.sign * s1;
         }
     }
-    const long long b = token / p.S, s = token - b * p.S;
-    const int head_end = min(head0 + p.heads_per_wave, p.H_all);
-    const int first = INTERLEAVED ? 16 * c : 8 * c, second = INTERLEAVED ? 16 * c + 8 : half + 8 * c;
-    // U heads at a time, all their loads before their stores (which the compiler must take for aliases)
-    constexpr int U = 4;
-    for (int head = head0; head < head_end; head += U) {
-        t8 lo[U], hi[U];
-        T *out[U];
+    for (int head = head0;;) {
 #pragma unroll
-        for (int j = 0; j < U; ++j) {
-            const int at = min(head + j, head_end - 1);
-            const int w = at >= p.H_q, h = w ? at - p.H_q : at;
-            const T *x = static_cast<const T *>(p.x[w]) + b * p.sx[w][0] + h * p.sx[w][1] + s * p.sx[w][2];
-            out[j] = static_cast<T *>(p.y[w]) + b * p.sy[w][0] + h * p.sy[w][1] + s * p.sy[w][2];
-            if (turns) {
-                lo[j] = *reinterpret_cast<const t8 *>(x + first);
-                hi[j] = *reinterpret_cast<const t8 *>(x + second);
-            }
-            if (head + j < head_end && x != out[j])
-                for (int e = p.R + 8 * c; e < p.D; e += 8 << p.lanes_log2)
-                    *reinterpret_cast<t8 *>(out[j] + e) = *reinterpret_cast<const t8 *>(x + e);
-        }
-        if (!turns)
-            continue;
-#pragma unroll
-        for (int j = 0; j < U; ++j) {
+        for (int j = 0; j < U && turns; ++j) {
             const f8 u = __builtin_convertvector(lo[j], f8), v = __builtin_convertvector(hi[j], f8);
             f8 a, d;
 #pragma unroll
@@ -108,7 +113,7 @@ __global__ __launch_bounds__(256) void attn_rope_kernel(const RopeParams p)
                     d[i] = u[i] * sn[i] + v[i] * cs[i];
                 }
             }
-            if (head + j < head_end) {
+            if (head + j < head_end && mine) {
                 const t8 ya = __builtin_convertvector(a, t8), yd = __builtin_convertvector(d, t8);      // to nearest even
                 if (PAST) {
                     __builtin_nontemporal_store(ya, reinterpret_cast<t8 *>(out[j] + first));
@@ -119,6 +124,10 @@ __global__ __launch_bounds__(256) void attn_rope_kernel(const RopeParams p)
                 }
             }
         }
+        head += U;
+        if (head >= head_end)
+            break;
+        load(head);
     }
 }
 
