@@ -6,10 +6,12 @@
 // is (sequence, key head, tile of BM rows, range of keys).  A row is a query head of a token: the G query heads that
 // share a key head lie side by side (row = token * G + head in group), so that a key is fetched once for all of them.
 //
-// All ranges of a call have the same length L, in blocks of 64 keys, whatever the lengths of the sequences: L is what
-// lets about `target` units (what the chip holds at once) share all the keys that the call has to walk, so a long
-// sequence among short ones is walked by many workgroups.  A sequence of one range is finished by its unit;
+// No range of a call is longer than L blocks of 64 keys, and the ranges of a sequence are alike: L is what
+// lets about `target` units (what the chip holds at once), or a few times that, share all the keys that the call has to walk,
+// so a long sequence among short ones is walked by many workgroups.  A sequence of one range is finished by its unit;
 // the units of the others leave normalised fp32 rows and their log-sum-exp, which attn_paged_merge_kernel joins.
+// Working a cut out takes 0.5 us of a workgroup for one sequence, 1.2 for 64; the merge is a launch of 4 us, of which
+// most is its own latency: its partial rows are 2 to 30 MB.
 #pragma once
 #include <type_traits>
 

