@@ -3,7 +3,7 @@
 //
 // Bound by memory (58000 positions written in 16 bits at 6.5 TB/s); for the few rows of a decoding step (64 rows: 2.6 us) by the chain of dependent loads: start -> kv_len -> page table -> row.
 // Two kernels.  With few tokens a wave works on one (the chain is uniform and walked once) and on 64 pieces of 8 elements of
-// its heads' K and V rows.  With many, a wave takes eight neighbouring tokens and up to four of their (tensor, head) rows: in the
+// its heads' K and V rows.  With many, a wave takes eight neighbouring tokens and some of their (tensor, head) rows: in the
 // pool neighbouring positions of a head are contiguous, so that its accesses there are long, as are the rows'
 // in the tensors (eight tokens of all heads are 128-byte pieces of the pool, page_size apart, and a cache line of
 // units for every byte of them: 58000 positions of 8 heads, D = 128, read from e4m3 in 107 us that way, in 56 us this way, 6.3 TB/s).
@@ -12,6 +12,8 @@
 // a function of the numbers alone and not of how a division was carried out; against amplitude / 448 as the
 // unit it gives up less than one of the format's seventeen binades at the small end.
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include <math.h>
 
@@ -47,6 +49,22 @@ struct RowPiece {
     typedef T t8 __attribute__((ext_vector_type(8)));
     typedef uint32_t pool_t __attribute__((ext_vector_type(E4M3 ? 2 : 4)));     // in the pool
 
+    // The largest of LPR neighbouring lanes' x, in all of them: exchanges across a pair, a quad, eight and sixteen lanes are part
+    // of a vector instruction (through LDS: 58000 positions of 8 heads 89 us, so 86).
+    template <int LPR>
+    static __device__ __forceinline__ float most(float x)
+    {
+        auto across = [](float v, auto ctrl) {
+            return fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, 0xf, 0xf, true)));
+        };
+        x = across(x, std::integral_constant<int, 0xb1>{});              // quad_perm 1 0 3 2
+        x = across(x, std::integral_constant<int, 0x4e>{});              // quad_perm 2 3 0 1
+        x = across(x, std::integral_constant<int, 0x141>{});             // row_half_mirror
+        if (LPR > 8)
+            x = across(x, std::integral_constant<int, 0x140>{});         // row_mirror
+        return LPR > 16 ? fmaxf(x, __shfl_xor(x, 16, 64)) : x;
+    }
+
     // rows -> pool; e4m3: LPR lanes hold the row, its exponent comes back
     template <int LPR>
     static __device__ __forceinline__ pool_t stored(t8 x, int &exponent)
@@ -59,9 +77,7 @@ struct RowPiece {
 #pragma unroll
             for (int k = 0; k < 8; ++k)
                 amp = fmaxf(amp, fabsf(y[k]));
-#pragma unroll
-            for (int m = 1; m < LPR; m *= 2)
-                amp = fmaxf(amp, __shfl_xor(amp, m, 64));
+            amp = most<LPR>(amp);
             // amp = 1.f * 2^(bits >> 23 - 127), 448 = 1.75 * 2^8
             const int bits = __builtin_bit_cast(int, amp);
             exponent = min(max((bits >> 23) - 127 - 8 + ((bits & 0x7fffff) > 0x600000), -126), 120);
@@ -136,8 +152,11 @@ __global__ __launch_bounds__(256) void attn_cache_token_kernel(const RowsParams 
     }
 }
 
-// Many tokens: a wave has eight neighbouring ones and kRunRows of their (tensor, head) rows.
-constexpr int kRunTokens = 8, kRunRows = 4;
+// Many tokens: a wave has eight neighbouring ones and so many of their (tensor, head) rows that they are 8 KB, 128 bytes to a lane.
+// (e4m3, written and read: 131000 positions of 8 heads, D = 64, in fours 166 us, in eights 151; 33000 of one, D = 256, in fours
+// 31.5, in twos 25.)
+constexpr int kRunTokens = 8;
+constexpr int run_rows(int D) { return 512 / D; }
 
 template <typename T, int D, bool E4M3, bool WRITE>
 __global__ __launch_bounds__(256) void attn_cache_run_kernel(const RowsParams p)
@@ -145,6 +164,7 @@ __global__ __launch_bounds__(256) void attn_cache_run_kernel(const RowsParams p)
     typedef RowPiece<T, E4M3> P;
     typedef typename P::t8 t8;
     typedef typename P::pool_t pool_t;
+    constexpr int kRunRows = run_rows(D);
     constexpr int LPR = D / 8, TPI = 64 / LPR, F = kRunTokens / TPI;   // lanes of a row, tokens of an access, accesses of a row
     const int lane = threadIdx.x & 63;
     const long long wave = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -257,7 +277,7 @@ int launch(RowsParams &p, hipStream_t st)
 {
     // many tokens, if their runs fill the chip
     const long long runs = ((long long)p.c.T + attn::kRunTokens - 1) / attn::kRunTokens;
-    const int row_slices = (2 * p.c.H_kv + attn::kRunRows - 1) / attn::kRunRows;
+    const int row_slices = (2 * p.c.H_kv + attn::run_rows(D) - 1) / attn::run_rows(D);
     const bool many = runs * row_slices >= 1024;
     p.slices = many ? row_slices : (2 * p.c.H_kv * (D / 8) + 63) / 64;
     const long long blocks = ((many ? runs : (long long)p.c.T) * p.slices + 3) / 4;
