@@ -281,13 +281,18 @@ __device__ __forceinline__ Plan plan_cut(const PagedParams &p, const Scope &scop
     });
     work *= (float)p.c.H_kv;
     int total, held;                            // units of a key head, and slots of those that share their rows with others
+    int longest;                                // range
     auto count = [&](int L) {
         plan.per_block = (1.f - 0x1p-22f) / (float)L;
-        total = held = 0;
+        total = held = longest = 0;
         pass([&] {
             const int nr = plan.ranges(s);
             total += sum(s.tiles * nr);
             held += sum(nr > 1 ? s.tiles * nr : 0);
+            if (p.rounds > 1)
+                longest = max(longest, scope.most(s.tiles ? quotient(s.blocks + nr - 1, nr) : 0));
+            else
+                longest = L;
         });
         return (long long)held * p.c.H_kv <= p.slots;
     };
@@ -301,15 +306,21 @@ __device__ __forceinline__ Plan plan_cut(const PagedParams &p, const Scope &scop
     float soonest = ends(tiles, most);
     int L = 0;                                  // whole sequences
     for (int k = 1; k <= p.rounds; ++k) {
-        const int l = max(p.min_range, (int)fminf(ceilf(work / (float)(k * p.target)), 0x1p24f));
-        if (l >= most)
-            continue;
-        if (!count(l))
-            break;
-        const float e = ends(total, l) + (float)p.merging;
-        if (e < soonest)
-            L = l, soonest = e;
-        if (l == p.min_range)
+        int l = max(p.min_range, (int)fminf(ceilf(work / (float)(k * p.target)), 0x1p24f));
+        const bool last = l == p.min_range;
+        // ranges are whole blocks and a sequence's are alike, so the units may be a good deal more than k rounds: then so much
+        // longer ranges too
+        for (int again = 0; again < (p.rounds > 1 ? 2 : 1) && l < most; ++again) {
+            const bool fits = count(l);
+            const float e = ends(total, longest) + (float)p.merging;
+            if (fits && e < soonest)
+                L = l, soonest = e;
+            const float over = (float)total * (float)p.c.H_kv / (float)(k * p.target);
+            if (over <= 1.f)
+                break;
+            l = (int)fminf(ceilf((float)l * over), 0x1p24f);
+        }
+        if (last)
             break;
     }
     if (L == 0)
