@@ -282,6 +282,7 @@ __device__ __forceinline__ Plan plan_cut(const PagedParams &p, const Scope &scop
     work *= (float)p.c.H_kv;
     int total, held;                            // units of a key head, and slots of those that share their rows with others
     int longest;                                // range
+    constexpr bool kFit = BM > 64;              // the tile kernels, whose units are long
     auto count = [&](int L) {
         plan.per_block = (1.f - 0x1p-22f) / (float)L;
         total = held = longest = 0;
@@ -289,7 +290,7 @@ __device__ __forceinline__ Plan plan_cut(const PagedParams &p, const Scope &scop
             const int nr = plan.ranges(s);
             total += sum(s.tiles * nr);
             held += sum(nr > 1 ? s.tiles * nr : 0);
-            if (p.rounds > 1)
+            if (kFit)
                 longest = max(longest, scope.most(s.tiles ? quotient(s.blocks + nr - 1, nr) : 0));
             else
                 longest = L;
@@ -310,11 +311,13 @@ __device__ __forceinline__ Plan plan_cut(const PagedParams &p, const Scope &scop
         const bool last = l == p.min_range;
         // ranges are whole blocks and a sequence's are alike, so the units may be a good deal more than k rounds: then so much
         // longer ranges too
-        for (int again = 0; again < (p.rounds > 1 ? 2 : 1) && l < most; ++again) {
+        for (int again = 0; again < (kFit ? 2 : 1) && l < most; ++again) {
             const bool fits = count(l);
             const float e = ends(total, longest) + (float)p.merging;
             if (fits && e < soonest)
                 L = l, soonest = e;
+            if (!kFit)
+                break;
             const float over = (float)total * (float)p.c.H_kv / (float)(k * p.target);
             if (over <= 1.f)
                 break;
