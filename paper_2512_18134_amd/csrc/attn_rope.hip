@@ -1,6 +1,6 @@
 // attn_rope.hip -- rotary positions: kernel and entry points (include/attn_rope.h).
 //
-// Bound by memory: every element is read and written once.  8192 tokens of 40 heads, D = 128: 28.9 us, 5.8 TB/s; 64 tokens: 4.4
+// Bound by memory: every element is read and written once.  8192 tokens of 40 heads, D = 128: 30.1 us, 5.6 TB/s; 64 tokens: 4.4
 // us, one: 4.2, the latency of a launch that loads, turns and stores.  What has to be kept off that path is the sine and cosine of
 // a far position's angle, some hundred instructions with the reduction in 64 bits: a lane owns eight pairs of one
 // token, forms their sines and cosines once and walks over heads with them.
@@ -58,8 +58,9 @@ __global__ __launch_bounds__(256) void attn_rope_kernel(const RopeParams p)
     const long long b = p.tokens == p.S ? 0 : quotient(token, p.S), s = token - b * p.S;
     const int head_end = min(head0 + p.heads_per_wave, p.H_all);
     const int first = INTERLEAVED ? 16 * c : 8 * c, second = INTERLEAVED ? 16 * c + 8 : half + 8 * c;
-    // U heads at a time, all their loads before their stores (which the compiler must take for aliases), the first ones' before
-    // the sines and cosines: a small call is a chain of latencies
+    // U heads at a time, all their loads before their stores (which the compiler must take for aliases); the first ones' before
+    // the sines and cosines, since a small call is a chain of latencies (2 x 777 tokens of 20 heads 5.6 us, behind them 5.9),
+    // but not in a large one, where other waves fill the wait (4 x 4096 tokens there and back 101 us, before them 114)
     constexpr int U = 4;
     t8 lo[U], hi[U];
     T *out[U];
@@ -79,7 +80,8 @@ __global__ __launch_bounds__(256) void attn_rope_kernel(const RopeParams p)
                     *reinterpret_cast<t8 *>(out[j] + e) = *reinterpret_cast<const t8 *>(x + e);
         }
     };
-    load(head0);
+    if (!PAST)
+        load(head0);
     f8 cs, sn;
     if (turns) {
 #pragma unroll
@@ -97,6 +99,8 @@ __global__ __launch_bounds__(256) void attn_rope_kernel(const RopeParams p)
         }
     }
     for (int head = head0;;) {
+        if (PAST)
+            load(head);
 #pragma unroll
         for (int j = 0; j < U && turns; ++j) {
             const f8 u = __builtin_convertvector(lo[j], f8), v = __builtin_convertvector(hi[j], f8);
@@ -128,7 +132,8 @@ __global__ __launch_bounds__(256) void attn_rope_kernel(const RopeParams p)
         head += U;
         if (head >= head_end)
             break;
-        load(head);
+        if (!PAST)
+            load(head);
     }
 }
 
