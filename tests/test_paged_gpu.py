@@ -142,6 +142,19 @@ def test_batches_of_many_sequences(most, dt, e4m3):
         check_attention(c, o, lse, ref)
 
 
+@pytest.mark.parametrize("long", [700, 8000])
+def test_more_sequences_than_the_cut_takes_at_once(long):
+    """More than the 1024 lanes that work the cut out, one of them cut into ranges."""
+    from paper_2512_18134_amd import binding as M
+    gen = torch.Generator().manual_seed(19)
+    news = torch.randint(0, 2, (2100,), generator=gen).tolist()
+    kvs = [n + int(torch.randint(0, 30, (1,), generator=gen)) for n in news]
+    news[1500], kvs[1500] = 1, long
+    c = Cache(news, kvs, 1, 64, 16, "bf16", False, 20)
+    _, o, lse, ref = attend(M, c, 2, True, 1)
+    check_attention(c, o, lse, ref)
+
+
 @pytest.mark.parametrize("n", [1, 70])
 def test_rows_that_see_nothing(n):
     from paper_2512_18134_amd import binding as M
