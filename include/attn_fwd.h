@@ -34,7 +34,7 @@ typedef enum attn_status {
     ATTN_ERR_SHAPE = -2,         /* a size (B, H, S_q, S_kv ...) < 1, or beyond 2^31-1 rows, 2^40 elements or a limit the entry point states */
     ATTN_ERR_UNSUPPORTED_D = -3, /* D not in {64, 128, 256} */
     ATTN_ERR_ALIGN = -4,         /* q, k, v, o ... not 16-byte aligned, or lse (int32 arrays) not 4-byte, fp64 arrays not 8-byte aligned */
-    ATTN_ERR_SCALE = -5,         /* scale is NaN, infinite or negative */
+    ATTN_ERR_SCALE = -5,         /* scale is NaN, infinite or negative, or 0 where the entry point asks for more than 0 */
     ATTN_ERR_LAUNCH = -6,        /* the HIP runtime refused the launch (see hipGetLastError) */
     ATTN_ERR_UNSUPPORTED = -7,   /* the entry point does not implement this combination of arguments */
     ATTN_ERR_WORKSPACE = -8      /* the workspace is too small */

@@ -705,7 +705,7 @@ extern "C" const char *attn_strerror(int status)
     case ATTN_ERR_ALIGN:
         return "element tensors (q, k, v, o ...) must be 16-byte aligned, lse and int32 arrays 4-byte aligned, fp64 arrays 8-byte aligned";
     case ATTN_ERR_SCALE:
-        return "scale must be finite and >= 0";
+        return "scale must be finite and > 0 (attn_fwd and attn_bwd take 0 as well)";
     case ATTN_ERR_LAUNCH:
         return "the HIP runtime rejected the kernel launch";
     case ATTN_ERR_UNSUPPORTED:
