@@ -46,7 +46,7 @@ enum { ATTN_CACHE_16BIT = 0, ATTN_CACHE_E4M3 = 1 };
  *   page_table, start, kv_len            device pointers, int32                                     (read only)
  *   kind       ATTN_CACHE_16BIT or ATTN_CACHE_E4M3
  *   T, B, H_kv, n_pages, table_width     >= 1;  D 64, 128 or 256;  page_size a power of two, 16 .. 256;
- *              table_width * page_size at most 2^30
+ *              B and table_width * page_size at most 2^30
  *
  * ATTN_CACHE_E4M3: a row of amplitude a is stored in multiples of 2^e, the smallest e in [-126, 120] with
  * a <= 448 * 2^e, each element rounded to nearest even: a power of two keeps the division exact, so that the

@@ -301,7 +301,7 @@ int rows(const void *k, const void *v, const long long *strides, const void *k_p
     if (!k || !v || !strides || !k_pages || !v_pages || !page_table || !start || !kv_len ||
         (kind == ATTN_CACHE_E4M3 && (!k_scale || !v_scale)))
         return ATTN_ERR_NULL;
-    if (T_rows < 1 || B < 1 || H_kv < 1 || n_pages < 1 || table_width < 1 || B == 0x7fffffff)
+    if (T_rows < 1 || B < 1 || H_kv < 1 || n_pages < 1 || table_width < 1 || B > attn::kMostSequences)
         return ATTN_ERR_SHAPE;
     if (D != 64 && D != 128 && D != 256)
         return ATTN_ERR_UNSUPPORTED_D;

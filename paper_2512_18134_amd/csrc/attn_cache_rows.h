@@ -21,6 +21,9 @@ __device__ __forceinline__ int quotient(int a, int b)
 // The same of a count that may pass 32 bits (the compiler's 64-bit division is some 100 instructions).
 __device__ __forceinline__ long long quotient(long long a, int b) { return a < 1 << 22 ? quotient((int)a, b) : a / b; }
 
+// Sequences of a call, at most: the kernels count them in steps of up to 1024 lanes, which have to stay below 2^31.
+constexpr int kMostSequences = 1 << 30;
+
 struct CacheParams {
     const int *page_table, *start, *kv_len;
     int T, B, H_kv;

@@ -217,7 +217,7 @@ int paged_fwd(const void *q, const long long *strides, void *o, float *lse, cons
     if (!q || !strides || !o || !lse || !k_pages || !v_pages || !page_table || !start || !kv_len || !workspace ||
         (kind == ATTN_CACHE_E4M3 && (!k_scale || !v_scale)))
         return ATTN_ERR_NULL;
-    if (T < 1 || B < 1 || H_q < 1 || H_kv < 1 || H_q % H_kv || n_pages < 1 || table_width < 1 || max_q < 1 || B == 0x7fffffff)
+    if (T < 1 || B < 1 || H_q < 1 || H_kv < 1 || H_q % H_kv || n_pages < 1 || table_width < 1 || max_q < 1 || B > attn::kMostSequences)
         return ATTN_ERR_SHAPE;
     if (D != 64 && D != 128 && D != 256)
         return ATTN_ERR_UNSUPPORTED_D;
@@ -278,7 +278,7 @@ int paged_fwd(const void *q, const long long *strides, void *o, float *lse, cons
 extern "C" long long attn_paged_fwd_workspace_bytes(int T, int B, int H_q, int H_kv, int D)
 {
     if (T < 1 || B < 1 || H_q < 1 || H_kv < 1 || H_q % H_kv || (D != 64 && D != 128 && D != 256) ||
-        (long long)T * H_q > 0x3fffffffLL)
+        (long long)T * H_q > 0x3fffffffLL || B > attn::kMostSequences)
         return -1;
     return attn::workspace_of(T, B, H_q / H_kv, D).bytes;
 }
