@@ -55,7 +55,8 @@ enum { ATTN_CACHE_16BIT = 0, ATTN_CACHE_E4M3 = 1 };
  * or less).  NaN and infinities are not checked: such a row's elements are unspecified.
  * Two rows of a call must not have the same place (pages that sequences share are written by none of them).
  *
- * Ownership, streams and errors are those of attn_fwd (attn_fwd.h); ATTN_ERR_SHAPE stands for sizes and strides,
+ * Ownership, streams and errors are those of attn_fwd (attn_fwd.h); ATTN_ERR_SHAPE stands for sizes and strides, and
+ * for a call that would take 2^32 threads (one head of 2^29 rows at D = 64),
  * ATTN_ERR_UNSUPPORTED for kind and page_size, ATTN_ERR_ALIGN for k, v, pages that are not 16-byte aligned, int32
  * arrays that are not 4-byte aligned and scales that are not 16-byte aligned.
  */

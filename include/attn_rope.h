@@ -40,8 +40,9 @@ extern "C" {
  * other.  No output row may be stored twice (a stride of 0 is for inputs).
  *
  * Ownership, errors and streams are those of attn_fwd (attn_fwd.h): arguments are validated on the host
- * before any HIP call; ATTN_ERR_SHAPE stands for sizes, sections, strides and R alike, ATTN_ERR_ALIGN for
- * tensors that are not 16-byte aligned (pos 4, freq 8).  Bitwise reproducible.
+ * before any HIP call; ATTN_ERR_SHAPE stands for sizes, sections, strides and R alike, and for a call
+ * that would take 2^32 threads (one head of 2^30 tokens at R = 64), ATTN_ERR_ALIGN for tensors that are not 16-byte
+ * aligned (pos 4, freq 8).  Bitwise reproducible.
  */
 int attn_rope(const void *q, void *q_out, const void *k, void *k_out, const long long *strides,
               const int *pos, const double *freq, const int *sections, int n_axes,

@@ -21,6 +21,7 @@
 #include "attn_cache_rows.h"
 #include "attn_common.h"
 #include "attn_fwd.h"
+#include "attn_launch.h"
 
 
 namespace attn {
@@ -281,7 +282,7 @@ int launch(RowsParams &p, hipStream_t st)
     const bool many = runs * row_slices >= 1024;
     p.slices = many ? row_slices : (2 * p.c.H_kv * (D / 8) + 63) / 64;
     const long long blocks = ((many ? runs : (long long)p.c.T) * p.slices + 3) / 4;
-    if (blocks > 0x7fffffffLL)
+    if (blocks > attn::most_workgroups(256))
         return ATTN_ERR_SHAPE;
     if (many)
         hipLaunchKernelGGL((attn::attn_cache_run_kernel<T, D, E4M3, WRITE>), dim3((unsigned)blocks), dim3(256), 0, st, p);

@@ -34,6 +34,9 @@ inline bool allow_lds(const void *kern, int bytes)
     return true;
 }
 
+// Workgroups that a launch may have: the runtime takes less than 2^32 threads in a dimension.
+constexpr long long most_workgroups(int threads) { return 0xffffffffLL / threads; }
+
 // Compute units of the current device (asked once per device), rounded down to a multiple of `multiple`;
 // 0 when the runtime cannot tell.
 inline int cu_count(int multiple)

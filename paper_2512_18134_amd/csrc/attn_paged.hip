@@ -108,7 +108,7 @@ int launch_rows(PagedParams p, int upto, hipStream_t st)
     if (NW > 4)
         p.rounds = 0;                                      // whole sequences
     const long long grid = most_units(p, 16 * MT);
-    if (grid > 0x7fffffffLL)
+    if (grid > attn::most_workgroups(NW * 64))
         return ATTN_ERR_SHAPE;
     p.most_units = (int)grid;
     if (const int rc = launch_cut<16 * MT>(p, st))
@@ -183,15 +183,10 @@ int launch(PagedParams &p, int max_q, hipStream_t st)
         if (few && MT == 1 && ((long long)p.c.T * p.G / 16 + (p.c.B < p.c.T ? p.c.B : p.c.T)) * p.c.H_kv <= attn::kTarget / 2 &&
             ((long long)p.c.table_width << p.c.page_log2) * D * (E4M3 ? 2 : 4) <= attn::kWholeBytes)
             return launch_rows<D, 1, E, E4M3, attn::kWaves>(p, 0x7fffffff, st);
-    if (few || both)
-        rc = launch_rows<D, E, E4M3>(p, MT, both ? most : 0x7fffffff, st);
-    if (rc == ATTN_OK && many)
-        rc = launch_tiles<D, E, E4M3>(p, both ? most : 0, st);
     // no sequence can be longer than one range: nothing to merge
     static_assert(attn::kRowsMinRange <= attn::kTilesMinRange, "the row kernel's ranges are the shorter ones");
     const int shortest = few || both ? attn::kRowsMinRange : attn::kTilesMinRange;
-    if (rc != ATTN_OK || ((long long)p.c.table_width << p.c.page_log2) <= (long long)shortest * attn::kPlanBlock)
-        return rc;
+    const bool merged = ((long long)p.c.table_width << p.c.page_log2) > (long long)shortest * attn::kPlanBlock;
     constexpr int kGroups = 256 / (D / 4);
     const long long o_rows = (long long)p.c.T * p.H_q;
     // eight ranges to a walker, of as many as a sequence may be expected to have: a launch has one for each head and row tile,
@@ -204,6 +199,14 @@ int launch(PagedParams &p, int max_q, hipStream_t st)
     while (walkers < kGroups && 8 * walkers < expected && 8 * walkers < most_ranges)
         walkers *= 2;
     const long long blocks = (o_rows * walkers + kGroups - 1) / kGroups;
+    if (merged && blocks > attn::most_workgroups(256))     // (before anything is launched)
+        return ATTN_ERR_SHAPE;
+    if (few || both)
+        rc = launch_rows<D, E, E4M3>(p, MT, both ? most : 0x7fffffff, st);
+    if (rc == ATTN_OK && many)
+        rc = launch_tiles<D, E, E4M3>(p, both ? most : 0, st);
+    if (rc != ATTN_OK || !merged)
+        return rc;
     hipLaunchKernelGGL((attn::attn_paged_merge_kernel<D, typename E::t>), dim3((unsigned)blocks), dim3(256), 0, st, p, walkers);
     return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH;
 }

@@ -10,6 +10,7 @@
 
 #include "attn_cache_rows.h"   // quotient
 #include "attn_fwd.h"
+#include "attn_launch.h"   // most_workgroups
 #include "attn_rope.h"
 
 namespace attn {
@@ -201,7 +202,7 @@ int rope(const void *q, void *q_out, const void *k, void *k_out, const long long
         p.heads_per_wave *= 2;
     p.head_groups = (int)((heads + p.heads_per_wave - 1) / p.heads_per_wave);
     const long long blocks = (groups * p.head_groups + 3) / 4;
-    if (blocks > 0x7fffffffLL)
+    if (blocks > attn::most_workgroups(256))
         return ATTN_ERR_SHAPE;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     // Outputs that the 256 MB of the last-level cache do not hold next to the inputs are stored past the caches: forward and back

@@ -1,4 +1,6 @@
 """The largest calls of the serving entry points, and what a refusal says, on the host (no GPU needed)."""
+import ctypes
+
 import pytest
 
 from test_serving_abi import OK, PAGED, ROPE, ROWS, arr, b, caller  # noqa: F401
@@ -23,3 +25,20 @@ def test_a_batch_that_the_lanes_cannot_count_is_refused(b, entry, spec):  # noqa
         assert b.attn_paged_fwd_workspace_bytes(3, B, 4, 2, 64) == -1
     assert f(B=1 << 30, start=OK + 2) == b.ATTN_ERR_ALIGN
     assert b.attn_paged_fwd_workspace_bytes(3, 1 << 30, 4, 2, 64) > 0
+
+
+@pytest.mark.parametrize("suffix", ["", "_f16"])
+def test_launches_of_too_many_threads_are_refused_before_any(b, suffix):  # noqa: F811
+    """The runtime takes less than 2^32 threads in a dimension: a call that needs more is refused with its arguments, not by one of
+    its launches (of which attention has up to three)."""
+    rope = caller(b, "attn_rope" + suffix, ROPE)
+    one = dict(H_kv=0, H_q=1, S=1 << 30, n_axes=1, sections=arr([32], ctypes.c_int), strides=arr([0, 0, 64] * 4))
+    assert rope(**one) == b.ATTN_ERR_SHAPE                                        # 2^24 workgroups of 256 threads
+    for entry in ("attn_cache_write", "attn_cache_read"):
+        rows = caller(b, entry + suffix, ROWS)
+        assert rows(T=1 << 29, H_kv=1, strides=arr([64, 0] * 2)) == b.ATTN_ERR_SHAPE
+    paged = caller(b, "attn_paged_fwd" + suffix, PAGED)
+    many = dict(T=1 << 22, B=1 << 22, H_q=8, H_kv=8, strides=arr([512, 64]))
+    assert paged(**many) == b.ATTN_ERR_SHAPE                                      # a row workgroup for every sequence and head
+    merge = dict(T=(1 << 26) - 1, B=1, H_q=8, H_kv=8, D=256, max_q=1 << 26, width=64, strides=arr([2048, 256]))
+    assert paged(**merge) == b.ATTN_ERR_SHAPE                                     # tiles: as many workgroups as run at once; the merge: 2^27
