@@ -401,6 +401,7 @@ def _marshal_splitkv(entry, dt, q, k, v, n_split, o, lse, workspace, causal, sca
 ATTN_CACHE_16BIT = 0
 ATTN_CACHE_E4M3 = 1
 
+_INT_MAX = 2 ** 31 - 1
 _pointer, _int, _int64, _float = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_float
 for _name, _args in (("attn_rope", [_pointer] * 8 + [_int] * 8 + [_pointer]),
                      ("attn_cache_write", [_pointer] * 10 + [_int] * 8 + [_pointer]),
@@ -422,6 +423,8 @@ def _check_rows(t, dt, dims, name, device):
     """Rows of contiguous elements, any strides between them."""
     if t.dtype != dt or not t.is_cuda or t.dim() != dims or (t.shape[-1] > 1 and t.stride(-1) != 1):
         raise TypeError("%s must be a %d-D %s tensor on the GPU whose last dimension is contiguous" % (name, dims, dt))
+    if max(t.shape) > _INT_MAX:                       # (a broadcast view may be; ctypes would keep 32 bits of it)
+        raise ValueError("%s has a dimension beyond 2^31 - 1" % name)
     if t.device != device:
         raise ValueError("%s is on another device" % name)
 
@@ -691,7 +694,7 @@ def _marshal_paged(entry, dt, q, k_pages, v_pages, page_table, start, kv_len, k_
     with torch.cuda.device(q.device):
         rc = entry(q.data_ptr(), _strides((q, 0), (q, 1)), o.data_ptr(), lse.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
                    _address(k_scale), _address(v_scale), page_table.data_ptr(), start.data_ptr(), kv_len.data_ptr(), kind,
-                   workspace.data_ptr(), workspace.numel() * workspace.element_size(), T if max_q is None else int(max_q),
+                   workspace.data_ptr(), workspace.numel() * workspace.element_size(), T if max_q is None else min(int(max_q), _INT_MAX),
                    T, B, H_q, H_kv, D, n_pages, page_size, width, int(bool(causal)), float(scale), stream.cuda_stream)
     if rc != ATTN_OK:
         raise AttnError(rc)

@@ -2,6 +2,7 @@
 import ctypes
 
 import pytest
+import torch
 
 from test_serving_abi import OK, PAGED, ROPE, ROWS, arr, b, caller  # noqa: F401
 
@@ -42,3 +43,17 @@ def test_launches_of_too_many_threads_are_refused_before_any(b, suffix):  # noqa
     assert paged(**many) == b.ATTN_ERR_SHAPE                                      # a row workgroup for every sequence and head
     merge = dict(T=(1 << 26) - 1, B=1, H_q=8, H_kv=8, D=256, max_q=1 << 26, width=64, strides=arr([2048, 256]))
     assert paged(**merge) == b.ATTN_ERR_SHAPE                                     # tiles: as many workgroups as run at once; the merge: 2^27
+
+
+def test_rows_that_a_c_int_cannot_count_are_refused(b):  # noqa: F811
+    """A view that repeats one row 2^32 + 1 times is a legal input of attn_cache_write; handed on in 32 bits it would be one row."""
+    class Rows:
+        dtype, is_cuda, device = torch.bfloat16, True, torch.device("cuda", 0)
+
+        def __init__(self, t):
+            self.shape, self.stride, self.dim = t.shape, t.stride, t.dim
+    fine = torch.zeros(1, 1, 64, dtype=torch.bfloat16)
+    b._check_rows(Rows(fine.expand(2 ** 31 - 1, 1, 64)), torch.bfloat16, 3, "k", Rows.device)
+    for n in (2 ** 31, 2 ** 32 + 1):
+        with pytest.raises(ValueError):
+            b._check_rows(Rows(fine.expand(n, 1, 64)), torch.bfloat16, 3, "k", Rows.device)
