@@ -105,7 +105,9 @@ int attn_cache_read_f16(void *k, void *v, const long long *strides,
  *   k_pages .. kv_len, kind   as above (the cache read only)
  *   workspace  device pointer, 16-byte aligned, owned by the caller, overwritten; workspace_bytes at least
  *              attn_paged_fwd_workspace_bytes(T, B, H_q, H_kv, D), else ATTN_ERR_WORKSPACE.  It holds nothing
- *              between calls; calls that overlap in time need one each
+ *              between calls; calls that overlap in time need one each, layers that follow each other share one.
+ *              At D = 128 it takes 9 to 36 MB for up to 128 rows (T * H_q / H_kv), 179 MB for more, besides 16 bytes
+ *              for every token (at D = 64 half, at D = 256 18, 36 and 178 MB): what the chip's workgroups leave at once
  *   max_q      the largest n_b, or an upper bound (T if nothing better is known): it chooses the kernels.  A wrong
  *              value costs speed, not correctness
  *   H_q        a multiple of H_kv;  scale finite and > 0;  T * H_q and H_kv * page_size * D below 2^30

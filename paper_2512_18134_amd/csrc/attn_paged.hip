@@ -47,13 +47,17 @@ struct Workspace {
     long long part_o[2], part_lse[2], merge, cut[2], bytes;   // offsets in bytes
 };
 
+// D = 128: 9, 18 or 36 MB for the row kernel, by the tiles that T tokens can need (no max_q asks for taller ones), and 143 MB for
+// the tile kernels of calls with more rows than it takes.  How many slots a call uses is up to lengths that the host
+// does not see.
 inline Workspace workspace_of(int T, int B, int G, int D)
 {
     Workspace w;
     long long at = 0;
+    const long long most = rows_kernel_most(D), call = (long long)T * G;
     for (int kernel = 0; kernel < 2; ++kernel) {
-        const long long rows = kernel ? (D == 256 ? 128 : 256) : D == 256 ? 32 : 64;
-        const long long slots = kernel && (long long)T * G <= rows_kernel_most(D) ? 0 : kSlots;
+        const long long rows = kernel ? (D == 256 ? 128 : 256) : 16 * row_tiles(D, call < most ? call : most);
+        const long long slots = kernel && call <= most ? 0 : kSlots;
         w.part_o[kernel] = at;
         at += slots * rows * D * 4;
         w.part_lse[kernel] = at;

@@ -57,3 +57,19 @@ def test_rows_that_a_c_int_cannot_count_are_refused(b):  # noqa: F811
     for n in (2 ** 31, 2 ** 32 + 1):
         with pytest.raises(ValueError):
             b._check_rows(Rows(fine.expand(n, 1, 64)), torch.bfloat16, 3, "k", Rows.device)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_the_workspace_follows_the_rows_of_the_call(b, D):  # noqa: F811
+    """Partial rows for as many units as run at once, in tiles that the call's rows can need: a single token of four query heads to
+    a key head does not pay for tiles of 64 rows.  (1088 slots; tiles of 16 rows up to 16, 32 up to 32, then 64, but 32 at D = 256.)"""
+    need = lambda T, B=1, G=1: b.attn_paged_fwd_workspace_bytes(T, B, 2 * G, 2, D)
+    slots = lambda rows: 1088 * rows * (D + 1) * 4
+    assert need(1, 1, 4) == slots(16) + 16 and need(4, 4, 4) == slots(16) + 4 * 16
+    assert need(17) == slots(32) + 17 * 16 and need(8, 1, 4) == slots(32) + 8 * 16
+    assert need(33) == slots(32 if D == 256 else 64) + 33 * 16
+    most = 64 if D == 256 else 128
+    assert need(most) == slots(most // 2) + most * 16
+    assert need(most + 1) == slots(most // 2) + slots(2 * most) + (most + 1) * 16      # the tile kernels too
+    sizes = [need(T, 1, G) for G in (1, 4) for T in range(1, 300)]
+    assert sizes[:299] == sorted(sizes[:299]) and sizes[299:] == sorted(sizes[299:])
