@@ -11,13 +11,14 @@
 
 namespace attn {
 
-// Workgroups that the chip holds at once: on each of 256 compute units two of the e4m3 tile kernel, one of the 16-bit one, two
-// of the row kernel where its registers let two waves share a SIMD.  (16 sequences of four drafted tokens and 512 .. 4100
-// positions, D = 256: 26.0 us cut for 512, 22.0 for 256; 16 tokens over 8000 positions, D = 128: see row_slots.)
+// Workgroups that the chip holds at once: on each of 256 compute units two of the e4m3 tile kernel, one of the 16-bit one, and of
+// the row kernel what its tiling promises the compiler.  (16 sequences of four drafted tokens and 512 .. 4100
+// positions, D = 256: 26.0 us cut for 512, 22.0 for 256.)
 constexpr int kTarget = 512;
-constexpr int row_slots(int D, int MT, bool e4m3)
+template <int D, int MT>
+constexpr int row_slots()
 {
-    return (MT == 1 && D <= 128) || (MT == 2 && (D == 64 || (D == 128 && e4m3))) ? kTarget : kTarget / 2;
+    return kTarget / 2 * PagedRowsTiling<D, MT, 4>::PER_CU;
 }
 // Cuts that a launch may choose from (PagedParams::rounds).  Four for tiles gain nothing: four sequences of 200 new tokens at 2000
 // 62.6 us, with two 59.9; a chunk of 2048 at 32768 823 and 817.
@@ -106,7 +107,7 @@ template <int D, int MT, typename E, bool E4M3, int NW = 4>
 int launch_rows(PagedParams p, int upto, hipStream_t st)
 {
     p.kernel = 0, p.slots = p.parts[0].slots, p.rows_above = 0, p.rows_upto = upto;
-    p.target = attn::row_slots(D, MT, E4M3), p.rounds = attn::kRowsRounds, p.min_range = attn::kRowsMinRange, p.overhead = attn::kRowsOverhead;
+    p.target = attn::row_slots<D, MT>(), p.rounds = attn::kRowsRounds, p.min_range = attn::kRowsMinRange, p.overhead = attn::kRowsOverhead;
     p.merging = attn::kRowsMerging;
     p.halve = 0;
     if (NW > 4)
