@@ -49,3 +49,48 @@ def test_a_call_is_cut_for_the_workgroups_that_the_chip_holds(tmp_path):
         assert x["target"] == 256 * min(per_cu, 2), (size, L.template(x["kernel"]), have[x["kernel"]])
         seen.add(x["kernel"])
     assert len(seen) == 3 * 4 * 4 - 4               # (D = 256 has no tiles of 64 rows)
+
+
+def test_the_cache_tests_sizes_are_written_and_read_in_runs(tmp_path):
+    """The kernel that takes runs of tokens, in all its variants, is what the sizes of test_cache_runs_gpu.py launch."""
+    import test_cache_runs_gpu as C
+    calls = [L.rows(what, T, len(C.batch(T, page, 91)[0]), H, D, page, 1 << 20, 64, dt, e4m3)
+             for D, H, T, page in C.SIZES for what in ("write", "read") for dt in ("bf16", "f16") for e4m3 in (False, True)]
+    seen = set()
+    for call, (rc, lines) in zip(calls, L.launches(tmp_path, calls)):
+        assert rc == 0 and len(lines) == 1
+        assert "attn_cache_run_kernel" in lines[0]["kernel"], call
+        seen.add(lines[0]["kernel"])
+    assert len(seen) == 3 * 2 * 2 * 2
+    for D, H, T, page in C.SIZES:
+        news, _, front, behind = C.batch(T, page, 91)
+        assert T % 8 and news[-1] > 0 and front + sum(news) + behind == T
+        start = front
+        crowded = 0                                        # empty sequences that begin inside one run of eight tokens
+        at = {}
+        for n in news:
+            if n == 0:
+                at[start // 8] = at.get(start // 8, 0) + 1
+            start += n
+        crowded = max(at.values())
+        assert crowded > 64
+    assert any(2 * H % (512 // D) for D, H, _, _ in C.SIZES)
+
+
+def test_the_rope_tests_sizes_take_the_kernels_of_large_calls(tmp_path):
+    """How many heads a wave takes is read from the launch's workgroups of four waves; whether it stores past the caches from the
+    kernel's last template argument."""
+    import test_rope_large_gpu as P
+    calls = [L.rope(*size[:6], interleaved=inter) for size in P.SIZES for inter in (0, 1)]
+    found = L.launches(tmp_path, calls)
+    for i, (rc, lines) in enumerate(found):
+        b, hq, hkv, s, d, sections, per_wave, past = P.SIZES[i // 2]
+        assert rc == 0 and len(lines) == 1
+        name = lines[0]["kernel"]
+        lanes = 1
+        while 8 * lanes < sum(sections):
+            lanes *= 2
+        groups = -(-b * s * lanes // 64)
+        assert lines[0]["grid"] == -(-groups * -(-(hq + hkv) // per_wave) // 4), (P.SIZES[i // 2], lines[0])
+        assert name.split("attn_rope_kernelI")[1].count("Lb1E") == i % 2 + past, name      # INTERLEAVED, PAST
+    assert {size[6] for size in P.SIZES} >= {1, 4, 8, 16} and any(size[7] for size in P.SIZES)
