@@ -158,9 +158,10 @@ def test_chunks_whose_windows_are_refilled_and_workgroups_that_take_three_units(
     check(pool, news, 1, q, o, lse, dt)
 
 
+@pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("D", [64, 128, 256])
-def test_long_ranges_of_a_cut_chunk(D, e4m3):
+def test_long_ranges_of_a_cut_chunk(D, e4m3, causal):
     """One sequence of many keys, cut: walks that begin in the middle of it, with refilled windows, and the merge of their rows."""
     if torch.cuda.mem_get_info()[0] < 60 << 30:
         pytest.skip("needs 60 GB")
@@ -170,10 +171,10 @@ def test_long_ranges_of_a_cut_chunk(D, e4m3):
     pool = Pool([kv], H, D, 64, "bf16", e4m3, 32, pages_beyond(H, 64, D, e4m3))
     for i in (11, 60, 61, 200, 333):
         pool.table[0, i] = -1
-    q, o, lse, notes = attend(pool, [n], G, "bf16")
+    q, o, lse, notes = attend(pool, [n], G, "bf16", causal)
     units, longest = plan_of(notes, [n], [kv], H, G, BM)
     assert int(notes[0, 2]) > 1 and longest > keys_of_window, (units, longest)
-    check(pool, [n], G, q, o, lse, "bf16")
+    check(pool, [n], G, q, o, lse, "bf16", causal)
 
 
 # ---- rows: 32 steps of a wave to a window, 4096 keys of a workgroup
@@ -196,3 +197,20 @@ def test_steps_whose_windows_are_refilled(D, new, G, dt, e4m3):
     units, longest = plan_of(notes, news, kvs, H, G, BM)
     assert (notes[:, 3] & 1 == 0).all() and longest > 4096, (units, longest)
     check(pool, news, G, q, o, lse, dt, every=9)
+
+
+@pytest.mark.parametrize("dt, e4m3", [("bf16", False), ("f16", False), ("bf16", True), ("f16", True)])
+@pytest.mark.parametrize("D, new, G", [(D, n, G) for D in (64, 128, 256)
+                                       for n, G in ((1, 1), (4, 4), (17, 1), (8, 4), (11, 3), (16, 4), (32, 4))
+                                       if n * G <= (64 if D == 256 else 128)], ids=lambda x: str(x))
+def test_a_cut_step_keeps_to_its_workspace(D, new, G, dt, e4m3):
+    """Partial rows of tiles of 16, 32 and 64 rows, merged; nothing behind the workspace is written, which is as large as the call's
+    rows can make it."""
+    rows = new * G
+    BM = 16 if rows <= 16 else 32 if rows <= 32 or D == 256 else 64
+    kvs, news, H = [9001, 2000 + new], [new, max(1, new // 2)], 3
+    pool = Pool(kvs, H, D, 16, dt, e4m3, 34, 0)
+    q, o, lse, notes = attend(pool, news, G, dt)
+    units, longest = plan_of(notes, news, kvs, H, G, BM)
+    assert int(notes[0, 2]) > 8, (units, longest)
+    check(pool, news, G, q, o, lse, dt)
