@@ -8,7 +8,8 @@
  *     kind ATTN_CACHE_16BIT   elements of the type of the rows (bf16, or fp16 in the _f16 entry points)
  *     kind ATTN_CACHE_E4M3    e4m3 elements (OCP FP8, largest 448); every position and head of K and of V has a
  *                             power of two of its own, stored as its exponent + 127 in one byte of
- *                             k_scale / v_scale [page][h][place]: an element stands for e4m3 * 2^(scale - 127)
+ *                             k_scale / v_scale [page][h][place]: an element stands for e4m3 * 2^(scale - 127).
+ *                             (attn_cache_write leaves 1 .. 247; a pool filled otherwise keeps to 1 .. 254)
  *
  * The calls take a batch of B sequences.  Three arrays say which rows and positions belong to whom:
  *
@@ -73,7 +74,7 @@ int attn_cache_write_f16(const void *k, const void *v, const long long *strides,
  * attn_cache_read -- enqueue the copy of the rows' positions out of the cache and return (asynchronous): the inverse of
  * attn_cache_write.  n_b = kv_len[b] reads the whole sequence.  Arguments as there, with k and v written and the cache
  * read only.  e4m3 elements are returned as the values they stand for, rounded to the row type (exact within its
- * normal range).  No two rows of k or of v may overlap.
+ * normal range; what lies beyond the type, of a pool that rows of the other type have filled, is unspecified).  No two rows of k or of v may overlap.
  */
 int attn_cache_read(void *k, void *v, const long long *strides,
                     const void *k_pages, const void *v_pages, const unsigned char *k_scale, const unsigned char *v_scale,
@@ -96,8 +97,10 @@ int attn_cache_read_f16(void *k, void *v, const long long *strides,
  *
  * An empty J gives o = 0 and lse = -inf.  (attn_fwd's causal mask is aligned to the first key; the two agree
  * where n_b = kv_len[b].)  The rows' own keys have to be in the cache: attn_cache_write comes first.
- * Products run on bf16 (fp16) MFMA with fp32 accumulation, e4m3 elements enter them as the exact values they stand
- * for; P is rounded to bf16 (fp16) before the second product, the row sum is taken over the unrounded fp32 P.
+ * Products run on bf16 (fp16) MFMA with fp32 accumulation, e4m3 elements enter them as the values they stand for
+ * (rounded as attn_cache_read rounds them); as in attn_fwd, P is rounded to bf16 (fp16) before the second product and the
+ * row sum is taken over the unrounded fp32 P.  Against 64 bits o is then off by 0.0021 to 0.0024 of its norm (bf16; 0.00028
+ * fp16), of which rounding o alone makes 0.0017 (0.00021).
  *
  *   q          device pointer, bf16, row t and head h of D contiguous elements at t * strides[0] + h * strides[1]
  *   strides    host array of 2, in elements, multiples of 8, not negative
@@ -112,10 +115,15 @@ int attn_cache_read_f16(void *k, void *v, const long long *strides,
  *              value costs speed, not correctness
  *   H_q        a multiple of H_kv;  scale finite and > 0;  T * H_q and H_kv * page_size * D below 2^30
  *
- * Rows of o and lse that belong to nobody are left as they were.  NaN and infinities in K and V are not checked, except
- * that places behind a sequence's last position may hold anything.  Bitwise reproducible for the same lengths
- * and max_q (long sequences are cut into ranges whose partial results a second kernel merges; the cut depends on the
- * lengths of the whole batch).
+ * Rows of o and lse that belong to nobody are left as they were.  NaN and infinities in q, K and V are not checked (what
+ * the rows and sequences that hold them give is unspecified, causally earlier tokens of such a sequence's chunk
+ * included), except that places behind a sequence's last position may hold anything.  Bitwise reproducible
+ * for the same sizes, lengths and max_q (long sequences are cut into ranges whose partial results a second kernel merges;
+ * the cut depends on the lengths of the whole batch).
+ *
+ * The host chooses the kernels by sizes alone, so a table that could hold long sequences gets the launches that those
+ * need: one token over 1000 positions (16 heads, D = 64) takes 9.4 us with a table of 1000 positions and 10.6 with one
+ * of 131072, one over 500 (32 heads over 8, D = 128) 9.2 and 11.0, where the narrow table saves the merge.
  */
 int attn_paged_fwd(const void *q, const long long *strides, void *o, float *lse,
                    const void *k_pages, const void *v_pages, const unsigned char *k_scale, const unsigned char *v_scale,

@@ -452,8 +452,8 @@ def _address(t):
 def attn_rope(q, k, pos, freq, sections, q_out=None, k_out=None, interleaved=False, inverse=False, stream=None):
     """attn_rope on torch device tensors (include/attn_rope.h): q and k turned by the positions of their tokens.
 
-    q [B,H_q,S,D], k [B,H_kv,S,D] (or None): bf16 on the GPU, any strides with D contiguous elements, so slices of a
-    projection's rows are fine (rows[:, :H_q].transpose(0, 1)[None]).  pos int32 [n_axes,B,S], freq fp64 [pairs], radians
+    q [B,H_q,S,D], k [B,H_kv,S,D] (or None): bf16 on the GPU, D contiguous elements, other strides in multiples of 8, so slices
+    of a projection's rows are fine (rows[:, :H_q].transpose(0, 1)[None]).  pos int32 [n_axes,B,S], freq fp64 [pairs], radians
     per unit of position; sections: how many pairs follow each axis (sum = pairs; 2 * pairs of a head's D elements are
     turned, the others are copied).  q_out and k_out are allocated when not given (contiguous); they may be q and k.
     inverse=True turns back: with the gradients of the outputs in place of q and k it gives the gradients of the inputs.
@@ -544,7 +544,7 @@ def _check_cache(dt, k_pages, v_pages, page_table, start, kv_len, k_scale, v_sca
 def attn_cache_write(k, v, k_pages, v_pages, page_table, start, kv_len, k_scale=None, v_scale=None, stream=None):
     """attn_cache_write on torch device tensors (include/attn_cache.h): new rows of K and V into their pages.
 
-    k, v [T,H_kv,D] bf16, any strides with D contiguous elements.  k_pages, v_pages [n_pages,H_kv,page_size,D]: bf16, or
+    k, v [T,H_kv,D] bf16, D contiguous elements, other strides in multiples of 8.  k_pages, v_pages [n_pages,H_kv,page_size,D]: bf16, or
     float8_e4m3fn with k_scale, v_scale uint8 [n_pages,H_kv,page_size].  page_table int32 [B,table_width], start int32 [B+1],
     kv_len int32 [B]: rows start[b] .. start[b+1]-1 become the last positions below kv_len[b] of sequence b.
     Asynchronous on `stream`.  Returns (k_pages, v_pages).
@@ -572,8 +572,8 @@ def attn_cache_write_f16(k, v, k_pages, v_pages, page_table, start, kv_len, k_sc
 def attn_cache_read(k_pages, v_pages, page_table, start, kv_len, n_rows, k_scale=None, v_scale=None, k=None, v=None,
                     stream=None):
     """attn_cache_read on torch device tensors (include/attn_cache.h): the last positions below kv_len[b] of sequence b into
-    rows start[b] .. start[b+1]-1 of k and v, [n_rows,H_kv,D] bf16, allocated when not given (any strides with D contiguous
-    elements: [H_kv,n_rows,D] tensors transposed are what attn_fwd takes).  Rows of no sequence are left as they were.  The
+    rows start[b] .. start[b+1]-1 of k and v, [n_rows,H_kv,D] bf16, allocated when not given (D contiguous elements,
+    other strides in multiples of 8: [H_kv,n_rows,D] tensors transposed are what attn_fwd takes).  Rows of no sequence are left as they were.  The
     cache's arguments are those of attn_cache_write.  Asynchronous on `stream`.  Returns (k, v).
     """
     r = (_marshal_module or _native()).read(0, k_pages, v_pages, page_table, start, kv_len, n_rows, k_scale, v_scale, k, v,
@@ -639,7 +639,7 @@ def attn_paged_fwd(q, k_pages, v_pages, page_table, start, kv_len, k_scale=None,
                    causal=True, scale=None, max_q=None, stream=None):
     """attn_paged_fwd on torch device tensors (include/attn_cache.h): the new tokens' queries against the cache.
 
-    q [T,H_q,D] bf16, any strides with D contiguous elements; H_q a multiple of the cache's H_kv.  The cache's arguments are
+    q [T,H_q,D] bf16, D contiguous elements, other strides in multiples of 8; H_q a multiple of the cache's H_kv.  The cache's arguments are
     those of attn_cache_write, which has put the same rows' keys and values there.  o (bf16 [T,H_q,D]) and lse (fp32 [T,H_q])
     are allocated when not given; rows of no sequence are left as they were.  workspace: a contiguous GPU tensor of at least
     attn_paged_fwd_workspace_bytes(...) bytes (allocated when not given); calls that overlap in time need one each.

@@ -8,8 +8,9 @@
 //   D = 64    8 waves x 32 rows, 64-key tiles, two waves per SIMD
 //   D = 128   4 waves x 64 rows, 32-key tiles, O and Q in AGPRs
 //   D = 256   4 waves x 32 rows, 32-key tiles, O and Q in AGPRs
-// 2048 new tokens at the end of 32768, 32 heads over 8, D = 128: 1065 GFLOP in 800 to 830 us by card, 1280 to 1330 TFLOP/s (a large matrix product
-// of the library: 1141), the matrix pipe busy in 79 % of the cycles and the clock at its power limit; K and V of a head come
+// 2048 new tokens at the end of 32768, 32 heads over 8, D = 128: 1065 GFLOP in 795 to 834 us on most cards, 940 on the slowest,
+// 1340 to 1130 TFLOP/s (a large matrix product of the library: 1141), the matrix pipe busy in 79 % of the cycles and the
+// clock at its power limit; two sequences of 2048 at 16384, D = 64: 500 us; 2048 at 16384, 16 heads over 4, D = 256: 430 us.  K and V of a head come
 // from HBM once and are then read from the L2 of the one XCD that walks the head.  A prompt of 4096 from its start, D = 128:
 // 135 us.  Before units of a head were kept on an XCD the first took 1567 us.
 // Requires H_kv * page_size * D * 2 < 2^31 (the loop multiplies a page's bytes in 32 bits).

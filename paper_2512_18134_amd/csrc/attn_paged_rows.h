@@ -21,7 +21,8 @@
 //
 // Softmax against a lazily moved reference: a row's reference moves only where a score exceeds it by more than 8 (in the
 // base-2 domain), so most steps need no maximum across lanes and no rescaling; sums and accumulators
-// are fp32, and a P of at most 2^8 loses nothing in either 16-bit type.
+// are fp32.  P enters the second product in 16 bits (at most half a step, 2^-8 of it in bf16 and 2^-11 in fp16: there
+// is no product of fp32 operands at this rate; the row sum keeps its 32), and a P of up to 2^8 is as exact there as one of up to 1.
 #pragma once
 #include "attn_paged_plan.h"
 

@@ -14,9 +14,10 @@
 // numbers of 64 tiles.  The rows pass through registers, where they become 16-bit ones once for all waves: e4m3 times a power
 // of two is exact in either type.
 //
-// 2048 new tokens at the end of 32768, 32 heads over 8, D = 128: 1146 us, 930 TFLOP/s, the matrix pipe busy in 43 % of the
-// cycles; two sequences of 2048 at the end of 16384, D = 64: 678 us; 16 heads over 4, D = 256: 717 us.  The scheduled loops
-// of attn_paged_asm.h take 16-bit rows of the same shapes in 806, 521 and 450 us: their direct loads cannot convert.
+// 2048 new tokens at the end of 32768, 32 heads over 8, D = 128: 1027 to 1146 us by card, 930 to 1040 TFLOP/s, the matrix pipe
+// busy in 43 % of the cycles; two sequences of 2048 at the end of 16384, 32 heads over 8, D = 64: 659 us; 2048 at the end of 16384, 16
+// heads over 4, D = 256: 611 us.  The scheduled loops of attn_paged_asm.h take 16-bit rows of these in 796, 500 and 429 us on
+// the same card as the lower figures: their direct loads cannot convert.
 #pragma once
 #include "attn_paged_rows.h"
 

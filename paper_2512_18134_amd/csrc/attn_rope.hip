@@ -61,7 +61,8 @@ __global__ __launch_bounds__(256) void attn_rope_kernel(const RopeParams p)
     const int first = INTERLEAVED ? 16 * c : 8 * c, second = INTERLEAVED ? 16 * c + 8 : half + 8 * c;
     // U heads at a time, all their loads before their stores (which the compiler must take for aliases); the first ones' before
     // the sines and cosines, since a small call is a chain of latencies (2 x 777 tokens of 20 heads 5.6 us, behind them 5.9),
-    // but not in a large one, where other waves fill the wait (4 x 4096 tokens there and back 101 us, before them 114)
+    // but not in a large one, where other waves fill the wait (4 x 4096 tokens of 32 heads there and back, other tensors every time:
+    // 101 us, before them 114)
     constexpr int U = 4;
     t8 lo[U], hi[U];
     T *out[U];
@@ -206,7 +207,8 @@ int rope(const void *q, void *q_out, const void *k, void *k_out, const long long
         return ATTN_ERR_SHAPE;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     // Outputs that the 256 MB of the last-level cache do not hold next to the inputs are stored past the caches: forward and back
-    // of 4 x 32 heads of 4096 tokens, D = 128, 110 us through them, 93 past them; 16 heads of 16384, D = 64 (34 MB), 15.0 and 16.0.
+    // of 4 x 32 heads of 4096 tokens, D = 128, the same tensors again and again, 110 us through them, 93 past them (102 to 106 on
+    // tensors that change); 16 heads of 16384, D = 64 (34 MB), 15.0 and 16.0.
     const bool past = tokens * heads * D * 2 > (64LL << 20);
     const dim3 grid((unsigned)blocks), threads(256);
     if (interleaved && past)
