@@ -98,7 +98,7 @@ int attn_cache_read_f16(void *k, void *v, const long long *strides,
  * An empty J gives o = 0 and lse = -inf.  (attn_fwd's causal mask is aligned to the first key; the two agree
  * where n_b = kv_len[b].)  The rows' own keys have to be in the cache: attn_cache_write comes first.
  * Products run on bf16 (fp16) MFMA with fp32 accumulation, e4m3 elements enter them as the values they stand for
- * (rounded as attn_cache_read rounds them); as in attn_fwd, P is rounded to bf16 (fp16) before the second product and the
+ * (exact within the row type's normal range); as in attn_fwd, P is rounded to bf16 (fp16) before the second product and the
  * row sum is taken over the unrounded fp32 P.  Against 64 bits o is then off by 0.0021 to 0.0024 of its norm (bf16; 0.00028
  * fp16), of which rounding o alone makes 0.0017 (0.00021).
  *
@@ -109,8 +109,9 @@ int attn_cache_read_f16(void *k, void *v, const long long *strides,
  *   workspace  device pointer, 16-byte aligned, owned by the caller, overwritten; workspace_bytes at least
  *              attn_paged_fwd_workspace_bytes(T, B, H_q, H_kv, D), else ATTN_ERR_WORKSPACE.  It holds nothing
  *              between calls; calls that overlap in time need one each, layers that follow each other share one.
- *              At D = 128 it takes 9 to 36 MB for up to 128 rows (T * H_q / H_kv), 179 MB for more, besides 16 bytes
- *              for every token (at D = 64 half, at D = 256 18, 36 and 178 MB): what the chip's workgroups leave at once
+ *              It takes what the chip's workgroups leave at once, by rows (T * H_q / H_kv): at D = 128 9 MB up to 16 of
+ *              them, 18 up to 32, 36 up to 128, 180 beyond; half of that at D = 64; at D = 256 18 up to 16, 36 up to 64,
+ *              179 beyond; and 16 bytes for every token
  *   max_q      the largest n_b, or an upper bound (T if nothing better is known): it chooses the kernels.  A wrong
  *              value costs speed, not correctness
  *   H_q        a multiple of H_kv;  scale finite and > 0;  T * H_q and H_kv * page_size * D below 2^30
