@@ -1,0 +1,49 @@
+/*
+ * attn_tree.h -- C ABI of libmi355attn.so: attention of a tree of drafted tokens over the paged cache of attn_cache.h, for
+ * MI355X (gfx950).
+ */
+#ifndef MI355_ATTN_TREE_H
+#define MI355_ATTN_TREE_H
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/*
+ * attn_paged_tree -- enqueue the attention of drafted tokens over the cache and return (asynchronous): attn_paged_fwd
+ * (attn_cache.h) with a mask among a sequence's new tokens.  Row t = start[b] + i, at position kv_len[b] - n_b + i, sees
+ *
+ *     J = { j : 0 <= j < kv_len[b] - n_b, j has a page }                             all that lay there before
+ *       + { kv_len[b] - n_b + m : 0 <= m < n_b, bit m of the row is set, a position >= 0 that has a page }
+ *
+ *   mask        device pointer, 8-byte aligned, contiguous [T][mask_words] words of 64 bits: bit m % 64 of word m / 64 of row t
+ *               says that row t sees row start[b] + m of its own sequence                               (read only)
+ *   mask_words  1 .. 1024; new tokens behind the mask's last bit are seen by none
+ *
+ * A token of a tree of drafts sees its ancestors and itself, but any set will do: a row's own bit is not taken for granted, and
+ * bits from n_b on are ignored.  A lower triangle gives attn_paged_fwd's causal mask.  The drafted tokens' keys and values have
+ * to be in the cache, in the order of the rows (attn_cache_write); attn_cache_move (attn_evict.h) moves an accepted path together.
+ *
+ * The mask is device memory like start and kv_len: its values may change between the replays of a captured graph.
+ *
+ * All other arguments, the workspace (attn_paged_fwd_workspace_bytes), results, limits, ownership and errors are those of
+ * attn_paged_fwd; ATTN_ERR_NULL, ATTN_ERR_SHAPE and ATTN_ERR_ALIGN stand for the mask's arguments too.  Every row reads every
+ * key that its sequence has, so no row is cheaper for what its mask hides.
+ */
+int attn_paged_tree(const void *q, const long long *strides, void *o, float *lse,
+                    const void *k_pages, const void *v_pages, const unsigned char *k_scale, const unsigned char *v_scale,
+                    const int *page_table, const int *start, const int *kv_len, int kind,
+                    const unsigned long long *mask, int mask_words, void *workspace, long long workspace_bytes, int max_q,
+                    int T, int B, int H_q, int H_kv, int D, int n_pages, int page_size, int table_width,
+                    float scale, void *stream);
+int attn_paged_tree_f16(const void *q, const long long *strides, void *o, float *lse,
+                        const void *k_pages, const void *v_pages, const unsigned char *k_scale, const unsigned char *v_scale,
+                        const int *page_table, const int *start, const int *kv_len, int kind,
+                        const unsigned long long *mask, int mask_words, void *workspace, long long workspace_bytes, int max_q,
+                        int T, int B, int H_q, int H_kv, int D, int n_pages, int page_size, int table_width,
+                        float scale, void *stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* MI355_ATTN_TREE_H */

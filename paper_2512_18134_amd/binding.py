@@ -669,6 +669,13 @@ def attn_paged_fwd_f16(q, k_pages, v_pages, page_table, start, kv_len, k_scale=N
 
 def _marshal_paged(entry, dt, q, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale, o, lse, workspace, causal, scale,
                    max_q, stream):
+    return _paged(entry, dt, q, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale, o, lse, workspace, (), (int(bool(causal)),),
+                  scale, max_q, stream)
+
+
+def _paged(entry, dt, q, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale, o, lse, workspace, mask, causal, scale, max_q,
+           stream):
+    """mask, causal: the C entry point's arguments behind kind and behind table_width."""
     import torch
 
     _check_rows(q, dt, 3, "q", q.device)
@@ -693,9 +700,51 @@ def _marshal_paged(entry, dt, q, k_pages, v_pages, page_table, start, kv_len, k_
         stream = torch.cuda.current_stream(q.device)
     with torch.cuda.device(q.device):
         rc = entry(q.data_ptr(), _strides((q, 0), (q, 1)), o.data_ptr(), lse.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
-                   _address(k_scale), _address(v_scale), page_table.data_ptr(), start.data_ptr(), kv_len.data_ptr(), kind,
+                   _address(k_scale), _address(v_scale), page_table.data_ptr(), start.data_ptr(), kv_len.data_ptr(), kind, *mask,
                    workspace.data_ptr(), workspace.numel() * workspace.element_size(), T if max_q is None else min(int(max_q), _INT_MAX),
-                   T, B, H_q, H_kv, D, n_pages, page_size, width, int(bool(causal)), float(scale), stream.cuda_stream)
+                   T, B, H_q, H_kv, D, n_pages, page_size, width, *causal, float(scale), stream.cuda_stream)
     if rc != ATTN_OK:
         raise AttnError(rc)
     return o, lse
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# Trees of drafted tokens (include/attn_tree.h)
+
+for _suffix in ("", "_f16"):
+    getattr(_lib, "attn_paged_tree" + _suffix).restype = _int
+    getattr(_lib, "attn_paged_tree" + _suffix).argtypes = ([_pointer] * 11 + [_int, _pointer, _int, _pointer, _int64, _int] + [_int] * 8
+                                                           + [_float, _pointer])
+
+
+def attn_paged_tree(q, k_pages, v_pages, page_table, start, kv_len, mask, k_scale=None, v_scale=None, o=None, lse=None,
+                    workspace=None, scale=None, max_q=None, stream=None):
+    """attn_paged_tree on torch device tensors (include/attn_tree.h): drafted tokens' queries against the cache, with a mask among them.
+
+    mask int64 [T,words]: bit m % 64 of word m // 64 of row t says that row t sees row start[b] + m of its own sequence (bit 63 is
+    the sign); what lies in the cache before a sequence's new tokens is seen by all of them.  Everything else is as in
+    attn_paged_fwd.  Asynchronous on `stream`.  Returns (o, lse).
+    """
+    import torch
+    return _marshal_tree(_lib.attn_paged_tree, torch.bfloat16, q, k_pages, v_pages, page_table, start, kv_len, mask, k_scale, v_scale,
+                         o, lse, workspace, scale, max_q, stream)
+
+
+def attn_paged_tree_f16(q, k_pages, v_pages, page_table, start, kv_len, mask, k_scale=None, v_scale=None, o=None, lse=None,
+                        workspace=None, scale=None, max_q=None, stream=None):
+    """attn_paged_tree_f16 on torch device tensors: as attn_paged_tree, with fp16 q and o (and fp16 or e4m3 pages)."""
+    import torch
+    return _marshal_tree(_lib.attn_paged_tree_f16, torch.float16, q, k_pages, v_pages, page_table, start, kv_len, mask, k_scale,
+                         v_scale, o, lse, workspace, scale, max_q, stream)
+
+
+def _marshal_tree(entry, dt, q, k_pages, v_pages, page_table, start, kv_len, mask, k_scale, v_scale, o, lse, workspace, scale, max_q,
+                  stream):
+    import torch
+
+    _check_rows(q, dt, 3, "q", q.device)
+    if mask.dim() != 2 or mask.shape[1] > _INT_MAX:
+        raise TypeError("mask must be an int64 tensor [T, words]")
+    _check_array(mask, torch.int64, (q.shape[0], mask.shape[1]), "mask", q.device)
+    return _paged(entry, dt, q, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale, o, lse, workspace, (mask.data_ptr(), mask.shape[1]),
+                  (), scale, max_q, stream)

@@ -27,9 +27,6 @@ struct PagedAsmTiling {
     static constexpr int LDS_BYTES = 8 * BN * D * 2;          // K ring [4] and V ring [4]
 };
 
-// eight rows of zeros: what a tile without a page is made of
-__device__ const u32x4 kPagedZeroRows[8 * 512 / 16] = {};
-
 // One unit.
 template <int D, bool F16>
 __device__ __forceinline__ void attn_paged_asm_unit(const PagedParams &p, const Unit &u, unsigned char *smem)

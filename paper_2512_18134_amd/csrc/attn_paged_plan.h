@@ -63,6 +63,14 @@ struct PagedParams {
     }
 };
 
+// The same with a tree of drafted tokens: which of its sequence's new tokens a row sees, [T][mask_words] words of 32 bits.
+struct TreeParams : PagedParams {
+    const uint32_t *mask;
+    int mask_words;
+};
+template <bool TREE>
+using ParamsOf = typename std::conditional<TREE, TreeParams, PagedParams>::type;
+
 // What the merge kernel needs to know of a token: x = first slot of its sequence, y = row tiles of the sequence,
 // z = its ranges, w = first row of the token in its sequence * 2 + kernel.  Only sequences of several ranges have a
 // meaningful x and w.
@@ -368,8 +376,8 @@ __device__ __forceinline__ void leave_cut(const PagedParams &p, const Scope &sco
     }
 }
 
-template <int BM>
-__global__ __launch_bounds__(1024) void attn_paged_plan_kernel(const PagedParams p)
+template <int BM, bool TREE>
+__global__ __launch_bounds__(1024) void attn_paged_plan_kernel(const ParamsOf<TREE> p)
 {
     __shared__ int lds[16];
     leave_cut<BM>(p, GroupScope{lds});
@@ -463,8 +471,8 @@ __device__ __forceinline__ void leave_note(const PagedParams &p, const Unit &u)
 // a row's ranges in turn, eight at a time with their loads in flight together, and meet in LDS.  Few rows: a
 // workgroup to a row, for the bound is then the latency of the walk.  Many: a workgroup to as many rows as it holds, since
 // most of them will have nothing to merge.
-template <int D, typename OUT>
-__global__ __launch_bounds__(256) void attn_paged_merge_kernel(const PagedParams p, int walkers)
+template <int D, typename OUT, bool TREE>
+__global__ __launch_bounds__(256) void attn_paged_merge_kernel(const ParamsOf<TREE> p, int walkers)
 {
     constexpr int TPR = D / 4, U = 8;
     __shared__ f32x4 s_acc[256];

@@ -30,6 +30,9 @@ namespace attn {
 
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
+// eight rows of zeros: what a tile in LDS without a page is made of
+__device__ const u32x4 kPagedZeroRows[8 * 512 / 16] = {};
+
 struct PagedBF16 {
     typedef __bf16 t;
     typedef __attribute__((ext_vector_type(2))) __bf16 x2;
@@ -69,12 +72,13 @@ struct PagedF16 {
 
 // The launch's parameters, read anew from where the launch put them (p is the kernel's only argument): what a loop over units
 // keeps of them across a unit takes registers that the unit needs.
-__device__ __forceinline__ PagedParams params_again()
+template <bool TREE = false>
+__device__ __forceinline__ ParamsOf<TREE> params_again()
 {
-    typedef __attribute__((address_space(4))) const PagedParams Arguments;
+    typedef __attribute__((address_space(4))) const ParamsOf<TREE> Arguments;
     Arguments *args = (Arguments *)__builtin_amdgcn_kernarg_segment_ptr();
     asm volatile("" : "+s"(args));
-    return *(const PagedParams *)args;
+    return *(const ParamsOf<TREE> *)args;
 }
 
 // 2^(s - 127) of an e4m3 row's exponent byte
@@ -111,12 +115,33 @@ struct PagedRowsTiling {
     static constexpr int LDS_BYTES = (XCH_FLOATS + ML_FLOATS) * 4;
 };
 
+// Which of the 32 positions from `from` on a row of a tree sees, bit by bit: `before` is the position of its sequence's first
+// new token, and the positions before it are seen by all; mask: the row's words.  A new token behind the mask's last is
+// seen by none.
+__device__ __forceinline__ uint32_t seen_in_tree(const uint32_t *mask, int words, int before, int from)
+{
+    const int node = from - before, w = node >> 5;          // (arithmetic: to below)
+    auto word = [&](int i) -> uint32_t {
+        const uint32_t x = mask[min(max(i, 0), words - 1)];
+        return i < 0 ? 0xffffffffu : i < words ? x : 0u;
+    };
+    return __builtin_amdgcn_alignbit(word(w + 1), word(w), node & 31);
+}
+
+// TREE: seen_in_tree of a lane's rows, of the keys of a step.
+template <bool TREE, int MT>
+struct Seen {};
+template <int MT>
+struct Seen<true, MT> {
+    uint32_t seen[MT];
+};
+
 // E4M3: the pool's kind.  MT: 16-row column tiles.  NW: waves; 4, or 8 where a unit is a whole short sequence (kWholeBytes in
-// attn_paged.hip).  The waves' results meet in one exchange: handed on by four waves at a time, sixteen waves took 3.5 us of
-// a launch's 9.
-template <int D, int MT, typename E, bool E4M3, int NW>
+// attn_paged_launch.h).  The waves' results meet in one exchange: handed on by four waves at a time, sixteen waves took 3.5 us of
+// a launch's 9.  TREE: the sequence's new tokens see each other by the mask instead of by their order.
+template <int D, int MT, typename E, bool E4M3, int NW, bool TREE>
 __global__ __launch_bounds__(NW * 64, (PagedRowsTiling<D, MT, NW>::PER_CU))
-    void attn_paged_rows_kernel(const PagedParams p)
+    void attn_paged_rows_kernel(const ParamsOf<TREE> p)
 {
     typedef PagedRowsTiling<D, MT, NW> T;
     static_assert(NW == 4 || (MT == 1 && D <= 128), "the exchange holds all waves of 16 rows");
@@ -141,6 +166,7 @@ __global__ __launch_bounds__(NW * 64, (PagedRowsTiling<D, MT, NW>::PER_CU))
 
     // ---- the rows of this lane's columns: last visible key, Q
     int last[MT];
+    const uint32_t *sees[MT];                               // TREE: the row's mask
     u32x4 q[MT][KS];
     const int tile_row = u.tile * T::BM;
     const int first_pos = u.kv - u.n;
@@ -149,6 +175,8 @@ __global__ __launch_bounds__(NW * 64, (PagedRowsTiling<D, MT, NW>::PER_CU))
         const int row = min(tile_row + 16 * m + c, u.n_rows - 1);      // rows behind the last repeat it
         const int i = p.token_of(row), hq = u.h * p.G + row - i * p.G;
         last[m] = p.causal ? first_pos + i : u.kv - 1;
+        if constexpr (TREE)
+            sees[m] = p.mask + (size_t)(u.row0 + i) * p.mask_words;
         const typename E::t *src = static_cast<const typename E::t *>(p.q) + (long long)(u.row0 + i) * p.q_st + (long long)hq * p.q_sh;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
@@ -160,7 +188,7 @@ __global__ __launch_bounds__(NW * 64, (PagedRowsTiling<D, MT, NW>::PER_CU))
     // keys that no row of the tile sees are not walked; from `open` on some row does not see a key
     const int low = p.token_of(tile_row), high = p.token_of(min(tile_row + T::BM - 1, u.n_rows - 1));
     const int key1 = p.causal ? min(u.key1, first_pos + high + 1) : u.key1;
-    const int open = p.causal ? min(first_pos + low + 1, u.kv) : u.kv;
+    const int open = TREE ? min(first_pos, u.kv) : p.causal ? min(first_pos + low + 1, u.kv) : u.kv;
     const int n_steps = key1 > u.key0 ? (key1 - u.key0 + 31) / 32 : 0;
 
     f32x4 o[MT][NV];
@@ -175,7 +203,7 @@ __global__ __launch_bounds__(NW * 64, (PagedRowsTiling<D, MT, NW>::PER_CU))
     }
 
     // ---- the stream: registers of one step
-    struct Step {
+    struct Step : Seen<TREE, MT> {
         Piece<16> k[2][KL];
         Piece<NV * EB> v[2][4];
         uint32_t ks[2], vs[2];
@@ -202,6 +230,16 @@ __global__ __launch_bounds__(NW * 64, (PagedRowsTiling<D, MT, NW>::PER_CU))
     constexpr bool AHEAD = KL <= 2 && !LATE_V;
     auto load_k = [&](Step &x, int s, const int id[2]) {
         x.bad = (id[0] | id[1]) < 0;
+        if constexpr (TREE) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+                x.seen[m] = 0xffffffffu;
+            if (u.key0 + 32 * s + 32 > open) {
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+                    x.seen[m] = seen_in_tree(sees[m], p.mask_words, first_pos, u.key0 + 32 * s);
+            }
+        }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             x.ok[t] = id[t] >= 0;
@@ -278,9 +316,13 @@ __global__ __launch_bounds__(NW * 64, (PagedRowsTiling<D, MT, NW>::PER_CU))
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (!x.ok[t] || j0 + 16 * t + 4 * g + i > last[m])
+                    for (int i = 0; i < 4; ++i) {
+                        bool hidden = !x.ok[t] || j0 + 16 * t + 4 * g + i > last[m];
+                        if constexpr (TREE)
+                            hidden |= !(x.seen[m] >> (16 * t + 4 * g + i) & 1);
+                        if (hidden)
                             sc[m][t][i] = -INFINITY;
+                    }
         }
         if constexpr (LATE_V) {
             load_v(x, s, id);

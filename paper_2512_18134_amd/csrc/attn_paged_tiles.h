@@ -19,6 +19,7 @@
 // heads over 4, D = 256: 611 us.  The scheduled loops of attn_paged_asm.h take 16-bit rows of these in 796, 500 and 429 us on
 // the same card as the lower figures: their direct loads cannot convert.
 #pragma once
+#include "attn_dma.h"
 #include "attn_paged_rows.h"
 
 namespace attn {
@@ -47,9 +48,9 @@ struct PagedTilesTiling {
     static constexpr int Q_BYTES = QL * BM * 32, LDS_BYTES = 2 * STAGES * TB + Q_BYTES;
 };
 
-// One unit.
-template <int D, typename E>
-__device__ __forceinline__ void attn_paged_tiles_unit(const PagedParams &p, const Unit &u, unsigned char *smem)
+// One unit.  E4M3: the pool's kind.  TREE: the new tokens see each other by the mask.
+template <int D, typename E, bool E4M3, bool TREE>
+__device__ __forceinline__ void attn_paged_tiles_unit(const ParamsOf<TREE> &p, const Unit &u, unsigned char *smem)
 {
     typedef PagedTilesTiling<D> T;
     constexpr int QB = T::QB, ROWB = T::ROWB, TB = T::TB, BN = T::BN, ST = T::STAGES;
@@ -86,7 +87,7 @@ __device__ __forceinline__ void attn_paged_tiles_unit(const PagedParams &p, cons
     const int low = p.token_of(tile_row), high = p.token_of(min(tile_row + T::BM - 1, u.n_rows - 1));
     const int key1 = __builtin_amdgcn_readfirstlane(p.causal ? min(u.key1, first_pos + high + 1) : u.key1);
     // from here on some row does not see a key
-    const int open = __builtin_amdgcn_readfirstlane(p.causal ? min(first_pos + low + 1, u.kv) : u.kv);
+    const int open = __builtin_amdgcn_readfirstlane(TREE ? min(first_pos, u.kv) : p.causal ? min(first_pos + low + 1, u.kv) : u.kv);
     const int n = key1 > u.key0 ? (key1 - u.key0 + BN - 1) / BN : 0;        // tiles
 
     f32x16 o[QB][DB];
@@ -142,6 +143,29 @@ __device__ __forceinline__ void attn_paged_tiles_unit(const PagedParams &p, cons
             uint32_t ks[NP], vs[NP];
         };
         Rows x;
+        // 16 bits: memory -> LDS, tile t into its stage.  A load takes RPG of the wave's eight rows; lane -> (row, 16-byte chunk), the
+        // swizzle of the tile's rows is applied on the global side.  A tile without a page is made of zeros
+        constexpr int RPG = 1024 / ROWB;
+        auto bring = [&](int t) {
+            const uint32_t stage = lds0 + (t % ST) * 2 * TB + 8 * wave * ROWB;
+            int id, most;
+            size_t row;
+            locate(t, id, row, most);
+            auto scalar = [](uintptr_t a) {
+                return reinterpret_cast<const void *>((uintptr_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(a >> 32)) << 32 |
+                                                      (uint32_t)__builtin_amdgcn_readfirstlane((int)a));
+            };
+            const void *k = scalar(id < 0 ? (uintptr_t)kPagedZeroRows : (uintptr_t)p.k + row * ROWB);
+            const void *v = scalar(id < 0 ? (uintptr_t)kPagedZeroRows : (uintptr_t)p.v + row * ROWB);
+            asm volatile("s_nop 4" : "+s"(k), "+s"(v));     // five wait states between the vector unit's write of a scalar and a load
+#pragma unroll
+            for (int i = 0; i < 8 / RPG; ++i) {
+                const int r = i * RPG + lane / (ROWB / 16), ch = lane % (ROWB / 16);
+                const uint32_t off = (uint32_t)(min(r, most) * ROWB + ((ch & ~15) | ((ch & 15) ^ swz<D>(8 * wave + r))) * 16);
+                dma16(stage + i * 1024, k, off);
+                dma16(stage + TB + i * 1024, v, off);
+            }
+        };
         // (D = 256: places made anew in every tile, as the operands' are below; it has no registers to keep them in)
         auto anew = [](int x) {
             if constexpr (D == 256)
@@ -241,12 +265,30 @@ __device__ __forceinline__ void attn_paged_tiles_unit(const PagedParams &p, cons
                 int ok = 3;                                 // each 16 keys of the tile: is there a page?
                 if (bad)
                     ok = (p.c.page_of(u.b, j0) >= 0) | (p.c.page_of(u.b, min(j0 + 16, u.kv - 1)) >= 0) << 1;
+                if constexpr (TREE) {
+                    uint32_t there = (ok & 1 ? 0xffffu : 0u) | (ok & 2 ? 0xffff0000u : 0u);
+                    if (j0 + BN > u.kv)
+                        there &= (1u << (u.kv - j0)) - 1;
 #pragma unroll
-                for (int b = 0; b < QB; ++b)
+                    for (int b = 0; b < QB; ++b) {
+                        // (the row worked out again: kept across tiles it takes a register that they need)
+                        int row = lane;
+                        asm volatile("" : "+v"(row));
+                        const int i = p.token_of(min(tile_row + (wave * QB + b) * 32 + (row & 31), u.n_rows - 1));
+                        const uint32_t seen = (there & seen_in_tree(p.mask + (size_t)(u.row0 + i) * p.mask_words, p.mask_words, first_pos, j0)) >> 4 * (row >> 5);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (j0 + acc_row(r, g) > last[b] || !(ok >> (r >> 3) & 1))
-                            s[b][r] = -INFINITY;
+                        for (int r = 0; r < 16; ++r)
+                            if (!(seen >> acc_row(r, 0) & 1))
+                                s[b][r] = -INFINITY;
+                    }
+                } else {
+#pragma unroll
+                    for (int b = 0; b < QB; ++b)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            if (j0 + acc_row(r, g) > last[b] || !(ok >> (r >> 3) & 1))
+                                s[b][r] = -INFINITY;
+                }
             }
             u32x4 pt[QB][2];
 #pragma unroll
@@ -277,7 +319,7 @@ __device__ __forceinline__ void attn_paged_tiles_unit(const PagedParams &p, cons
                     }
                 l[b] += sum + sum2;
             }
-            if constexpr (LATE)
+            if constexpr (E4M3 && LATE)
                 fetch(j + 2);
 #pragma unroll
             for (int kc = 0; kc < 2; ++kc)
@@ -290,18 +332,32 @@ __device__ __forceinline__ void attn_paged_tiles_unit(const PagedParams &p, cons
                 }
         };
 
-        advance(0);
-        fetch(0);
-        store(0);
-        fetch(1);
+        if constexpr (E4M3) {
+            advance(0);
+            fetch(0);
+            store(0);
+            fetch(1);
 #pragma clang loop unroll(disable)
-        for (int j = 0; j < n; ++j) {
-            barrier();                                      // tile j is complete, tile j - 1 has been read
-            store(j + 1);
-            advance(j + 2);
-            if constexpr (!LATE)
-                fetch(j + 2);
-            tile(j);
+            for (int j = 0; j < n; ++j) {
+                barrier();                                  // tile j is complete, tile j - 1 has been read
+                store(j + 1);
+                advance(j + 2);
+                if constexpr (!LATE)
+                    fetch(j + 2);
+                tile(j);
+            }
+        } else {
+            advance(0);
+            bring(0);
+#pragma clang loop unroll(disable)
+            for (int j = 0; j < n; ++j) {
+                wait_vmcnt<0>();
+                barrier();                                  // tile j is complete, tile j - 1 has been read
+                advance(j + 1);
+                bring(j + 1);                               // (behind the last tile: that one once more)
+                tile(j);
+            }
+            wait_vmcnt<0>();
         }
     }
 
@@ -342,22 +398,22 @@ __device__ __forceinline__ void attn_paged_tiles_unit(const PagedParams &p, cons
 }
 
 // A workgroup takes every gridDim.x-th unit (attn_paged_asm.h).
-template <int D, typename E>
-__global__ __launch_bounds__(256, 2) void attn_paged_tiles_kernel(const PagedParams p)
+template <int D, typename E, bool E4M3, bool TREE>
+__global__ __launch_bounds__(256, 2) void attn_paged_tiles_kernel(const ParamsOf<TREE> p)
 {
     typedef PagedTilesTiling<D> T;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     PlanSeq seq;
     const Plan plan = plan_call<T::BM>(p, seq);
     for (int k = 0; k * (int)gridDim.x < plan.total; ++k) {
-        const PagedParams again = params_again();
+        const ParamsOf<TREE> again = params_again<TREE>();
         Unit u;
         if (find_unit<T::BM>(again, plan, seq, unit_of_pass(gridDim.x, k), u)) {
             leave_note<T::BM, T::THREADS>(again, u);
-            attn_paged_tiles_unit<D, E>(again, u, smem);
+            attn_paged_tiles_unit<D, E, E4M3, TREE>(again, u, smem);
         }
         __syncthreads();                                    // every wave has read its last tile
-        seq = plan_sequence<T::BM>(params_again(), threadIdx.x & 63);
+        seq = plan_sequence<T::BM>(params_again<TREE>(), threadIdx.x & 63);
     }
 }
 
