@@ -748,3 +748,172 @@ def _marshal_tree(entry, dt, q, k_pages, v_pages, page_table, start, kv_len, mas
     _check_array(mask, torch.int64, (q.shape[0], mask.shape[1]), "mask", q.device)
     return _paged(entry, dt, q, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale, o, lse, workspace, (mask.data_ptr(), mask.shape[1]),
                   (), scale, max_q, stream)
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# What attention looks at, and eviction (include/attn_evict.h)
+
+for _suffix in ("", "_f16"):
+    getattr(_lib, "attn_cache_weigh" + _suffix).restype = _int
+    getattr(_lib, "attn_cache_weigh" + _suffix).argtypes = ([_pointer] * 8 + [_int] + [_pointer] * 4 + [_float] + [_int] * 10
+                                                            + [_float, _pointer])
+_lib.attn_cache_select.restype = _int
+_lib.attn_cache_select.argtypes = [_pointer] * 8 + [_int] * 6 + [_pointer]
+_lib.attn_cache_move.restype = _int
+_lib.attn_cache_move.argtypes = [_pointer] * 7 + [_int] + [_pointer] * 2 + [_int] * 8 + [_pointer]
+
+
+def attn_cache_weigh(q, lse, k_pages, page_table, start, kv_len, weights, k_scale=None, out=None, stamps=None, seen=None, decay=1.0,
+                     causal=True, scale=None, max_q=None, stream=None):
+    """attn_cache_weigh on torch device tensors (include/attn_evict.h): the attention weights of the new tokens' queries, summed for
+    every cached position and key head, added to `decay` times what the position has in `weights`.
+
+    q [T,H_q,D] and lse fp32 [T,H_q]: as attn_paged_fwd took and returned them.  k_pages .. kv_len, k_scale: the cache, as there.
+    weights fp32 [B,H_kv,table_width * page_size], contiguous, or None (nothing is there yet); out: like it, where the sums go
+    (weights itself when not given).  The rows' own positions start from 0.  stamps int32, shaped like weights, with seen
+    int32 [B], the tokens that the sequences have had in all: the rows' own places get their token's number.
+    Asynchronous on `stream`.  Returns out.
+    """
+    import torch
+    return _weigh(_lib.attn_cache_weigh, torch.bfloat16, q, lse, k_pages, page_table, start, kv_len, weights, k_scale, out, stamps,
+                  seen, decay, causal, scale, max_q, stream)
+
+
+def attn_cache_weigh_f16(q, lse, k_pages, page_table, start, kv_len, weights, k_scale=None, out=None, stamps=None, seen=None,
+                         decay=1.0, causal=True, scale=None, max_q=None, stream=None):
+    """attn_cache_weigh_f16 on torch device tensors: as attn_cache_weigh, with fp16 q (and fp16 or e4m3 pages)."""
+    import torch
+    return _weigh(_lib.attn_cache_weigh_f16, torch.float16, q, lse, k_pages, page_table, start, kv_len, weights, k_scale, out, stamps,
+                  seen, decay, causal, scale, max_q, stream)
+
+
+def _weigh(entry, dt, q, lse, k_pages, page_table, start, kv_len, weights, k_scale, out, stamps, seen, decay, causal, scale, max_q,
+           stream):
+    import torch
+
+    _check_rows(q, dt, 3, "q", q.device)
+    T, H_q, D = q.shape
+    # (K alone: its tensors stand for those of V)
+    kind, n_pages, H_kv, page_size, D_cache, B, width = _check_cache(dt, k_pages, k_pages, page_table, start, kv_len, k_scale, k_scale,
+                                                                     q.device)
+    if D != D_cache or H_kv < 1 or H_q % H_kv:
+        raise ValueError("q's heads do not fit the cache's")
+    _check_array(lse, torch.float32, (T, H_q), "lse", q.device)
+    shape = (B, H_kv, width * page_size)
+    out = weights if out is None else out
+    if out is None:
+        raise TypeError("weights or out has to be given")
+    for t, name in ((weights, "weights"), (out, "out")):
+        if t is not None:
+            _check_array(t, torch.float32, shape, name, q.device)
+    if (stamps is None) != (seen is None):
+        raise TypeError("stamps and seen belong together")
+    if stamps is not None:
+        _check_array(stamps, torch.int32, shape, "stamps", q.device)
+        _check_array(seen, torch.int32, (B,), "seen", q.device)
+    if scale is None:
+        scale = 1.0 / float(D) ** 0.5
+    if stream is None:
+        stream = torch.cuda.current_stream(q.device)
+    with torch.cuda.device(q.device):
+        rc = entry(q.data_ptr(), _strides((q, 0), (q, 1)), lse.data_ptr(), k_pages.data_ptr(), _address(k_scale), page_table.data_ptr(),
+                   start.data_ptr(), kv_len.data_ptr(), kind, _address(weights), out.data_ptr(), _address(stamps), _address(seen),
+                   float(decay), T if max_q is None else min(int(max_q), _INT_MAX), T, B, H_q, H_kv, D, n_pages, page_size, width,
+                   int(bool(causal)), float(scale), stream.cuda_stream)
+    if rc != ATTN_OK:
+        raise AttnError(rc)
+    return out
+
+
+def attn_cache_select(weights, kv_len, keep, max_moves, stamps=None, seen=None, sinks=0, recent=0, dst=None, src=None, new_len=None,
+                      stream=None):
+    """attn_cache_select on torch device tensors (include/attn_evict.h): which places of every sequence and key head are kept.
+
+    weights fp32 [B,H_kv,width], kv_len and keep int32 [B]: of a sequence's kv_len places the `keep` ones with the largest weights
+    stay, tokens below number `sinks` and the last `recent` ones before all others.  stamps int32 like weights with seen int32 [B]
+    (attn_cache_weigh): the tokens' numbers, otherwise the places are.  max_moves: the lists' width, at least the smaller of
+    keep and kv_len - keep of every sequence (one for which it is not drops nothing).  dst, src int32 [B,H_kv,max_moves] and
+    new_len int32 [B] are allocated when not given.  Asynchronous on `stream`.  Returns (dst, src, new_len): the
+    moves for attn_cache_move, padded with -1, and the lengths that they leave.
+    """
+    import torch
+
+    if weights.dim() != 3:
+        raise TypeError("weights must be [B, H_kv, width]")
+    B, H_kv, width = weights.shape
+    device = weights.device
+    _check_array(weights, torch.float32, weights.shape, "weights", device)
+    _check_array(kv_len, torch.int32, (B,), "kv_len", device)
+    _check_array(keep, torch.int32, (B,), "keep", device)
+    if (stamps is None) != (seen is None):
+        raise TypeError("stamps and seen belong together")
+    if stamps is not None:
+        _check_array(stamps, torch.int32, weights.shape, "stamps", device)
+        _check_array(seen, torch.int32, (B,), "seen", device)
+    for n, name in ((max_moves, "max_moves"), (sinks, "sinks"), (recent, "recent"), (width, "width")):
+        if not 0 <= n <= _INT_MAX:
+            raise ValueError("%s is out of range" % name)
+    make = lambda *shape: _allocate(lambda: torch.empty(shape, dtype=torch.int32, device=device), device, stream)
+    dst = make(B, H_kv, max_moves) if dst is None else dst
+    src = make(B, H_kv, max_moves) if src is None else src
+    new_len = make(B) if new_len is None else new_len
+    _check_array(dst, torch.int32, (B, H_kv, max_moves), "dst", device)
+    _check_array(src, torch.int32, (B, H_kv, max_moves), "src", device)
+    _check_array(new_len, torch.int32, (B,), "new_len", device)
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    with torch.cuda.device(device):
+        rc = _lib.attn_cache_select(weights.data_ptr(), _address(stamps), _address(seen), kv_len.data_ptr(), keep.data_ptr(),
+                                    dst.data_ptr(), src.data_ptr(), new_len.data_ptr(), int(sinks), int(recent), B, H_kv, width,
+                                    int(max_moves), stream.cuda_stream)
+    if rc != ATTN_OK:
+        raise AttnError(rc)
+    return dst, src, new_len
+
+
+def attn_cache_move(k_pages, v_pages, page_table, dst, src, k_scale=None, v_scale=None, weights=None, stamps=None, stream=None):
+    """attn_cache_move on torch device tensors (include/attn_evict.h): what lies at place src[b,h,e] of sequence b goes to place
+    dst[b,h,e], keys, values and their scales, and weights and stamps ([B,H_kv,table_width * page_size]) if given.
+
+    dst, src int32 [B,H_kv,moves], or [B,1,moves] for all heads alike; elements outside the table move nothing.  In lists of more than
+    128 elements no place may be both source and destination.  An accepted path of a tree of n drafted tokens, token
+    numbers path [B,1,m] ascending: dst = kv_len - n + arange(m), src = kv_len - n + path.
+    Asynchronous on `stream`.  Returns (k_pages, v_pages).
+    """
+    import torch
+
+    if dst.dim() != 3 or page_table.dim() != 2 or k_pages.dim() != 4:
+        raise TypeError("dst must be [B, heads, moves], page_table [B, table_width], k_pages [n_pages, H_kv, page_size, D]")
+    device = k_pages.device
+    dt = k_pages.dtype
+    if dt not in (torch.bfloat16, torch.float16, torch.float8_e4m3fn):
+        raise TypeError("k_pages must be bfloat16, float16 or float8_e4m3fn")
+    kind = ATTN_CACHE_E4M3 if dt == torch.float8_e4m3fn else ATTN_CACHE_16BIT
+    _check_array(k_pages, dt, k_pages.shape, "k_pages", device)
+    _check_array(v_pages, dt, k_pages.shape, "v_pages", device)
+    if kind == ATTN_CACHE_E4M3:
+        if k_scale is None or v_scale is None:
+            raise TypeError("an e4m3 cache needs k_scale and v_scale")
+        _check_array(k_scale, torch.uint8, k_pages.shape[:3], "k_scale", device)
+        _check_array(v_scale, torch.uint8, k_pages.shape[:3], "v_scale", device)
+    elif k_scale is not None or v_scale is not None:
+        raise TypeError("a 16-bit cache has no scales")
+    B, width = page_table.shape
+    n_pages, H_kv, page_size, D = k_pages.shape
+    _check_array(page_table, torch.int32, page_table.shape, "page_table", device)
+    if dst.shape[0] != B or dst.shape[1] not in (1, H_kv) or max(dst.shape) > _INT_MAX:
+        raise ValueError("dst must be [B, H_kv, moves] or [B, 1, moves]")
+    _check_array(dst, torch.int32, dst.shape, "dst", device)
+    _check_array(src, torch.int32, dst.shape, "src", device)
+    for t, dtype, name in ((weights, torch.float32, "weights"), (stamps, torch.int32, "stamps")):
+        if t is not None:
+            _check_array(t, dtype, (B, H_kv, width * page_size), name, device)
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    with torch.cuda.device(device):
+        rc = _lib.attn_cache_move(k_pages.data_ptr(), v_pages.data_ptr(), _address(k_scale), _address(v_scale), page_table.data_ptr(),
+                                  dst.data_ptr(), src.data_ptr(), kind, _address(weights), _address(stamps), dst.shape[1], dst.shape[2],
+                                  B, H_kv, D, n_pages, page_size, width, stream.cuda_stream)
+    if rc != ATTN_OK:
+        raise AttnError(rc)
+    return k_pages, v_pages

@@ -20,7 +20,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = [os.path.join(HERE, "csrc", name) for name in ("attn_fwd.hip", "attn_bwd.hip", "attn_rope.hip", "attn_cache.hip",
-                                                         "attn_paged.hip", "attn_tree.hip")]
+                                                         "attn_paged.hip", "attn_tree.hip", "attn_weigh.hip", "attn_evict.hip")]
 LIB_PATH = os.path.join(HERE, "libmi355attn.so")
 MARSHAL_SOURCE = os.path.join(HERE, "csrc", "marshal.cpp")
 MARSHAL_PATH = os.path.join(HERE, "_marshal.so")

@@ -1,0 +1,287 @@
+// attn_weigh.hip -- attention weights of new tokens, added up for every cached position: kernel and entry points
+// (include/attn_evict.h).
+//
+// S = K Q^T once more, without a second product: exp(S - lse) summed over a position's column of queries.  Every position belongs
+// to one wave, which walks the rows that see it: sums stay in its registers, in a fixed order, and nothing is joined in
+// memory.  For few rows the kernel is a stream of keys; for many the matrix pipe and the exponentials bound it.
+//
+// Products are v_mfma_f32_16x16x32 as in attn_paged_rows.h: lane l has column c = l % 16 (a row of queries) and group g = l / 16,
+// K as A operand as it lies in memory, and S leaves lane (c, g) with keys 4g .. 4g+3 of a 16-key block.  A key's weight is the sum of
+// its register over the columns, which the 16 lanes of a group exchange once, at the end.
+#include <hip/hip_runtime.h>
+
+#include <math.h>
+
+#include "attn_cache.h"
+#include "attn_evict.h"
+#include "attn_fwd.h"
+#include "attn_launch.h"
+#include "attn_paged_rows.h"
+
+namespace attn {
+
+struct WeighParams {
+    CacheParams c;
+    const void *q, *k;
+    const unsigned char *k_scale;
+    const float *lse, *weights;
+    float *out;
+    int *stamps;
+    const int *seen;
+    long long q_st, q_sh;               // strides of q in elements
+    int H_q, G;
+    uint32_t g_mul, g_shift;            // row / G (PagedParams::token_of)
+    int causal;
+    float c_log2, decay;
+
+    __device__ __forceinline__ int token_of(int row) const
+    {
+        return G == 1 ? row : (int)((uint32_t)(((uint64_t)(uint32_t)row * g_mul) >> 32) >> g_shift);
+    }
+};
+
+// Units of a batch in the order of its sequences, KEYS positions of a key head each: block * H_kv + head, the blocks of all
+// sequences that have rows counted through.  A wave asks for ascending units; 64 sequences lie in its lanes.
+template <int KEYS>
+struct WeighUnits {
+    long long before;                   // blocks of the sequences before these 64
+    int base, n, kv, start, upto, all;  // first of them; this lane's rows, positions, first row, blocks up to it; blocks of all 64
+
+    __device__ __forceinline__ void load(const CacheParams &c)
+    {
+        const int b = base + (threadIdx.x & 63);
+        n = kv = start = 0;
+        if (b < c.B)
+            start = c.start_of(b), n = max(c.start_of(b + 1) - start, 0), kv = c.length_of(b);
+        upto = wave_prefix(n > 0 ? (kv + KEYS - 1) / KEYS : 0);
+        all = __builtin_amdgcn_readlane(upto, 63);
+    }
+    __device__ __forceinline__ void begin(const CacheParams &c)
+    {
+        before = 0, base = 0;
+        load(c);
+    }
+    // block `g` of the batch: its sequence and the sequence's rows, and its first position; false: there are no more
+    __device__ __forceinline__ bool find(const CacheParams &c, long long g, int &b, int &rows, int &row0, int &length, int &key0)
+    {
+        while (g >= before + all) {
+            if (c.B - base <= 64)
+                return false;
+            before += all, base += 64;
+            load(c);
+        }
+        const int at = (int)(g - before);
+        const int l = __ffsll(__ballot(upto > at)) - 1;
+        auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+        b = base + l, rows = of(n), row0 = of(start), length = of(kv);
+        key0 = (at - (l ? __builtin_amdgcn_readlane(upto, max(l - 1, 0)) : 0)) * KEYS;
+        return true;
+    }
+};
+
+// x summed over the 16 lanes of a group, in all of them
+__device__ __forceinline__ float sum16(float x)
+{
+    auto across = [](float v, auto ctrl) {
+        return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, 0xf, 0xf, true));
+    };
+    x = across(x, std::integral_constant<int, 0xb1>{});                  // quad_perm 1 0 3 2
+    x = across(x, std::integral_constant<int, 0x4e>{});                  // quad_perm 2 3 0 1
+    x = across(x, std::integral_constant<int, 0x141>{});                 // row_half_mirror
+    return across(x, std::integral_constant<int, 0x140>{});              // row_mirror
+}
+
+constexpr int kWeighKeys = 32;          // of a wave
+constexpr int kWeighGroups = 2048;      // workgroups of a launch, at most: what the chip holds at once
+
+template <int D, typename E, bool E4M3>
+__global__ __launch_bounds__(256) void attn_weigh_rows_kernel(const WeighParams p)
+{
+    constexpr int KEYS = 4 * kWeighKeys, EB = E4M3 ? 1 : 2, ROWB = D * EB, KL = ROWB / 64, KS = D / 32;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c = lane & 15, g = lane >> 4;
+    const int page_mask = (1 << p.c.page_log2) - 1;
+    WeighUnits<KEYS> units;
+    units.begin(p.c);
+    for (long long unit = blockIdx.x;; unit += gridDim.x) {
+        int b, n, row0, kv, key0;
+        const long long block = quotient(unit, p.c.H_kv);
+        const int h = (int)(unit - block * p.c.H_kv);
+        if (!units.find(p.c, block, b, n, row0, kv, key0))
+            return;
+        const int j0 = key0 + wave * kWeighKeys;
+        if (j0 >= kv)
+            continue;
+        // ---- this wave's keys as A operands
+        bool ok[2];
+        u32x4 a[2][KS];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int j = min(j0 + 16 * t, (kv - 1) & ~15);
+            const int id = __builtin_amdgcn_readfirstlane(p.c.page_of(b, j));
+            ok[t] = id >= 0;
+            const size_t row = p.c.page_row(max(id, 0), h) + (j & page_mask);
+            const unsigned char *k = static_cast<const unsigned char *>(p.k) + row * ROWB;
+            Piece<16> x[KL];
+#pragma unroll
+            for (int i = 0; i < KL; ++i)
+                x[i].load(k + c * ROWB + g * 16 + i * 64);
+            const float unit_k = E4M3 ? unit_of(p.k_scale[row + c]) : 1.f;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                if constexpr (E4M3) {
+                    const uint32_t lo = x[s >> 1].d[2 * (s & 1)], hi = x[s >> 1].d[2 * (s & 1) + 1];
+                    a[t][s] = u32x4{E::template from_e4m3<false>(lo, unit_k), E::template from_e4m3<true>(lo, unit_k),
+                                    E::template from_e4m3<false>(hi, unit_k), E::template from_e4m3<true>(hi, unit_k)};
+                } else {
+                    a[t][s] = u32x4{x[s].d[0], x[s].d[1], x[s].d[2], x[s].d[3]};
+                }
+            }
+        }
+        // ---- the rows that see some of them
+        const int n_rows = n * p.G, first_pos = kv - n;
+        const int from = p.causal ? (int)min((long long)max(j0 - first_pos, 0) * p.G, (long long)n_rows) : 0;
+        float w[2][4] = {};
+        for (int r0 = from & ~15; r0 < n_rows; r0 += 16) {
+            const int row = min(r0 + c, n_rows - 1), i = p.token_of(row), hq = h * p.G + row - i * p.G;
+            const typename E::t *src = static_cast<const typename E::t *>(p.q) + (long long)(row0 + i) * p.q_st + (long long)hq * p.q_sh;
+            u32x4 q[KS];
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+                q[s] = *reinterpret_cast<const u32x4 *>(src + (E4M3 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : s * 32 + g * 8));
+            const float lse = p.lse[(size_t)(row0 + i) * p.H_q + hq];
+            const bool sees = r0 + c < n_rows && lse != -INFINITY;
+            const int last = !sees ? -1 : p.causal ? first_pos + i : kv - 1;
+            const float shift = -lse * 1.44269504088896340736f;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                f32x4 s4 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+                    s4 = E::mfma16(a[t][s], q[s], s4);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float e = __builtin_amdgcn_exp2f(fmaf(s4[k], p.c_log2, shift));
+                    w[t][k] += j0 + 16 * t + 4 * g + k <= last ? e : 0.f;
+                }
+            }
+        }
+        // ---- one sum for every key; lane 0 of a group has four
+        const size_t at0 = ((size_t)b * p.c.H_kv + h) * ((size_t)p.c.table_width << p.c.page_log2);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                w[t][k] = ok[t] ? sum16(w[t][k]) : 0.f;
+            if (c != 0)
+                continue;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int j = j0 + 16 * t + 4 * g + k;
+                if (j >= kv)
+                    break;
+                float y = w[t][k];
+                if (j < first_pos && p.weights)
+                    y = fmaf(p.decay, p.weights[at0 + j], y);
+                p.out[at0 + j] = y;
+                if (p.stamps && j >= first_pos)
+                    p.stamps[at0 + j] = p.seen[b] - kv + j;
+            }
+        }
+    }
+}
+
+}  // namespace attn
+
+namespace {
+
+using attn::WeighParams;
+
+bool misaligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
+
+template <int D, typename E, bool E4M3>
+int launch(const WeighParams &p, hipStream_t st)
+{
+    // (no more units than the table holds, and than pages of positions that rows could belong to)
+    const long long blocks = (((long long)p.c.table_width << p.c.page_log2) + 4 * attn::kWeighKeys - 1) / (4 * attn::kWeighKeys);
+    const long long seqs = p.c.B < p.c.T ? p.c.B : p.c.T;
+    const long long most = attn::kWeighGroups, per_seq = blocks < most ? blocks * p.c.H_kv : most;
+    const long long grid = per_seq < most / seqs ? per_seq * seqs : most;
+    hipLaunchKernelGGL((attn::attn_weigh_rows_kernel<D, E, E4M3>), dim3((unsigned)grid), dim3(256), 0, st, p);
+    return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH;
+}
+
+template <typename E>
+int weigh(const void *q, const long long *strides, const float *lse, const void *k_pages, const unsigned char *k_scale,
+          const int *page_table, const int *start, const int *kv_len, int kind, const float *weights, float *weights_out, int *stamps,
+          const int *seen, float decay, int max_q, int T, int B, int H_q, int H_kv, int D, int n_pages, int page_size, int table_width,
+          int causal, float scale, void *stream)
+{
+    if (!q || !strides || !lse || !k_pages || !page_table || !start || !kv_len || !weights_out || !stamps != !seen ||
+        (kind == ATTN_CACHE_E4M3 && !k_scale))
+        return ATTN_ERR_NULL;
+    if (T < 1 || B < 1 || H_q < 1 || H_kv < 1 || H_q % H_kv || n_pages < 1 || table_width < 1 || max_q < 1 || B > attn::kMostSequences)
+        return ATTN_ERR_SHAPE;
+    if (D != 64 && D != 128 && D != 256)
+        return ATTN_ERR_UNSUPPORTED_D;
+    if ((kind != ATTN_CACHE_16BIT && kind != ATTN_CACHE_E4M3) || page_size < 16 || page_size > 256 ||
+        (page_size & (page_size - 1)))
+        return ATTN_ERR_UNSUPPORTED;
+    const long long width = (long long)table_width * page_size;
+    if ((long long)T * H_q > 0x3fffffffLL || (long long)n_pages * H_kv > (1LL << 40) / D / page_size || H_kv > (1 << 24) ||
+        width > (1 << 30) || (long long)H_kv * page_size >= (1 << 30) / D || (long long)B * H_kv > (1LL << 40) / width)
+        return ATTN_ERR_SHAPE;
+    for (int i = 0; i < 2; ++i) {
+        const long long n = i ? H_q : T;
+        if (n > 1 && (strides[i] < 0 || strides[i] % 8 || strides[i] > (1LL << 40) / n))
+            return ATTN_ERR_SHAPE;
+    }
+    const uintptr_t in = (uintptr_t)weights, out = (uintptr_t)weights_out, bytes = (uintptr_t)B * H_kv * width * 4;
+    if (weights && in != out && in < out + bytes && out < in + bytes)
+        return ATTN_ERR_SHAPE;
+    if (misaligned(q, 16) || misaligned(lse, 4) || misaligned(k_pages, 16) || misaligned(page_table, 4) || misaligned(start, 4) ||
+        misaligned(kv_len, 4) || misaligned(weights, 16) || misaligned(weights_out, 16) || misaligned(stamps, 16) ||
+        misaligned(seen, 4) || (kind == ATTN_CACHE_E4M3 && misaligned(k_scale, 16)))
+        return ATTN_ERR_ALIGN;
+    if (!(scale > 0.f) || !(scale < INFINITY) || !(decay >= 0.f) || !(decay < INFINITY))
+        return ATTN_ERR_SCALE;
+    WeighParams p;
+    p.c.page_table = page_table, p.c.start = start, p.c.kv_len = kv_len;
+    p.c.T = T, p.c.B = B, p.c.H_kv = H_kv, p.c.n_pages = n_pages, p.c.table_width = table_width;
+    p.c.page_log2 = __builtin_ctz((unsigned)page_size);
+    p.q = q, p.k = k_pages, p.k_scale = k_scale, p.lse = lse;
+    p.weights = decay == 0.f ? nullptr : weights, p.out = weights_out, p.stamps = stamps, p.seen = seen;
+    p.q_st = strides[0], p.q_sh = strides[1];
+    p.H_q = H_q, p.G = H_q / H_kv;
+    int log_g = 0;                                         // (PagedParams::token_of)
+    while ((1LL << log_g) < p.G)
+        ++log_g;
+    p.g_mul = p.G == 1 ? 0 : (uint32_t)(((1ULL << (31 + log_g)) + p.G - 1) / p.G);
+    p.g_shift = p.G == 1 ? 0 : log_g - 1;
+    p.causal = causal != 0;
+    p.c_log2 = (float)((double)scale * 1.44269504088896340736);
+    p.decay = decay;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const bool e4m3 = kind == ATTN_CACHE_E4M3;
+    switch (D) {
+    case 64: return e4m3 ? launch<64, E, true>(p, st) : launch<64, E, false>(p, st);
+    case 128: return e4m3 ? launch<128, E, true>(p, st) : launch<128, E, false>(p, st);
+    default: return e4m3 ? launch<256, E, true>(p, st) : launch<256, E, false>(p, st);
+    }
+}
+
+}  // namespace
+
+#define ATTN_WEIGH_ENTRY(name, E)                                                                                              \
+    extern "C" int name(const void *q, const long long *strides, const float *lse, const void *k_pages,                        \
+                        const unsigned char *k_scale, const int *page_table, const int *start, const int *kv_len, int kind,    \
+                        const float *weights, float *weights_out, int *stamps, const int *seen, float decay, int max_q, int T, \
+                        int B, int H_q, int H_kv, int D, int n_pages, int page_size, int table_width, int causal, float scale, \
+                        void *stream)                                                                                          \
+    {                                                                                                                          \
+        return weigh<E>(q, strides, lse, k_pages, k_scale, page_table, start, kv_len, kind, weights, weights_out, stamps,      \
+                        seen, decay, max_q, T, B, H_q, H_kv, D, n_pages, page_size, table_width, causal, scale, stream);       \
+    }
+
+ATTN_WEIGH_ENTRY(attn_cache_weigh, attn::PagedBF16)
+ATTN_WEIGH_ENTRY(attn_cache_weigh_f16, attn::PagedF16)
