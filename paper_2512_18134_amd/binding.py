@@ -103,7 +103,7 @@ _marshal_module = None
 
 class _NotBuilt:
     """In place of the extension module: every call is handed back."""
-    fwd = splitkv = bwd = rope = write = read = paged = staticmethod(lambda *args: None)
+    fwd = splitkv = bwd = rope = write = read = paged = tree = weigh = select = move = staticmethod(lambda *args: None)
 
 
 def _native():
@@ -123,6 +123,9 @@ def _native():
         module.set_serving_entries(*(address(getattr(_lib, name + suffix))
                                      for name in ("attn_rope", "attn_cache_write", "attn_cache_read", "attn_paged_fwd")
                                      for suffix in ("", "_f16")), address(_lib.attn_paged_fwd_workspace_bytes))
+        module.set_eviction_entries(*(address(getattr(_lib, name)) for name in
+                                      ("attn_paged_tree", "attn_paged_tree_f16", "attn_cache_weigh", "attn_cache_weigh_f16",
+                                       "attn_cache_select", "attn_cache_move")))
         _marshal_module = module
     return _marshal_module
 
@@ -725,6 +728,10 @@ def attn_paged_tree(q, k_pages, v_pages, page_table, start, kv_len, mask, k_scal
     the sign); what lies in the cache before a sequence's new tokens is seen by all of them.  Everything else is as in
     attn_paged_fwd.  Asynchronous on `stream`.  Returns (o, lse).
     """
+    r = (_marshal_module or _native()).tree(0, q, k_pages, v_pages, page_table, start, kv_len, mask, k_scale, v_scale, o, lse, workspace,
+                                            scale, max_q, stream)
+    if r is not None:
+        return _finish(r)
     import torch
     return _marshal_tree(_lib.attn_paged_tree, torch.bfloat16, q, k_pages, v_pages, page_table, start, kv_len, mask, k_scale, v_scale,
                          o, lse, workspace, scale, max_q, stream)
@@ -733,6 +740,10 @@ def attn_paged_tree(q, k_pages, v_pages, page_table, start, kv_len, mask, k_scal
 def attn_paged_tree_f16(q, k_pages, v_pages, page_table, start, kv_len, mask, k_scale=None, v_scale=None, o=None, lse=None,
                         workspace=None, scale=None, max_q=None, stream=None):
     """attn_paged_tree_f16 on torch device tensors: as attn_paged_tree, with fp16 q and o (and fp16 or e4m3 pages)."""
+    r = (_marshal_module or _native()).tree(1, q, k_pages, v_pages, page_table, start, kv_len, mask, k_scale, v_scale, o, lse, workspace,
+                                            scale, max_q, stream)
+    if r is not None:
+        return _finish(r)
     import torch
     return _marshal_tree(_lib.attn_paged_tree_f16, torch.float16, q, k_pages, v_pages, page_table, start, kv_len, mask, k_scale,
                          v_scale, o, lse, workspace, scale, max_q, stream)
@@ -774,6 +785,10 @@ def attn_cache_weigh(q, lse, k_pages, page_table, start, kv_len, weights, k_scal
     int32 [B], the tokens that the sequences have had in all: the rows' own places get their token's number.
     Asynchronous on `stream`.  Returns out.
     """
+    r = (_marshal_module or _native()).weigh(0, q, lse, k_pages, page_table, start, kv_len, weights, k_scale, out, stamps, seen, decay,
+                                             causal, scale, max_q, stream)
+    if r is not None:
+        return _finish(r)[0]
     import torch
     return _weigh(_lib.attn_cache_weigh, torch.bfloat16, q, lse, k_pages, page_table, start, kv_len, weights, k_scale, out, stamps,
                   seen, decay, causal, scale, max_q, stream)
@@ -782,6 +797,10 @@ def attn_cache_weigh(q, lse, k_pages, page_table, start, kv_len, weights, k_scal
 def attn_cache_weigh_f16(q, lse, k_pages, page_table, start, kv_len, weights, k_scale=None, out=None, stamps=None, seen=None,
                          decay=1.0, causal=True, scale=None, max_q=None, stream=None):
     """attn_cache_weigh_f16 on torch device tensors: as attn_cache_weigh, with fp16 q (and fp16 or e4m3 pages)."""
+    r = (_marshal_module or _native()).weigh(1, q, lse, k_pages, page_table, start, kv_len, weights, k_scale, out, stamps, seen, decay,
+                                             causal, scale, max_q, stream)
+    if r is not None:
+        return _finish(r)[0]
     import torch
     return _weigh(_lib.attn_cache_weigh_f16, torch.float16, q, lse, k_pages, page_table, start, kv_len, weights, k_scale, out, stamps,
                   seen, decay, causal, scale, max_q, stream)
@@ -836,6 +855,9 @@ def attn_cache_select(weights, kv_len, keep, max_moves, stamps=None, seen=None, 
     new_len int32 [B] are allocated when not given.  Asynchronous on `stream`.  Returns (dst, src, new_len): the
     moves for attn_cache_move, padded with -1, and the lengths that they leave.
     """
+    r = (_marshal_module or _native()).select(weights, kv_len, keep, max_moves, stamps, seen, sinks, recent, dst, src, new_len, stream)
+    if r is not None:
+        return _finish(r)
     import torch
 
     if weights.dim() != 3:
@@ -880,6 +902,9 @@ def attn_cache_move(k_pages, v_pages, page_table, dst, src, k_scale=None, v_scal
     numbers path [B,1,m] ascending: dst = kv_len - n + arange(m), src = kv_len - n + path.
     Asynchronous on `stream`.  Returns (k_pages, v_pages).
     """
+    r = (_marshal_module or _native()).move(k_pages, v_pages, page_table, dst, src, k_scale, v_scale, weights, stamps, stream)
+    if r is not None:
+        return _finish(r)
     import torch
 
     if dst.dim() != 3 or page_table.dim() != 2 or k_pages.dim() != 4:

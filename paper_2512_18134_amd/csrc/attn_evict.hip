@@ -35,12 +35,27 @@ __device__ __forceinline__ uint32_t rank_of(float x)
 }
 constexpr uint32_t kAlways = 0xffffffffu;                   // above the rank of +infinity
 
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
+typedef __attribute__((ext_vector_type(4))) int i32x4;
 
-__global__ __launch_bounds__(kSelectThreads) void attn_select_kernel(const SelectParams p)
+// THREADS of a workgroup; HELD: ranks stay in registers from the first reading on, in so many vectors of four to a thread (a list of up to
+// THREADS * 4 * HELD places), 0: every pass reads anew, which the L2 serves.
+template <int THREADS, int HELD>
+struct SelectTiling {
+    static constexpr int DIGIT = THREADS == 256 ? 11 : 12;  // bits of the first digit; the second one has half of the rest
+    static constexpr int BINS = 1 << DIGIT, WAVES = THREADS / 64;
+    static constexpr int STRIDE = THREADS * 4;              // places of a vector of all threads
+    static constexpr int SEGMENT = HELD ? STRIDE * HELD : 131072;     // places whose outcome lies in LDS at once, bit by bit
+};
+
+template <int THREADS, int HELD>
+__global__ __launch_bounds__(THREADS) void attn_select_kernel(const SelectParams p)
 {
-    __shared__ int count[2048];
-    __shared__ int wave_sum_lds[3][kSelectWaves];
+    typedef SelectTiling<THREADS, HELD> T;
+    constexpr int WAVES = T::WAVES;
+    __shared__ __attribute__((aligned(16))) int count[T::BINS];
+    // of every 256 places four words: bit l of word k is place 4 l + k, kept in any case and as one of the last rank
+    __shared__ unsigned long long above[T::SEGMENT / 64], equal[T::SEGMENT / 64];
+    __shared__ int of_wave[3][WAVES];
     __shared__ int found[2];                                // digit, how many are to be kept of its elements
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int b = quotient((int)blockIdx.x, p.H_kv), h = blockIdx.x - b * p.H_kv;
@@ -50,97 +65,190 @@ __global__ __launch_bounds__(kSelectThreads) void attn_select_kernel(const Selec
     const bool whole = min(keep, kv - keep) > p.moves;      // more moves than the lists may hold
     if (h == 0 && tid == 0)
         p.new_len[b] = whole ? kv : keep;
-    int n_moves = 0;
+    int at_dst = 0, at_src = 0;
     if (!whole && keep > 0 && keep < kv) {
         const float *const weights = p.weights + row * p.width;
         const int *const stamps = p.stamps ? p.stamps + row * p.width : nullptr;
-        const int seen = p.stamps ? p.seen[b] : kv;
-        const long long late = (long long)seen - p.recent;
-        auto rank = [&](int j) -> uint32_t {
-            const int stamp = stamps ? stamps[j] : j;
-            return stamp < p.sinks || stamp >= late ? kAlways : rank_of(weights[j]);
+        const long long late = (long long)(p.stamps ? p.seen[b] : kv) - p.recent;
+        // four ranks from place j on (a multiple of four; the rows end on one)
+        auto read = [&](int j) -> u32x4 {
+            const f32x4 w = *reinterpret_cast<const f32x4 *>(weights + j);
+            i32x4 number = {j, j + 1, j + 2, j + 3};
+            if (stamps)
+                number = *reinterpret_cast<const i32x4 *>(stamps + j);
+            u32x4 r;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                r[k] = number[k] < p.sinks || number[k] >= late ? kAlways : rank_of(w[k]);
+            return r;
         };
-        // ---- the keep-th largest rank: its leading bits, and how many of those that have them are kept
+        u32x4 held[HELD ? HELD : 1];
+        if constexpr (HELD != 0) {
+#pragma unroll
+            for (int i = 0; i < HELD; ++i)
+                if (i * T::STRIDE < kv) {
+                    const int j = i * T::STRIDE + 4 * tid;
+                    if (j < kv)
+                        held[i] = read(j);
+                }
+        }
+        // f(first place of the lane's four, their ranks) for the places from `from` to `upto`; lanes behind kv take part
+        auto each = [&](int from, int upto, auto f) {
+            if constexpr (HELD != 0) {
+#pragma unroll
+                for (int i = 0; i < HELD; ++i)
+                    if (i * T::STRIDE < kv)
+                        f(i * T::STRIDE + 4 * tid, held[i]);
+            } else {
+                constexpr int U = 4;
+                for (int j0 = from + 4 * tid; j0 - 4 * tid < upto; j0 += U * T::STRIDE) {
+                    u32x4 r[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+                        r[u] = read(min(j0 + u * T::STRIDE, (kv - 1) & ~3));
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+                        if (j0 - 4 * tid + u * T::STRIDE < upto)
+                            f(j0 + u * T::STRIDE, r[u]);
+                }
+            }
+        };
+        // ---- the keep-th largest rank, digit by digit: its leading bits, and how many of those that have them are kept
         uint32_t top = 0;
-        int left = keep;
+        int left = keep, shift = 32;
 #pragma unroll 1
         for (int pass = 0; pass < 3; ++pass) {
-            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-            const uint32_t above = pass == 0 ? 0u : ~0u << (shift + bits);    // bits that are known
-            for (int i = tid; i < 2048; i += kSelectThreads)
-                count[i] = 0;
+            const int bits = pass == 0 ? T::DIGIT : pass == 1 ? (33 - T::DIGIT) / 2 : (32 - T::DIGIT) / 2;
+            const uint32_t known = pass == 0 ? 0u : ~0u << shift;
+            shift -= bits;
+            for (int i = tid; i < T::BINS / 4; i += THREADS)
+                reinterpret_cast<i32x4 *>(count)[i] = i32x4{0, 0, 0, 0};
             __syncthreads();
-            for (int j = tid; j < kv; j += kSelectThreads) {
-                const uint32_t r = rank(j);
-                if ((r & above) == top)
-                    atomicAdd(&count[r >> shift & ((1 << bits) - 1)], 1);
-            }
+            each(0, kv, [&](int j, u32x4 r) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const bool mine = j + k < kv && (r[k] & known) == top;
+                    const int digit = r[k] >> shift & ((1 << bits) - 1);
+                    // the first lane counts for all that have its digit: one value may be everywhere
+                    const unsigned long long with = __ballot(mine);
+                    if (with == 0)
+                        continue;
+                    const int lead = __ffsll(with) - 1;
+                    const bool same = mine && digit == __builtin_amdgcn_readlane(digit, lead);
+                    const unsigned long long all = __ballot(same);
+                    if (mine && (!same || lane == lead))
+                        atomicAdd(&count[digit], same ? __popcll(all) : 1);
+                }
+            });
             __syncthreads();
-            // from the largest digit down: thread t has digits 2047 - 2t and 2046 - 2t
-            const int c0 = count[2047 - 2 * tid], c1 = count[2046 - 2 * tid];
-            const int upto = wave_prefix(c0 + c1);
+            // from the largest digit down, PER neighbouring ones to a thread
+            constexpr int PER = T::BINS / THREADS;
+            const int first = T::BINS - (tid + 1) * PER;
+            int mine = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                mine += count[first + i];
+            const int upto = wave_prefix(mine);
             if (lane == 63)
-                wave_sum_lds[0][wave] = upto;
+                of_wave[0][wave] = upto;
             __syncthreads();
-            int before = upto - c0 - c1;
+            int before = upto - mine;
             for (int w = 0; w < wave; ++w)
-                before += wave_sum_lds[0][w];
-            if (before < left && left <= before + c0 + c1) {
-                const bool second = left > before + c0;
-                found[0] = 2047 - 2 * tid - second;
-                found[1] = left - before - (second ? c0 : 0);
+                before += of_wave[0][w];
+            if (before < left && left <= before + mine) {
+                int digit = first + PER - 1;
+                while (before + count[digit] < left)
+                    before += count[digit--];
+                found[0] = digit, found[1] = left - before;
             }
             __syncthreads();
             top |= (uint32_t)found[0] << shift;
             left = found[1];
-            __syncthreads();
+            __syncthreads();                                // (before anything of it is written again)
         }
-        // ---- kept: above `top`, and the first `left` of those that equal it.  A wave has a stretch of places
-        const int stretch = ((kv + kSelectWaves - 1) / kSelectWaves + 63) & ~63;
-        const int first = min(wave * stretch, kv), behind = min(first + stretch, kv);
-        auto sum_before = [&](int x, int k) {               // of the waves before this one
-            if (lane == 0)
-                wave_sum_lds[k][wave] = x;
+        // ---- kept: above `top`, and the first `left` of those that equal it; a segment at a time
+        for (int seg = 0; seg < kv; seg += T::SEGMENT) {
+            const int n = min(kv - seg, T::SEGMENT), blocks = (n + 255) / 256;
+            each(seg, seg + n, [&](int j, u32x4 r) {
+                const int at = (j - seg) / 256 * 4;         // (a wave's 256 places are a block)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const unsigned long long more = __ballot(j + k < kv && r[k] > top), same = __ballot(j + k < kv && r[k] == top);
+                    if (lane == k && at < 4 * blocks)
+                        above[at + k] = more, equal[at + k] = same;
+                }
+            });
             __syncthreads();
-            int s = 0;
-            for (int w = 0; w < wave; ++w)
-                s += wave_sum_lds[k][w];
-            return s;
-        };
-        int equal = 0;
-        for (int j = first; j < behind; j += 64)
-            equal += __popcll(__ballot(j + lane < behind && rank(j + lane) == top));
-        equal = sum_before(equal, 0);
-        const unsigned long long lower = (1ull << lane) - 1;
-        auto walk = [&](auto f) {                           // f(place, is a free place before the end, is a kept one behind it)
-            int e = equal;
-            for (int j = first; j < behind; j += 64) {
-                const bool there = j + lane < behind;
-                const uint32_t r = there ? rank(j + lane) : 0u;
-                const unsigned long long same = __ballot(there && r == top);
-                const bool kept = there && (r > top || (r == top && e + __popcll(same & lower) < left));
-                e += __popcll(same);
-                f(j + lane, there && !kept && j + lane < keep, kept && j + lane >= keep);
+            // a wave has a stretch of blocks
+            const int stretch = (blocks + WAVES - 1) / WAVES;
+            const int first = min(wave * stretch, blocks), behind = min(first + stretch, blocks);
+            auto join = [&](int x, int k, int &all) {       // of the waves before this one, and of all
+                if (lane == 0)
+                    of_wave[k][wave] = x;
+                __syncthreads();
+                int s = 0;
+                all = 0;
+                for (int w = 0; w < WAVES; ++w) {
+                    s += w < wave ? of_wave[k][w] : 0;
+                    all += of_wave[k][w];
+                }
+                return s;
+            };
+            int same = 0, all_same, all_holes, all_movers;
+            for (int i = 4 * first + lane; i - lane < 4 * behind; i += 64)
+                same += wave_sum(i < 4 * behind ? __popcll(equal[i]) : 0);
+            int e = join(same, 0, all_same);
+            // what is kept of the last rank joins the others; free places before the end and kept ones behind it are counted
+            int holes = 0, movers = 0;
+            auto lower = [&](unsigned long long x) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(x >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)x, 0u)); };
+            for (int i = first; i < behind; ++i) {
+                unsigned long long m[4], q[4];
+                int rank = e;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    m[k] = above[4 * i + k], q[k] = equal[4 * i + k];
+                    rank += lower(q[k]);
+                    e += __popcll(q[k]);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const bool mine = q[k] >> lane & 1;
+                    m[k] |= __ballot(mine && rank < left);
+                    rank += mine;
+                    if (lane == k)
+                        above[4 * i + k] = m[k];
+                    const int j = seg + 256 * i + 4 * lane + k;
+                    const bool kept = m[k] >> lane & 1;
+                    holes += __popcll(__ballot(!kept && j < keep));
+                    movers += __popcll(__ballot(kept && j >= keep));
+                }
             }
-        };
-        int gives = 0, takes = 0;
-        walk([&](int, bool hole, bool mover) {
-            takes += __popcll(__ballot(hole));
-            gives += __popcll(__ballot(mover));
-        });
-        int at_dst = sum_before(takes, 1), at_src = sum_before(gives, 2);
-        for (int w = 0; w < kSelectWaves; ++w)
-            n_moves += wave_sum_lds[1][w];
-        walk([&](int j, bool hole, bool mover) {
-            const unsigned long long holes = __ballot(hole), movers = __ballot(mover);
-            if (hole)
-                dst[at_dst + __popcll(holes & lower)] = j;
-            if (mover)
-                src[at_src + __popcll(movers & lower)] = j;
-            at_dst += __popcll(holes), at_src += __popcll(movers);
-        });
+            int d = at_dst + join(holes, 1, all_holes), s = at_src + join(movers, 2, all_movers);
+            for (int i = first; i < behind; ++i) {
+                const int j = seg + 256 * i + 4 * lane;
+                bool hole[4], mover[4];
+                int to = d, from = s;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const bool kept = above[4 * i + k] >> lane & 1;
+                    hole[k] = !kept && j + k < keep, mover[k] = kept && j + k >= keep;
+                    const unsigned long long x = __ballot(hole[k]), y = __ballot(mover[k]);
+                    to += lower(x), from += lower(y);
+                    d += __popcll(x), s += __popcll(y);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (hole[k])
+                        dst[to++] = j + k;
+                    if (mover[k])
+                        src[from++] = j + k;
+                }
+            }
+            at_dst += all_holes, at_src += all_movers, left -= min(left, all_same);
+            __syncthreads();                                // the segment's words have been read
+        }
     }
-    for (int i = n_moves + tid; i < p.moves; i += kSelectThreads)
+    for (int i = at_dst + tid; i < p.moves; i += THREADS)
         dst[i] = src[i] = -1;
 }
 
@@ -269,8 +377,14 @@ extern "C" int attn_cache_select(const float *weights, const int *stamps, const 
     p.weights = weights, p.stamps = stamps, p.seen = seen, p.kv_len = kv_len, p.keep = keep;
     p.dst = dst, p.src = src, p.new_len = new_len;
     p.sinks = sinks, p.recent = recent, p.B = B, p.H_kv = H_kv, p.width = width, p.moves = moves_width;
-    hipLaunchKernelGGL(attn::attn_select_kernel, dim3((unsigned)(B * H_kv)), dim3(attn::kSelectThreads), 0,
-                       static_cast<hipStream_t>(stream), p);
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const dim3 grid((unsigned)(B * H_kv));
+    if (width <= attn::SelectTiling<256, 8>::SEGMENT)
+        hipLaunchKernelGGL((attn::attn_select_kernel<256, 8>), grid, dim3(256), 0, st, p);
+    else if (width <= attn::SelectTiling<1024, 8>::SEGMENT)
+        hipLaunchKernelGGL((attn::attn_select_kernel<1024, 8>), grid, dim3(1024), 0, st, p);
+    else
+        hipLaunchKernelGGL((attn::attn_select_kernel<1024, 0>), grid, dim3(1024), 0, st, p);
     return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH;
 }
 

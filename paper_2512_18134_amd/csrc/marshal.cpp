@@ -551,6 +551,238 @@ PyObject *py_paged(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- trees of drafted tokens, and eviction
+
+typedef int (*TreeFn)(const void *, const long long *, void *, float *, const void *, const void *, const unsigned char *,
+                      const unsigned char *, const int *, const int *, const int *, int, const unsigned long long *, int, void *,
+                      long long, int, int, int, int, int, int, int, int, int, float, void *);
+typedef int (*WeighFn)(const void *, const long long *, const float *, const void *, const unsigned char *, const int *, const int *,
+                       const int *, int, const float *, float *, int *, const int *, float, int, int, int, int, int, int, int, int,
+                       int, int, float, void *);
+typedef int (*SelectFn)(const float *, const int *, const int *, const int *, const int *, int *, int *, int *, int, int, int, int,
+                        int, int, void *);
+typedef int (*MoveFn)(void *, void *, unsigned char *, unsigned char *, const int *, const int *, const int *, int, float *, int *,
+                      int, int, int, int, int, int, int, int, void *);
+
+TreeFn g_tree[2];
+WeighFn g_weigh[2];
+SelectFn g_select;
+MoveFn g_move;
+
+// tree(type, q, k_pages, v_pages, page_table, start, kv_len, mask, k_scale, v_scale, o, lse, workspace, scale, max_q, stream)
+// -> (o, lse)
+PyObject *py_tree(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const int type = n == 16 ? type_of(a[0]) : 0;
+    Cache c;
+    void *stream;
+    float scale;
+    at::Tensor o, lse, ws;
+    if (n != 16 || !g_tree[type] || !g_paged_ws || !cache_of(a + 2, a[8], a[9], kElem[type], c) || !scale_of(a[13], c.D, scale))
+        Py_RETURN_NONE;
+    const at::Tensor *q = rows_of(a[1], kElem[type], 3), *mask = plain(a[7], at::kLong, 2);
+    if (!q || !mask || q->device() != c.k->device() || mask->device() != q->device() || q->size(2) != c.D || q->size(1) % c.H_kv ||
+        mask->size(0) != q->size(0) || mask->size(1) < 1 || mask->size(1) > INT_MAX ||
+        !stream_of(a[15], c.k->device(), any_none(a + 10, 3), stream))
+        Py_RETURN_NONE;
+    const int T = (int)q->size(0), H_q = (int)q->size(1);
+    int max_q = T;
+    if (a[14] != Py_None && !int_of(a[14], max_q))
+        Py_RETURN_NONE;
+    const long long need = g_paged_ws(T, c.B, H_q, c.H_kv, c.D);
+    if (need < 1)
+        Py_RETURN_NONE;
+    if (a[12] != Py_None) {
+        if (!THPVariable_CheckExact(a[12]))
+            Py_RETURN_NONE;
+        ws = THPVariable_Unpack(a[12]);
+        if (!plain(a[12], ws.scalar_type(), 0) || ws.device() != q->device())
+            Py_RETURN_NONE;
+    }
+    const int64_t o_shape[3] = {T, H_q, c.D}, lse_shape[2] = {T, H_q};
+    if (!rows_output(a[10], *q, o_shape, kElem[type], o) || !o.is_contiguous() ||
+        !rows_output(a[11], *q, lse_shape, at::kFloat, lse) || !lse.is_contiguous())
+        Py_RETURN_NONE;
+    if (!ws.defined())
+        ws = allocate([&] { return at::empty({need}, q->options().dtype(at::kByte)); });
+    const long long strides[2] = {stride_of(*q, 0), stride_of(*q, 1)};
+    const int rc = launch(q->device(), [&] {
+        return g_tree[type](q->data_ptr(), strides, o.data_ptr(), (float *)lse.data_ptr(), c.k->data_ptr(), c.v->data_ptr(),
+                            c.k_scale, c.v_scale, (const int *)c.table->data_ptr(), (const int *)c.start->data_ptr(),
+                            (const int *)c.kv_len->data_ptr(), c.kind, (const unsigned long long *)mask->data_ptr(),
+                            (int)mask->size(1), ws.data_ptr(), (long long)ws.nbytes(), max_q, T, c.B, H_q, c.H_kv, c.D, c.n_pages,
+                            c.page, c.width, scale, stream);
+    });
+    return rc ? PyLong_FromLong(rc) : pack({&o, &lse});
+    END_HANDLE_TH_ERRORS
+}
+
+// an array of this type and shape on the device, or (optional) None, whose address is then NULL; false: it is neither
+template <typename T>
+bool array_or_none(PyObject *o, at::ScalarType type, at::IntArrayRef shape, const c10::Device &dev, bool optional, T *&address)
+{
+    address = nullptr;
+    if (o == Py_None)
+        return optional;
+    const at::Tensor *t = plain(o, type, (int64_t)shape.size());
+    if (!t || t->sizes() != shape || t->device() != dev)
+        return false;
+    address = (T *)t->data_ptr();
+    return true;
+}
+
+// a Python number as it is written (no other object is asked)
+bool number_of(PyObject *o, float &x)
+{
+    if (!PyFloat_CheckExact(o))
+        return false;
+    x = (float)PyFloat_AS_DOUBLE(o);
+    return true;
+}
+
+// weigh(type, q, lse, k_pages, page_table, start, kv_len, weights, k_scale, out, stamps, seen, decay, causal, scale, max_q, stream)
+// -> (out,)
+PyObject *py_weigh(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const int type = n == 17 ? type_of(a[0]) : 0, causal = n == 17 ? truth(a[13]) : -1;
+    Cache c;
+    void *stream;
+    float scale, decay;
+    if (n != 17 || causal < 0 || !g_weigh[type])
+        Py_RETURN_NONE;
+    PyObject *const cache[5] = {a[3], a[3], a[4], a[5], a[6]};             // (K alone: it stands for V)
+    if (!cache_of(cache, a[8], a[8], kElem[type], c) || !scale_of(a[14], c.D, scale) || !number_of(a[12], decay))
+        Py_RETURN_NONE;
+    const at::Tensor *q = rows_of(a[1], kElem[type], 3);
+    if (!q || q->device() != c.k->device() || q->size(2) != c.D || q->size(1) % c.H_kv ||
+        !stream_of(a[16], c.k->device(), false, stream))
+        Py_RETURN_NONE;
+    const int T = (int)q->size(0), H_q = (int)q->size(1);
+    int max_q = T;
+    if (a[15] != Py_None && !int_of(a[15], max_q))
+        Py_RETURN_NONE;
+    PyObject *const to = a[9] == Py_None ? a[7] : a[9];
+    const int64_t shape[3] = {c.B, c.H_kv, (int64_t)c.width * c.page}, rows[2] = {T, H_q}, seqs[1] = {c.B};
+    const c10::Device dev = q->device();
+    float *lse, *weights, *out;
+    int *stamps, *seen;
+    if (!array_or_none(a[2], at::kFloat, rows, dev, false, lse) || !array_or_none(a[7], at::kFloat, shape, dev, true, weights) ||
+        !array_or_none(to, at::kFloat, shape, dev, false, out) || !array_or_none(a[10], at::kInt, shape, dev, true, stamps) ||
+        !array_or_none(a[11], at::kInt, seqs, dev, true, seen) || !stamps != !seen)
+        Py_RETURN_NONE;
+    const long long strides[2] = {stride_of(*q, 0), stride_of(*q, 1)};
+    const int rc = launch(dev, [&] {
+        return g_weigh[type](q->data_ptr(), strides, lse, c.k->data_ptr(), c.k_scale, (const int *)c.table->data_ptr(),
+                             (const int *)c.start->data_ptr(), (const int *)c.kv_len->data_ptr(), c.kind, weights, out, stamps, seen,
+                             decay, max_q, T, c.B, H_q, c.H_kv, c.D, c.n_pages, c.page, c.width, causal, scale, stream);
+    });
+    return rc ? PyLong_FromLong(rc) : PyTuple_Pack(1, to);
+    END_HANDLE_TH_ERRORS
+}
+
+bool int_output(PyObject *given, at::IntArrayRef shape, const at::Tensor &like, at::Tensor &out)
+{
+    if (given == Py_None) {
+        out = allocate([&] { return at::empty(shape, like.options().dtype(at::kInt)); });
+        return true;
+    }
+    const at::Tensor *t = plain(given, at::kInt, (int64_t)shape.size());
+    if (!t || t->sizes() != shape || t->device() != like.device())
+        return false;
+    out = *t;
+    return true;
+}
+
+// select(weights, kv_len, keep, max_moves, stamps, seen, sinks, recent, dst, src, new_len, stream) -> (dst, src, new_len)
+PyObject *py_select(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    const at::Tensor *w = n == 12 ? plain(a[0], at::kFloat, 3) : nullptr;
+    int moves, sinks, recent;
+    void *stream;
+    if (!w || !g_select || !int_of(a[3], moves) || !int_of(a[6], sinks) || !int_of(a[7], recent) || moves < 1 ||
+        !stream_of(a[11], w->device(), any_none(a + 8, 3), stream))
+        Py_RETURN_NONE;
+    const int64_t B = w->size(0), H = w->size(1), width = w->size(2);
+    if (B < 1 || H < 1 || width < 1 || B > INT_MAX || H > INT_MAX || width > INT_MAX)
+        Py_RETURN_NONE;
+    const int64_t seqs[1] = {B}, lists[3] = {B, H, moves};
+    const c10::Device dev = w->device();
+    int *kv_len, *keep, *stamps, *seen;
+    at::Tensor dst, src, len;
+    if (!array_or_none(a[1], at::kInt, seqs, dev, false, kv_len) || !array_or_none(a[2], at::kInt, seqs, dev, false, keep) ||
+        !array_or_none(a[4], at::kInt, w->sizes(), dev, true, stamps) || !array_or_none(a[5], at::kInt, seqs, dev, true, seen) ||
+        !stamps != !seen || !int_output(a[8], lists, *w, dst) || !int_output(a[9], lists, *w, src) || !int_output(a[10], seqs, *w, len))
+        Py_RETURN_NONE;
+    const int rc = launch(dev, [&] {
+        return g_select((const float *)w->data_ptr(), stamps, seen, kv_len, keep, (int *)dst.data_ptr(), (int *)src.data_ptr(),
+                        (int *)len.data_ptr(), sinks, recent, (int)B, (int)H, (int)width, moves, stream);
+    });
+    return rc ? PyLong_FromLong(rc) : pack({&dst, &src, &len});
+    END_HANDLE_TH_ERRORS
+}
+
+// move(k_pages, v_pages, page_table, dst, src, k_scale, v_scale, weights, stamps, stream) -> (k_pages, v_pages)
+PyObject *py_move(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 10 || !g_move || !THPVariable_CheckExact(a[0]))
+        Py_RETURN_NONE;
+    const at::ScalarType elem = THPVariable_Unpack(a[0]).scalar_type();
+    const bool e4m3 = elem == at::kFloat8_e4m3fn;
+    if (!e4m3 && elem != at::kBFloat16 && elem != at::kHalf)
+        Py_RETURN_NONE;
+    const at::Tensor *k = plain(a[0], elem, 4), *v = plain(a[1], elem, 4), *table = plain(a[2], at::kInt, 2), *dst = plain(a[3], at::kInt, 3);
+    void *stream;
+    if (!k || !v || !table || !dst || !same_shape(*k, *v) || table->device() != k->device() || dst->device() != k->device() ||
+        !stream_of(a[9], k->device(), false, stream))
+        Py_RETURN_NONE;
+    const auto s = k->sizes(), t = table->sizes(), d = dst->sizes();
+    for (int i = 0; i < 4; ++i)
+        if (s[i] < 1 || s[i] > INT_MAX)
+            Py_RETURN_NONE;
+    if (t[0] < 1 || t[0] > INT_MAX || t[1] < 1 || t[1] > INT_MAX || d[0] != t[0] || (d[1] != 1 && d[1] != s[1]) || d[2] < 1 || d[2] > INT_MAX)
+        Py_RETURN_NONE;
+    const c10::Device dev = k->device();
+    const int64_t rows[3] = {t[0], s[1], t[1] * s[2]};
+    unsigned char *k_scale, *v_scale;
+    float *weights;
+    int *src, *stamps;
+    if (!array_or_none(a[4], at::kInt, d, dev, false, src) || !array_or_none(a[5], at::kByte, s.slice(0, 3), dev, !e4m3, k_scale) ||
+        !array_or_none(a[6], at::kByte, s.slice(0, 3), dev, !e4m3, v_scale) || (!e4m3 && (k_scale || v_scale)) ||
+        !array_or_none(a[7], at::kFloat, rows, dev, true, weights) || !array_or_none(a[8], at::kInt, rows, dev, true, stamps))
+        Py_RETURN_NONE;
+    const int rc = launch(dev, [&] {
+        return g_move(k->data_ptr(), v->data_ptr(), k_scale, v_scale, (const int *)table->data_ptr(), (const int *)dst->data_ptr(), src,
+                      e4m3, weights, stamps, (int)d[1], (int)d[2], (int)t[0], (int)s[1], (int)s[3], (int)s[0], (int)s[2], (int)t[1], stream);
+    });
+    return rc ? PyLong_FromLong(rc) : PyTuple_Pack(2, a[0], a[1]);
+    END_HANDLE_TH_ERRORS
+}
+
+// set_eviction_entries(addresses of paged_tree and cache_weigh, bf16 and fp16 of each, cache_select and cache_move)
+PyObject *py_set_eviction_entries(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    void *p[6];
+    if (n != 6) {
+        PyErr_SetString(PyExc_TypeError, "set_eviction_entries takes six addresses");
+        return nullptr;
+    }
+    for (int i = 0; i < 6; ++i)
+        p[i] = PyLong_AsVoidPtr(a[i]);
+    if (PyErr_Occurred())
+        return nullptr;
+    for (int i = 0; i < 2; ++i) {
+        g_tree[i] = (TreeFn)p[i];
+        g_weigh[i] = (WeighFn)p[2 + i];
+    }
+    g_select = (SelectFn)p[4];
+    g_move = (MoveFn)p[5];
+    Py_RETURN_NONE;
+}
+
 // set_serving_entries(addresses of rope, cache_write, cache_read and paged_fwd, bf16 and fp16 of each, and of the last one's
 // workspace size)
 PyObject *py_set_serving_entries(PyObject *, PyObject *const *a, Py_ssize_t n)
@@ -606,6 +838,11 @@ PyMethodDef kMethods[] = {
     {"write", (PyCFunction)(void (*)(void))py_write, METH_FASTCALL, nullptr},
     {"read", (PyCFunction)(void (*)(void))py_read, METH_FASTCALL, nullptr},
     {"paged", (PyCFunction)(void (*)(void))py_paged, METH_FASTCALL, nullptr},
+    {"tree", (PyCFunction)(void (*)(void))py_tree, METH_FASTCALL, nullptr},
+    {"weigh", (PyCFunction)(void (*)(void))py_weigh, METH_FASTCALL, nullptr},
+    {"select", (PyCFunction)(void (*)(void))py_select, METH_FASTCALL, nullptr},
+    {"move", (PyCFunction)(void (*)(void))py_move, METH_FASTCALL, nullptr},
+    {"set_eviction_entries", (PyCFunction)(void (*)(void))py_set_eviction_entries, METH_FASTCALL, nullptr},
     {"set_serving_entries", (PyCFunction)(void (*)(void))py_set_serving_entries, METH_FASTCALL, nullptr},
     {"set_entries", (PyCFunction)(void (*)(void))py_set_entries, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
