@@ -16,7 +16,7 @@
 #include "attn_evict.h"
 #include "attn_fwd.h"
 #include "attn_launch.h"
-#include "attn_paged_rows.h"
+#include "attn_paged_tiles.h"
 
 namespace attn {
 
@@ -40,11 +40,11 @@ struct WeighParams {
     }
 };
 
-// Units of a batch in the order of its sequences, KEYS positions of a key head each: block * H_kv + head, the blocks of all
+// Units of a batch in the order of its sequences, 2^log2_keys positions of a key head each: block * H_kv + head, the blocks of all
 // sequences that have rows counted through.  A wave asks for ascending units; 64 sequences lie in its lanes.
-template <int KEYS>
 struct WeighUnits {
     long long before;                   // blocks of the sequences before these 64
+    int log2_keys;
     int base, n, kv, start, upto, all;  // first of them; this lane's rows, positions, first row, blocks up to it; blocks of all 64
 
     __device__ __forceinline__ void load(const CacheParams &c)
@@ -53,12 +53,12 @@ struct WeighUnits {
         n = kv = start = 0;
         if (b < c.B)
             start = c.start_of(b), n = max(c.start_of(b + 1) - start, 0), kv = c.length_of(b);
-        upto = wave_prefix(n > 0 ? (kv + KEYS - 1) / KEYS : 0);
+        upto = wave_prefix(n > 0 ? (kv + (1 << log2_keys) - 1) >> log2_keys : 0);
         all = __builtin_amdgcn_readlane(upto, 63);
     }
-    __device__ __forceinline__ void begin(const CacheParams &c)
+    __device__ __forceinline__ void begin(const CacheParams &c, int log2)
     {
-        before = 0, base = 0;
+        before = 0, base = 0, log2_keys = log2;
         load(c);
     }
     // block `g` of the batch: its sequence and the sequence's rows, and its first position; false: there are no more
@@ -74,7 +74,7 @@ struct WeighUnits {
         const int l = __ffsll(__ballot(upto > at)) - 1;
         auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
         b = base + l, rows = of(n), row0 = of(start), length = of(kv);
-        key0 = (at - (l ? __builtin_amdgcn_readlane(upto, max(l - 1, 0)) : 0)) * KEYS;
+        key0 = (at - (l ? __builtin_amdgcn_readlane(upto, max(l - 1, 0)) : 0)) << log2_keys;
         return true;
     }
 };
@@ -101,8 +101,8 @@ __global__ __launch_bounds__(256) void attn_weigh_rows_kernel(const WeighParams 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, g = lane >> 4;
     const int page_mask = (1 << p.c.page_log2) - 1;
-    WeighUnits<KEYS> units;
-    units.begin(p.c);
+    WeighUnits units;
+    units.begin(p.c, __builtin_ctz(KEYS));
     for (long long unit = blockIdx.x;; unit += gridDim.x) {
         int b, n, row0, kv, key0;
         const long long block = quotient(unit, p.c.H_kv);
@@ -150,21 +150,29 @@ __global__ __launch_bounds__(256) void attn_weigh_rows_kernel(const WeighParams 
             for (int s = 0; s < KS; ++s)
                 q[s] = *reinterpret_cast<const u32x4 *>(src + (E4M3 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : s * 32 + g * 8));
             const float lse = p.lse[(size_t)(row0 + i) * p.H_q + hq];
-            const bool sees = r0 + c < n_rows && lse != -INFINITY;
-            const int last = !sees ? -1 : p.causal ? first_pos + i : kv - 1;
-            const float shift = -lse * 1.44269504088896340736f;
+            // (a row that sees nothing, or is none: exp2(-inf))
+            const float shift = r0 + c < n_rows && lse != -INFINITY ? -lse * 1.44269504088896340736f : -INFINITY;
+            f32x4 s4[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                f32x4 s4 = {0.f, 0.f, 0.f, 0.f};
+                s4[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int s = 0; s < KS; ++s)
-                    s4 = E::mfma16(a[t][s], q[s], s4);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float e = __builtin_amdgcn_exp2f(fmaf(s4[k], p.c_log2, shift));
-                    w[t][k] += j0 + 16 * t + 4 * g + k <= last ? e : 0.f;
-                }
+                    s4[t] = E::mfma16(a[t][s], q[s], s4[t]);
             }
+            if (p.causal && __any(first_pos + i < j0 + kWeighKeys - 1)) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (j0 + 16 * t + 4 * g + k > first_pos + i)
+                            s4[t][k] = -INFINITY;
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    w[t][k] += __builtin_amdgcn_exp2f(fmaf(s4[t][k], p.c_log2, shift));
         }
         // ---- one sum for every key; lane 0 of a group has four
         const size_t at0 = ((size_t)b * p.c.H_kv + h) * ((size_t)p.c.table_width << p.c.page_log2);
@@ -191,6 +199,218 @@ __global__ __launch_bounds__(256) void attn_weigh_rows_kernel(const WeighParams 
     }
 }
 
+// Many rows: a workgroup has 256 keys (128 at D = 256), each wave its part of them in registers as A operands of v_mfma_f32_32x32x16,
+// and the rows pass through LDS in stages that all waves read.  A batch with few blocks of so many keys is cut finer: the
+// waves of a workgroup then have the same keys and take a stage's 32-row tiles in turn.
+template <int D>
+struct WeighTiling {
+    static constexpr int ROWB = D * 2, SUB = D == 256 ? 2 : 4;     // 32-row tiles of a stage
+    static constexpr int ROWS = 32 * SUB, STAGE = ROWS * ROWB;
+    static constexpr int KB = D == 256 ? 1 : 2;                    // 32-key blocks of a wave
+    static constexpr int KEYS = 4 * 32 * KB;                       // of a workgroup
+    static constexpr int LDS_BYTES = 2 * STAGE;
+};
+constexpr int kWeighTileGroups = 512;   // workgroups of a launch: two to a compute unit
+
+template <int D, typename E, bool E4M3>
+__global__ __launch_bounds__(256, 2) void attn_weigh_tiles_kernel(const WeighParams p)
+{
+    typedef WeighTiling<D> T;
+    constexpr int ROWB = T::ROWB, SUB = T::SUB, KB = T::KB, KS = D / 16, CROWB = D * (E4M3 ? 1 : 2);
+    constexpr int LOADS = T::STAGE / 4096, CPR = ROWB / 16, RPL = 64 / CPR;    // loads of a wave and stage, chunks of a row, rows of a load
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(ATTN_LDS_PTR(unsigned char))smem;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lq = lane & 31, g = lane >> 5;
+    const int page_mask = (1 << p.c.page_log2) - 1;
+    WeighUnits units;
+    units.begin(p.c, __builtin_ctz(T::KEYS));
+    const bool split = p.c.B <= 64 && (long long)units.all * p.c.H_kv < kWeighTileGroups;
+    if (split)
+        units.begin(p.c, __builtin_ctz(T::KEYS / SUB));
+    const int my_keys = (split ? wave / SUB : wave) * 32 * KB, my_tile = split ? wave % SUB : -1;
+    const uint32_t k0 = (uint32_t)(lq * ROWB + ((g ^ swz<D>(lq)) * 16));       // chunk g of row lq; chunk 2 s + g: k0 ^ 32 s
+    const uint32_t st = (uint32_t)p.q_st * 2, sh = (uint32_t)p.q_sh * 2;       // (the host keeps offsets of a call's rows to 32 bits)
+
+    for (long long unit = blockIdx.x;; unit += gridDim.x) {
+        int b, n, row0, kv, key0;
+        const long long block = quotient(unit, p.c.H_kv);
+        const int h = (int)(unit - block * p.c.H_kv);
+        if (!units.find(p.c, block, b, n, row0, kv, key0))
+            return;
+        const int j0 = key0 + my_keys, n_rows = n * p.G, first_pos = kv - n;
+        const int from = p.causal ? (int)min((long long)max(key0 - first_pos, 0) * p.G, (long long)n_rows) : 0;
+        const int stages = (n_rows - from + T::ROWS - 1) / T::ROWS;
+
+        // ---- rows: memory -> LDS, stage i into its half.  A load takes RPL rows; lane -> (row, 16-byte chunk), the swizzle of a
+        // tile's rows is applied on the global side.  Rows behind the last repeat it
+        const uint64_t at = (uint64_t)(uintptr_t)p.q + 2 * ((long long)row0 * p.q_st + (long long)h * p.G * p.q_sh);
+        const void *rows = reinterpret_cast<const void *>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32 |
+                                                          (uint32_t)__builtin_amdgcn_readfirstlane((int)at));
+        asm volatile("s_nop 4" : "+s"(rows));               // five wait states between the vector unit's write of a scalar and a load
+        uint32_t off[LOADS];
+        int rem[LOADS];                                     // head of the row in its group
+        const int step_rem = T::ROWS % p.G;
+        const uint32_t step = (uint32_t)(T::ROWS / p.G) * st + (uint32_t)step_rem * sh, wrap = st - (uint32_t)p.G * sh;
+        auto bring = [&](int i) {
+            if (i >= stages)
+                return;
+            const int first = from + i * T::ROWS;
+#pragma unroll
+            for (int l = 0; l < LOADS; ++l) {
+                const int r = (wave * LOADS + l) * RPL + lane / CPR, ch = lane % CPR;
+                if (i == 0 || first + T::ROWS > n_rows) {
+                    const int row = min(first + r, n_rows - 1), token = p.token_of(row);
+                    rem[l] = row - token * p.G;
+                    off[l] = (uint32_t)token * st + (uint32_t)rem[l] * sh + (uint32_t)(((ch & ~15) | ((ch & 15) ^ swz<D>(r))) * 16);
+                } else {
+                    off[l] += step;
+                    if (step_rem) {
+                        rem[l] += step_rem;
+                        off[l] += rem[l] >= p.G ? wrap : 0;
+                        rem[l] -= rem[l] >= p.G ? p.G : 0;
+                    }
+                }
+                dma16(lds0 + (i & 1) * T::STAGE + (wave * LOADS + l) * 1024, rows, off[l]);
+            }
+        };
+        // what a row's scores are lowered by (base 2): infinity where it sees nothing or there is no row
+        float shift[SUB], next[SUB];
+        auto ask = [&](int i) {
+#pragma unroll
+            for (int t = 0; t < SUB; ++t) {
+                if (split && t != my_tile)
+                    continue;
+                const int r = from + i * T::ROWS + 32 * t + lq, row = min(r, n_rows - 1), token = p.token_of(row);
+                const float x = p.lse[(size_t)(row0 + token) * p.H_q + h * p.G + row - token * p.G];
+                next[t] = r < n_rows ? x : -INFINITY;
+            }
+        };
+        __syncthreads();                                    // the last unit's rows have been read
+        if (stages > 0) {
+            bring(0);
+            ask(0);
+        }
+
+        // ---- keys: lane l has key l % 32 of a block, elements 16 s + 8 g on of step s
+        u32x4 a[KB][KS];
+#pragma unroll
+        for (int t = 0; t < KB; ++t) {
+            const int j = min(j0 + 32 * t + lq, kv - 1);
+            const size_t row = p.c.page_row(max(p.c.page_of(b, j), 0), h) + (j & page_mask);
+            const unsigned char *k = static_cast<const unsigned char *>(p.k) + row * CROWB;
+            if constexpr (E4M3) {
+                const float unit_k = unit_of(p.k_scale[row]);
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    Piece<8> x;
+                    x.load(k + 16 * s + 8 * g);
+                    a[t][s] = u32x4{E::template from_e4m3<false>(x.d[0], unit_k), E::template from_e4m3<true>(x.d[0], unit_k),
+                                    E::template from_e4m3<false>(x.d[1], unit_k), E::template from_e4m3<true>(x.d[1], unit_k)};
+                }
+            } else {
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+                    a[t][s] = *reinterpret_cast<const u32x4 *>(k + 32 * s + 16 * g);
+            }
+        }
+
+        f32x16 w[KB];
+#pragma unroll
+        for (int t = 0; t < KB; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                w[t][r] = 0.f;
+#pragma clang loop unroll(disable)
+        for (int i = 0; i < stages; ++i) {
+            wait_vmcnt<0>();
+#pragma unroll
+            for (int t = 0; t < SUB; ++t)
+                shift[t] = next[t] == -INFINITY ? -INFINITY : -next[t] * 1.44269504088896340736f;
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");     // stage i is complete, stage i - 1 has been read
+            bring(i + 1);
+            if (i + 1 < stages)
+                ask(i + 1);
+#pragma unroll
+            for (int t = 0; t < SUB; ++t) {
+                if (split && t != my_tile)
+                    continue;
+                const uint32_t base = lds0 + (i & 1) * T::STAGE + t * 32 * ROWB;
+                f32x16 s[KB];
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        s[kb][r] = 0.f;
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    const u32x4 q = *(ATTN_LDS_PTR(const u32x4))(uintptr_t)((k0 ^ (32 * ks)) + base);
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb)
+                        s[kb] = mfma32<E>(a[kb][ks], q, s[kb]);
+                }
+                const int first = from + i * T::ROWS + 32 * t;
+                const bool cut = p.causal && first_pos + p.token_of(min(first, n_rows - 1)) < j0 + 32 * KB - 1;
+                if (cut) {                                  // some row does not see some key
+                    const int last = first_pos + p.token_of(min(first + lq, n_rows - 1));
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            if (j0 + 32 * kb + acc_row(r, g) > last)
+                                s[kb][r] = -INFINITY;
+                }
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        w[kb][r] += __builtin_amdgcn_exp2f(fmaf(s[kb][r], p.c_log2, shift[t]));
+            }
+        }
+
+        // ---- one sum for every key: over the 32 rows of a tile, and in a split unit over its waves
+        float y[KB];                                        // of key acc_row(lq % 16, g)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            y[kb] = 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float x = sum16(w[kb][r]), all = x + __shfl_xor(x, 16, 64);
+                y[kb] = (lq & 15) == r ? all : y[kb];
+            }
+        }
+        if (split) {
+            float *const part = reinterpret_cast<float *>(smem);
+            __syncthreads();                                // the rows have been read
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+                part[(wave * KB + kb) * 64 + lane] = y[kb];
+            __syncthreads();
+            if (my_tile != 0)
+                continue;
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                y[kb] = 0.f;
+                for (int v = wave; v < wave + SUB; ++v)
+                    y[kb] += part[(v * KB + kb) * 64 + lane];
+            }
+        }
+        const size_t at0 = ((size_t)b * p.c.H_kv + h) * ((size_t)p.c.table_width << p.c.page_log2);
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            const int j = j0 + 32 * kb + acc_row(lq & 15, g);
+            if (lq >= 16 || j >= kv)
+                continue;
+            float x = p.c.page_of(b, j) >= 0 ? y[kb] : 0.f;
+            if (j < first_pos && p.weights)
+                x = fmaf(p.decay, p.weights[at0 + j], x);
+            p.out[at0 + j] = x;
+            if (p.stamps && j >= first_pos)
+                p.stamps[at0 + j] = p.seen[b] - kv + j;
+        }
+    }
+}
+
 }  // namespace attn
 
 namespace {
@@ -199,15 +419,30 @@ using attn::WeighParams;
 
 bool misaligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
+// rows of a sequence up to which the row kernel takes a call
+constexpr long long kRowsMost = 128;
+
 template <int D, typename E, bool E4M3>
-int launch(const WeighParams &p, hipStream_t st)
+int launch(const WeighParams &p, int max_q, hipStream_t st)
 {
-    // (no more units than the table holds, and than pages of positions that rows could belong to)
-    const long long blocks = (((long long)p.c.table_width << p.c.page_log2) + 4 * attn::kWeighKeys - 1) / (4 * attn::kWeighKeys);
+    const long long rows = (long long)(max_q < p.c.T ? max_q : p.c.T) * p.G;
+    const long long reach = 2 * ((long long)p.c.T * p.q_st + (long long)p.G * p.q_sh + D);  // bytes of a head's rows
+    const bool tiles = rows > kRowsMost && reach < 1LL << 32;
+    // no more workgroups than units that the table can hold
+    const long long keys = tiles ? attn::WeighTiling<D>::KEYS / attn::WeighTiling<D>::SUB : 4 * attn::kWeighKeys;
+    const long long blocks = (((long long)p.c.table_width << p.c.page_log2) + keys - 1) / keys;
     const long long seqs = p.c.B < p.c.T ? p.c.B : p.c.T;
-    const long long most = attn::kWeighGroups, per_seq = blocks < most ? blocks * p.c.H_kv : most;
+    const int held = tiles ? attn::kWeighTileGroups : attn::persistent_slots(reinterpret_cast<const void *>(attn::attn_weigh_rows_kernel<D, E, E4M3>), 256, 0, 1);
+    const long long most = held > 0 ? held : attn::kWeighGroups, per_seq = blocks < most ? blocks * p.c.H_kv : most;
     const long long grid = per_seq < most / seqs ? per_seq * seqs : most;
-    hipLaunchKernelGGL((attn::attn_weigh_rows_kernel<D, E, E4M3>), dim3((unsigned)grid), dim3(256), 0, st, p);
+    if (tiles) {
+        constexpr int lds = attn::WeighTiling<D>::LDS_BYTES;
+        if (!attn::allow_lds(reinterpret_cast<const void *>(attn::attn_weigh_tiles_kernel<D, E, E4M3>), lds))
+            return ATTN_ERR_LAUNCH;
+        hipLaunchKernelGGL((attn::attn_weigh_tiles_kernel<D, E, E4M3>), dim3((unsigned)grid), dim3(256), lds, st, p);
+    } else {
+        hipLaunchKernelGGL((attn::attn_weigh_rows_kernel<D, E, E4M3>), dim3((unsigned)grid), dim3(256), 0, st, p);
+    }
     return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH;
 }
 
@@ -264,9 +499,9 @@ int weigh(const void *q, const long long *strides, const float *lse, const void 
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const bool e4m3 = kind == ATTN_CACHE_E4M3;
     switch (D) {
-    case 64: return e4m3 ? launch<64, E, true>(p, st) : launch<64, E, false>(p, st);
-    case 128: return e4m3 ? launch<128, E, true>(p, st) : launch<128, E, false>(p, st);
-    default: return e4m3 ? launch<256, E, true>(p, st) : launch<256, E, false>(p, st);
+    case 64: return e4m3 ? launch<64, E, true>(p, max_q, st) : launch<64, E, false>(p, max_q, st);
+    case 128: return e4m3 ? launch<128, E, true>(p, max_q, st) : launch<128, E, false>(p, max_q, st);
+    default: return e4m3 ? launch<256, E, true>(p, max_q, st) : launch<256, E, false>(p, max_q, st);
     }
 }
 

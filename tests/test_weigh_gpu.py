@@ -137,3 +137,26 @@ def test_weights_of_a_row_add_up_to_one():
     M.attn_cache_weigh(q, lse, args[0], *args[2:], w, max_q=20)
     total = w.double().sum(-1).cpu()
     assert ((total - torch.tensor([[80.0, 80.0], [4.0, 4.0]])).abs() < 1e-4 * total).all()
+
+
+@pytest.mark.parametrize("D, kv, e4m3", [(64, 16500, False), (128, 16500, True), (128, 16500, False), (256, 8400, False)])
+def test_many_rows_on_many_blocks_of_keys(D, kv, e4m3):
+    """So many blocks that a wave has keys of its own (with fewer, a workgroup's waves share theirs)."""
+    from paper_2512_18134_amd import binding as M
+    c = Cache([70, 3], [kv, 200], 8, D, 64, "bf16", e4m3, 107)
+    check(M, c, 1, True, 0.5, stamps=True, max_q=70)
+    c = Cache([140], [kv], 8, D, 64, "f16", e4m3, 109)
+    check(M, c, 1, False, 0.0, in_place=False, empty=[1, 139])
+
+
+def test_strided_queries():
+    from paper_2512_18134_amd import binding as M
+    for n, G in ((3, 4), (90, 3)):
+        c = Cache([n, 1], [300, 40], 2, 128, 16, "bf16", False, 113)
+        fused = torch.randn((c.T, 2 * G + 5, 128), generator=c.gen).bfloat16()
+        args, _ = c.on_gpu()
+        lse = torch.randn((c.T, 2 * G), generator=c.gen).cuda()
+        w = [torch.zeros((2, 2, c.table.shape[1] * 16), device="cuda") for _ in range(2)]
+        M.attn_cache_weigh(fused.cuda()[:, 2:2 + 2 * G], lse, args[0], *args[2:], w[0], max_q=n)
+        M.attn_cache_weigh(fused[:, 2:2 + 2 * G].contiguous().cuda(), lse, args[0], *args[2:], w[1], max_q=n)
+        assert torch.equal(*w) and float(w[0].sum()) > 0
