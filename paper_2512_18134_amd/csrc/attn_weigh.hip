@@ -94,52 +94,86 @@ __device__ __forceinline__ float sum16(float x)
 constexpr int kWeighKeys = 32;          // of a wave
 constexpr int kWeighGroups = 2048;      // workgroups of a launch, at most: what the chip holds at once
 
+// Few rows: a wave to 32 keys of a head, and no wave waits for another.  The next unit and its pages are looked up while the
+// keys of this one are on their way.
 template <int D, typename E, bool E4M3>
 __global__ __launch_bounds__(256) void attn_weigh_rows_kernel(const WeighParams p)
 {
-    constexpr int KEYS = 4 * kWeighKeys, EB = E4M3 ? 1 : 2, ROWB = D * EB, KL = ROWB / 64, KS = D / 32;
+    constexpr int EB = E4M3 ? 1 : 2, ROWB = D * EB, KL = ROWB / 64, KS = D / 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, g = lane >> 4;
     const int page_mask = (1 << p.c.page_log2) - 1;
     WeighUnits units;
-    units.begin(p.c, __builtin_ctz(KEYS));
-    for (long long unit = blockIdx.x;; unit += gridDim.x) {
-        int b, n, row0, kv, key0;
+    units.begin(p.c, __builtin_ctz(4 * kWeighKeys));
+    struct Next {
+        bool exists;
+        int b, n, row0, kv, j0, h, page[2];                 // pages as the table has them, in a lane's register
+    };
+    long long unit = blockIdx.x;
+    auto look_up = [&] {
+        Next x;
         const long long block = quotient(unit, p.c.H_kv);
-        const int h = (int)(unit - block * p.c.H_kv);
-        if (!units.find(p.c, block, b, n, row0, kv, key0))
-            return;
-        const int j0 = key0 + wave * kWeighKeys;
-        if (j0 >= kv)
+        x.h = (int)(unit - block * p.c.H_kv);
+        x.exists = units.find(p.c, block, x.b, x.n, x.row0, x.kv, x.j0);
+        unit += gridDim.x;
+        x.j0 += wave * kWeighKeys;
+        if (x.exists) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+                x.page[t] = p.c.page_table[(size_t)x.b * p.c.table_width + (min(x.j0 + 16 * t, x.kv - 1) >> p.c.page_log2)];
+        }
+        return x;
+    };
+    for (Next next = look_up(); next.exists;) {
+        if (next.j0 >= next.kv) {                           // (none of the unit's last keys)
+            next = look_up();
             continue;
-        // ---- this wave's keys as A operands
+        }
+        const int b = next.b, n = next.n, row0 = next.row0, kv = next.kv, j0 = next.j0, h = next.h;
+        // ---- this wave's keys, on their way
         bool ok[2];
+        Piece<16> x[2][KL];
+        uint32_t units_k[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int id = __builtin_amdgcn_readfirstlane(next.page[t]);
+            ok[t] = (unsigned)id < (unsigned)p.c.n_pages;
+            const size_t row = p.c.page_row(ok[t] ? id : 0, h) + (min(j0 + 16 * t, (kv - 1) & ~15) & page_mask);
+            const unsigned char *k = static_cast<const unsigned char *>(p.k) + row * ROWB;
+#pragma unroll
+            for (int i = 0; i < KL; ++i)
+                x[t][i].load(k + c * ROWB + g * 16 + i * 64);
+            if (E4M3)
+                units_k[t] = p.k_scale[row + c];
+        }
+        // ---- and what they have: four to a group of lanes
+        const size_t at0 = ((size_t)b * p.c.H_kv + h) * ((size_t)p.c.table_width << p.c.page_log2) + j0 + 4 * g;
+        const int first_pos = kv - n;
+        f32x4 old[2] = {};
+        if (p.weights && j0 < first_pos) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+                old[t] = *reinterpret_cast<const f32x4 *>(p.weights + at0 + (j0 + 16 * t < kv ? 16 * t : 0));
+        }
+        next = look_up();
+        // ---- as A operands
         u32x4 a[2][KS];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const int j = min(j0 + 16 * t, (kv - 1) & ~15);
-            const int id = __builtin_amdgcn_readfirstlane(p.c.page_of(b, j));
-            ok[t] = id >= 0;
-            const size_t row = p.c.page_row(max(id, 0), h) + (j & page_mask);
-            const unsigned char *k = static_cast<const unsigned char *>(p.k) + row * ROWB;
-            Piece<16> x[KL];
-#pragma unroll
-            for (int i = 0; i < KL; ++i)
-                x[i].load(k + c * ROWB + g * 16 + i * 64);
-            const float unit_k = E4M3 ? unit_of(p.k_scale[row + c]) : 1.f;
+            const float unit_k = E4M3 ? unit_of(units_k[t]) : 1.f;
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 if constexpr (E4M3) {
-                    const uint32_t lo = x[s >> 1].d[2 * (s & 1)], hi = x[s >> 1].d[2 * (s & 1) + 1];
+                    const uint32_t lo = x[t][s >> 1].d[2 * (s & 1)], hi = x[t][s >> 1].d[2 * (s & 1) + 1];
                     a[t][s] = u32x4{E::template from_e4m3<false>(lo, unit_k), E::template from_e4m3<true>(lo, unit_k),
                                     E::template from_e4m3<false>(hi, unit_k), E::template from_e4m3<true>(hi, unit_k)};
                 } else {
-                    a[t][s] = u32x4{x[s].d[0], x[s].d[1], x[s].d[2], x[s].d[3]};
+                    a[t][s] = u32x4{x[t][s].d[0], x[t][s].d[1], x[t][s].d[2], x[t][s].d[3]};
                 }
             }
         }
         // ---- the rows that see some of them
-        const int n_rows = n * p.G, first_pos = kv - n;
+        const int n_rows = n * p.G;
         const int from = p.causal ? (int)min((long long)max(j0 - first_pos, 0) * p.G, (long long)n_rows) : 0;
         float w[2][4] = {};
         for (int r0 = from & ~15; r0 < n_rows; r0 += 16) {
@@ -175,25 +209,31 @@ __global__ __launch_bounds__(256) void attn_weigh_rows_kernel(const WeighParams 
                     w[t][k] += __builtin_amdgcn_exp2f(fmaf(s4[t][k], p.c_log2, shift));
         }
         // ---- one sum for every key; lane 0 of a group has four
-        const size_t at0 = ((size_t)b * p.c.H_kv + h) * ((size_t)p.c.table_width << p.c.page_log2);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                w[t][k] = ok[t] ? sum16(w[t][k]) : 0.f;
-            if (c != 0)
-                continue;
+            const int j = j0 + 16 * t + 4 * g;
+            f32x4 y;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int j = j0 + 16 * t + 4 * g + k;
-                if (j >= kv)
-                    break;
-                float y = w[t][k];
-                if (j < first_pos && p.weights)
-                    y = fmaf(p.decay, p.weights[at0 + j], y);
-                p.out[at0 + j] = y;
-                if (p.stamps && j >= first_pos)
-                    p.stamps[at0 + j] = p.seen[b] - kv + j;
+                y[k] = ok[t] ? sum16(w[t][k]) : 0.f;
+                if (p.weights && j + k < first_pos)
+                    y[k] = fmaf(p.decay, old[t][k], y[k]);
+            }
+            if (c != 0)
+                continue;
+            if (j + 4 <= kv) {
+                *reinterpret_cast<f32x4 *>(p.out + at0 + 16 * t) = y;
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (j + k < kv)
+                        p.out[at0 + 16 * t + k] = y[k];
+            }
+            if (p.stamps && j + 4 > first_pos) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (j + k >= first_pos && j + k < kv)
+                        p.stamps[at0 + 16 * t + k] = p.seen[b] - kv + j + k;
             }
         }
     }
