@@ -34,6 +34,8 @@ constexpr int kRowsMinRange = 2, kTilesMinRange = 4;
 // keys 13.6 whole, 9.9 cut.
 constexpr long long kWholeBytes = 1 << 18;
 constexpr int kWaves = 8;
+// Bytes of K and V, counted for every 16-row tile that reads them, up to which a tree's rows are taken 16 at a time.
+constexpr long long kFewBytes = 32 << 20;
 constexpr int kSlots = 2 * kTarget + 64;
 // words of 64 bits of a row's mask, at most: as many new tokens as a tree of drafts will not have
 constexpr int kMostMaskWords = 1 << 10;
@@ -134,7 +136,8 @@ int launch_rows(const ParamsOf<TREE> &p, int MT, int upto, hipStream_t st)
     return launch_rows<D, 2, E, E4M3, TREE>(p, upto, st);
 }
 
-template <int D, typename E, bool E4M3, bool TREE>
+// QB (TREE): 32-row blocks of a wave of the tile kernel
+template <int D, typename E, bool E4M3, bool TREE, int QB = PagedTilesTiling<D>::QB>
 int launch_tiles(ParamsOf<TREE> p, int above, hipStream_t st)
 {
     p.kernel = 1, p.slots = p.parts[1].slots, p.rows_above = above, p.rows_upto = 0x7fffffff;
@@ -144,9 +147,9 @@ int launch_tiles(ParamsOf<TREE> p, int above, hipStream_t st)
     const void *kern;
     int lds, threads;
     if constexpr (E4M3 || TREE) {
-        typedef PagedTilesTiling<D> T;
-        p.target = kTarget;                                // two of its workgroups to a compute unit
-        kern = reinterpret_cast<const void *>(attn_paged_tiles_kernel<D, E, E4M3, TREE>);
+        typedef PagedTilesTiling<D, QB> T;
+        p.target = kTarget / 2 * T::PER_CU;
+        kern = reinterpret_cast<const void *>(attn_paged_tiles_kernel<D, E, E4M3, TREE, QB>);
         lds = T::LDS_BYTES, threads = T::THREADS;
     } else {
         typedef PagedAsmTiling<D> T;
@@ -161,9 +164,9 @@ int launch_tiles(ParamsOf<TREE> p, int above, hipStream_t st)
     if (!allow_lds(kern, lds))
         return ATTN_ERR_LAUNCH;
     if constexpr (E4M3 || TREE) {
-        if (const int rc = launch_cut<PagedTilesTiling<D>::BM, TREE>(p, st))
+        if (const int rc = launch_cut<PagedTilesTiling<D, QB>::BM, TREE>(p, st))
             return rc;
-        hipLaunchKernelGGL((attn_paged_tiles_kernel<D, E, E4M3, TREE>), dim3((unsigned)grid), dim3(threads), lds, st, p);
+        hipLaunchKernelGGL((attn_paged_tiles_kernel<D, E, E4M3, TREE, QB>), dim3((unsigned)grid), dim3(threads), lds, st, p);
     } else {
         if (const int rc = launch_cut<PagedAsmTiling<D>::BM, TREE>(p, st))
             return rc;
@@ -172,26 +175,19 @@ int launch_tiles(ParamsOf<TREE> p, int above, hipStream_t st)
     return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH;
 }
 
-template <int D, typename E, bool E4M3, bool TREE>
-int launch(ParamsOf<TREE> &p, int max_q, hipStream_t st)
+// The merge behind a call's kernels: workgroups, 0 where no sequence can be longer than one range.
+struct Merge {
+    int walkers;
+    long long blocks;
+};
+
+// many: the tile kernel's partial results are most of them; shortest: blocks of the shortest range
+template <int D>
+Merge merge_of(const PagedParams &p, bool many, int shortest)
 {
-    // Sequences of few rows and of many may be in one batch; each kernel takes its own.  One launch where max_q, or a
-    // single sequence, says that there is one kind (and then for whatever the batch holds).
-    const int most = rows_kernel_most(D);
-    const long long rows = (long long)(max_q < p.c.T ? max_q : p.c.T) * p.G;
-    const bool few = rows <= most, many = !few, both = many && p.c.B > 1;
-    const int MT = row_tiles(D, rows < most ? rows : most);
-    p.parts[0].BM = 16 * MT, p.parts[1].BM = E4M3 || TREE ? PagedTilesTiling<D>::BM : PagedAsmTiling<D>::BM;
-    int rc = ATTN_OK;
-    // Short sequences, and no more of them than compute units.  (The bound is what the page table can hold.)
-    if constexpr (D != 256)
-        if (few && MT == 1 && ((long long)p.c.T * p.G / 16 + (p.c.B < p.c.T ? p.c.B : p.c.T)) * p.c.H_kv <= kTarget / 2 &&
-            ((long long)p.c.table_width << p.c.page_log2) * D * (E4M3 ? 2 : 4) <= kWholeBytes)
-            return launch_rows<D, 1, E, E4M3, TREE, kWaves>(p, 0x7fffffff, st);
-    // no sequence can be longer than one range: nothing to merge
-    static_assert(kRowsMinRange <= kTilesMinRange, "the row kernel's ranges are the shorter ones");
-    const int shortest = few || both ? kRowsMinRange : kTilesMinRange;
-    const bool merged = ((long long)p.c.table_width << p.c.page_log2) > (long long)shortest * kPlanBlock;
+    Merge m = {1, 0};
+    if (((long long)p.c.table_width << p.c.page_log2) <= (long long)shortest * kPlanBlock)
+        return m;
     constexpr int kGroups = 256 / (D / 4);
     const long long o_rows = (long long)p.c.T * p.H_q;
     // eight ranges to a walker, of as many as a sequence may be expected to have: a launch has one for each head and row tile,
@@ -200,20 +196,90 @@ int launch(ParamsOf<TREE> &p, int max_q, hipStream_t st)
     const long long tiles = (long long)p.c.T * p.G / p.parts[many].BM + 1;
     const long long alone = (p.c.B > tiles ? p.c.B : tiles) * p.c.H_kv;
     const long long expected = 1 + 2 * kTarget / alone;
-    int walkers = 1;
-    while (walkers < kGroups && 8 * walkers < expected && 8 * walkers < most_ranges)
-        walkers *= 2;
-    const long long blocks = (o_rows * walkers + kGroups - 1) / kGroups;
-    if (merged && blocks > most_workgroups(256))     // (before anything is launched)
+    while (m.walkers < kGroups && 8 * m.walkers < expected && 8 * m.walkers < most_ranges)
+        m.walkers *= 2;
+    m.blocks = (o_rows * m.walkers + kGroups - 1) / kGroups;
+    return m;
+}
+
+template <int D, typename E, bool TREE>
+int launch_merge(const ParamsOf<TREE> &p, const Merge &m, hipStream_t st)
+{
+    if (m.blocks)
+        hipLaunchKernelGGL((attn_paged_merge_kernel<D, typename E::t, TREE>), dim3((unsigned)m.blocks), dim3(256), 0, st, p, m.walkers);
+    return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH;
+}
+
+template <int D, typename E, bool E4M3>
+int launch(PagedParams &p, int max_q, hipStream_t st)
+{
+    // Sequences of few rows and of many may be in one batch; each kernel takes its own.  One launch where max_q, or a
+    // single sequence, says that there is one kind (and then for whatever the batch holds).
+    const int most = rows_kernel_most(D);
+    const long long rows = (long long)(max_q < p.c.T ? max_q : p.c.T) * p.G;
+    const bool few = rows <= most, many = !few, both = many && p.c.B > 1;
+    const int MT = row_tiles(D, rows < most ? rows : most);
+    p.parts[0].BM = 16 * MT, p.parts[1].BM = E4M3 ? PagedTilesTiling<D>::BM : PagedAsmTiling<D>::BM;
+    int rc = ATTN_OK;
+    // Short sequences, and no more of them than compute units.  (The bound is what the page table can hold.)
+    if constexpr (D != 256)
+        if (few && MT == 1 && ((long long)p.c.T * p.G / 16 + (p.c.B < p.c.T ? p.c.B : p.c.T)) * p.c.H_kv <= kTarget / 2 &&
+            ((long long)p.c.table_width << p.c.page_log2) * D * (E4M3 ? 2 : 4) <= kWholeBytes)
+            return launch_rows<D, 1, E, E4M3, false, kWaves>(p, 0x7fffffff, st);
+    static_assert(kRowsMinRange <= kTilesMinRange, "the row kernel's ranges are the shorter ones");
+    const Merge merge = merge_of<D>(p, many, few || both ? kRowsMinRange : kTilesMinRange);
+    if (merge.blocks > most_workgroups(256))               // (before anything is launched)
         return ATTN_ERR_SHAPE;
     if (few || both)
-        rc = launch_rows<D, E, E4M3, TREE>(p, MT, both ? most : 0x7fffffff, st);
+        rc = launch_rows<D, E, E4M3, false>(p, MT, both ? most : 0x7fffffff, st);
     if (rc == ATTN_OK && many)
-        rc = launch_tiles<D, E, E4M3, TREE>(p, both ? most : 0, st);
-    if (rc != ATTN_OK || !merged)
-        return rc;
-    hipLaunchKernelGGL((attn_paged_merge_kernel<D, typename E::t, TREE>), dim3((unsigned)blocks), dim3(256), 0, st, p, walkers);
-    return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH;
+        rc = launch_tiles<D, E, E4M3, false>(p, both ? most : 0, st);
+    return rc == ATTN_OK ? launch_merge<D, E, false>(p, merge, st) : rc;
+}
+
+// Trees of drafted tokens: few rows of many heads, or some hundreds.  One kernel takes all sequences of a call: 16-row tiles of the row
+// kernel where no sequence has more, or where K and V are so small that reading them for every such tile takes no time (kFewBytes); otherwise
+// the tile kernel, whose waves share a tile of keys, with 32 or 64 rows to a wave.  A wave without rows brings its share of
+// the keys and has nothing else to do, so that a sequence of few rows costs the tile kernel no more than its stream.
+template <int D, typename E, bool E4M3>
+int launch(TreeParams &p, int max_q, const Workspace &w, hipStream_t st)
+{
+    const long long rows = (long long)(max_q < p.c.T ? max_q : p.c.T) * p.G;
+    const long long tiles16 = (long long)p.c.T * p.G / 16 + (p.c.B < p.c.T ? p.c.B : p.c.T);
+    const long long head_bytes = ((long long)p.c.table_width << p.c.page_log2) * D * (E4M3 ? 2 : 4);
+    const bool few = rows <= 16 || tiles16 * p.c.H_kv * head_bytes <= kFewBytes;
+    if constexpr (D != 256)
+        if (few && tiles16 * p.c.H_kv <= kTarget / 2 && head_bytes <= kWholeBytes)
+            return launch_rows<D, 1, E, E4M3, true, kWaves>(p, 0x7fffffff, st);
+    // the kernel has the workspace for itself
+    PagedParams::Parts &parts = p.parts[few ? 0 : 1];
+    parts.BM = few ? 16 : D == 256 || rows <= 128 ? 128 : 256;
+    const long long fit = w.merge / ((long long)parts.BM * (D + 1) * 4);
+    parts.slots = (int)(fit < kSlots ? fit : kSlots);
+    parts.o = p.parts[0].o;
+    parts.lse = parts.o + (long long)parts.slots * parts.BM * D;
+    const Merge merge = merge_of<D>(p, !few, few ? kRowsMinRange : kTilesMinRange);
+    if (merge.blocks > most_workgroups(256))
+        return ATTN_ERR_SHAPE;
+    int rc;
+    if (few)
+        rc = launch_rows<D, 1, E, E4M3, true>(p, 0x7fffffff, st);
+    else if (parts.BM == 128)
+        rc = launch_tiles<D, E, E4M3, true, 1>(p, 0, st);
+    else
+        rc = launch_tiles<D, E, E4M3, true>(p, 0, st);
+    return rc == ATTN_OK ? launch_merge<D, E, true>(p, merge, st) : rc;
+}
+
+template <int D, typename E, bool E4M3>
+int go(PagedParams &p, int max_q, const Workspace &, hipStream_t st)
+{
+    return launch<D, E, E4M3>(p, max_q, st);
+}
+template <int D, typename E, bool E4M3>
+int go(TreeParams &p, int max_q, const Workspace &w, hipStream_t st)
+{
+    return launch<D, E, E4M3>(p, max_q, w, st);
 }
 
 // The call of either entry point.  mask: [T][mask_words] words of 64 bits (TREE), otherwise NULL.
@@ -280,9 +346,9 @@ int paged_call(const void *q, const long long *strides, void *o, float *lse, con
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const bool e4m3 = kind == ATTN_CACHE_E4M3;
     switch (D) {
-    case 64: return e4m3 ? launch<64, E, true, TREE>(p, max_q, st) : launch<64, E, false, TREE>(p, max_q, st);
-    case 128: return e4m3 ? launch<128, E, true, TREE>(p, max_q, st) : launch<128, E, false, TREE>(p, max_q, st);
-    default: return e4m3 ? launch<256, E, true, TREE>(p, max_q, st) : launch<256, E, false, TREE>(p, max_q, st);
+    case 64: return e4m3 ? go<64, E, true>(p, max_q, w, st) : go<64, E, false>(p, max_q, w, st);
+    case 128: return e4m3 ? go<128, E, true>(p, max_q, w, st) : go<128, E, false>(p, max_q, w, st);
+    default: return e4m3 ? go<256, E, true>(p, max_q, w, st) : go<256, E, false>(p, max_q, w, st);
     }
 }
 

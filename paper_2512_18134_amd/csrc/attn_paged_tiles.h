@@ -37,23 +37,25 @@ __device__ __forceinline__ f32x16 mfma32<PagedF16>(u32x4 a, u32x4 b, f32x16 c)
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(PagedF16::x8, a), __builtin_bit_cast(PagedF16::x8, b), c, 0, 0, 0);
 }
 
-template <int D>
+// QB: 32-row blocks of a wave
+template <int D, int QB_ = D == 256 ? 1 : 2>
 struct PagedTilesTiling {
-    static constexpr int QB = D == 256 ? 1 : 2;             // 32-row blocks of a wave
+    static constexpr int QB = QB_;
     static constexpr int NW = 4, THREADS = NW * 64, BM = NW * QB * 32, BN = 32;
     static constexpr int ROWB = D * 2, TB = BN * ROWB;      // bytes of a tile in LDS
     static constexpr int STAGES = 2;                        // of K and V: tile j is read while j + 1 is written
     // steps of S whose part of Q waits in LDS: 128 registers of O and 64 of Q leave too few for the rest
-    static constexpr int QL = D == 64 ? 0 : D == 256 ? 4 : 5;
+    static constexpr int QL = D == 64 || (D == 128 && QB == 1) ? 0 : D == 256 ? 4 : 5;
+    static constexpr int PER_CU = D < 256 && QB == 1 ? 3 : 2;      // workgroups of a compute unit, for which registers are kept
     static constexpr int Q_BYTES = QL * BM * 32, LDS_BYTES = 2 * STAGES * TB + Q_BYTES;
 };
 
 // One unit.  E4M3: the pool's kind.  TREE: the new tokens see each other by the mask.
-template <int D, typename E, bool E4M3, bool TREE>
+template <int D, typename E, bool E4M3, bool TREE, int QB>
 __device__ __forceinline__ void attn_paged_tiles_unit(const ParamsOf<TREE> &p, const Unit &u, unsigned char *smem)
 {
-    typedef PagedTilesTiling<D> T;
-    constexpr int QB = T::QB, ROWB = T::ROWB, TB = T::TB, BN = T::BN, ST = T::STAGES;
+    typedef PagedTilesTiling<D, QB> T;
+    constexpr int ROWB = T::ROWB, TB = T::TB, BN = T::BN, ST = T::STAGES;
     constexpr int KS = D / 16, DB = D / 32;
     constexpr int CROWB = D;                                // bytes of a cached row
     // what a lane brings of a wave's eight rows: pieces of 16 bytes of memory (D = 64: 8 bytes)
@@ -241,7 +243,14 @@ __device__ __forceinline__ void attn_paged_tiles_unit(const ParamsOf<TREE> &p, c
 
         // D = 256: the next rows are asked for once S has left its registers, otherwise first of all
         constexpr bool LATE = D == 256;
+        const bool idle = TREE && tile_row + wave * QB * 32 >= u.n_rows;      // (a wave without rows)
         auto tile = [&](int j) {
+            if constexpr (TREE)
+                if (idle) {
+                    if constexpr (E4M3 && LATE)
+                        fetch(j + 2);
+                    return;
+                }
             const uint32_t base = lds0 + (j % ST) * 2 * TB;
             // the offsets of the later steps are made anew in every tile: kept across tiles they take registers from O and Q
             asm volatile("" : "+v"(k0), "+v"(v0[0]), "+v"(v0[1]));
@@ -398,10 +407,10 @@ __device__ __forceinline__ void attn_paged_tiles_unit(const ParamsOf<TREE> &p, c
 }
 
 // A workgroup takes every gridDim.x-th unit (attn_paged_asm.h).
-template <int D, typename E, bool E4M3, bool TREE>
-__global__ __launch_bounds__(256, 2) void attn_paged_tiles_kernel(const ParamsOf<TREE> p)
+template <int D, typename E, bool E4M3, bool TREE, int QB = PagedTilesTiling<D>::QB>
+__global__ __launch_bounds__(256, (PagedTilesTiling<D, QB>::PER_CU)) void attn_paged_tiles_kernel(const ParamsOf<TREE> p)
 {
-    typedef PagedTilesTiling<D> T;
+    typedef PagedTilesTiling<D, QB> T;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     PlanSeq seq;
     const Plan plan = plan_call<T::BM>(p, seq);
@@ -410,7 +419,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tiles_kernel(const ParamsOf
         Unit u;
         if (find_unit<T::BM>(again, plan, seq, unit_of_pass(gridDim.x, k), u)) {
             leave_note<T::BM, T::THREADS>(again, u);
-            attn_paged_tiles_unit<D, E, E4M3, TREE>(again, u, smem);
+            attn_paged_tiles_unit<D, E, E4M3, TREE, QB>(again, u, smem);
         }
         __syncthreads();                                    // every wave has read its last tile
         seq = plan_sequence<T::BM>(params_again<TREE>(), threadIdx.x & 63);
