@@ -84,10 +84,17 @@ int attn_cache_weigh_f16(const void *q, const long long *strides, const float *l
  *   width      a multiple of 16, up to 2^30;  moves_width >= 1;  B, H_kv >= 1, B * H_kv * max(width, moves_width) at most 2^40,
  *              B * H_kv below 2^22
  *   sinks, recent   >= 0
+ *   workspace  device pointer, 16-byte aligned, owned by the caller, overwritten; workspace_bytes at least
+ *              attn_cache_select_workspace_bytes(B, H_kv, width), else ATTN_ERR_WORKSPACE; NULL where that is 0.  It holds nothing
+ *              between calls; calls that overlap in time need one each
  */
 int attn_cache_select(const float *weights, const int *stamps, const int *seen, const int *kv_len, const int *keep,
-                      int *dst, int *src, int *new_len, int sinks, int recent,
+                      int *dst, int *src, int *new_len, int sinks, int recent, void *workspace, long long workspace_bytes,
                       int B, int H_kv, int width, int moves_width, void *stream);
+
+/* Bytes of workspace attn_cache_select needs (0 up to 8192 places, a few KB for each 16384 places of a list beyond); -1 on
+ * invalid arguments. */
+long long attn_cache_select_workspace_bytes(int B, int H_kv, int width);
 
 /*
  * attn_cache_move -- enqueue moves of cached positions and return (asynchronous): for every sequence b, key head h and list element e,

@@ -125,7 +125,7 @@ def _native():
                                      for suffix in ("", "_f16")), address(_lib.attn_paged_fwd_workspace_bytes))
         module.set_eviction_entries(*(address(getattr(_lib, name)) for name in
                                       ("attn_paged_tree", "attn_paged_tree_f16", "attn_cache_weigh", "attn_cache_weigh_f16",
-                                       "attn_cache_select", "attn_cache_move")))
+                                       "attn_cache_select", "attn_cache_move", "attn_cache_select_workspace_bytes")))
         _marshal_module = module
     return _marshal_module
 
@@ -769,7 +769,9 @@ for _suffix in ("", "_f16"):
     getattr(_lib, "attn_cache_weigh" + _suffix).argtypes = ([_pointer] * 8 + [_int] + [_pointer] * 4 + [_float] + [_int] * 10
                                                             + [_float, _pointer])
 _lib.attn_cache_select.restype = _int
-_lib.attn_cache_select.argtypes = [_pointer] * 8 + [_int] * 6 + [_pointer]
+_lib.attn_cache_select.argtypes = [_pointer] * 8 + [_int] * 2 + [_pointer, _int64] + [_int] * 4 + [_pointer]
+_lib.attn_cache_select_workspace_bytes.restype = _int64
+_lib.attn_cache_select_workspace_bytes.argtypes = [_int] * 3
 _lib.attn_cache_move.restype = _int
 _lib.attn_cache_move.argtypes = [_pointer] * 7 + [_int] + [_pointer] * 2 + [_int] * 8 + [_pointer]
 
@@ -844,18 +846,24 @@ def _weigh(entry, dt, q, lse, k_pages, page_table, start, kv_len, weights, k_sca
     return out
 
 
+def attn_cache_select_workspace_bytes(B, H_kv, width):
+    return int(_lib.attn_cache_select_workspace_bytes(B, H_kv, width))
+
+
 def attn_cache_select(weights, kv_len, keep, max_moves, stamps=None, seen=None, sinks=0, recent=0, dst=None, src=None, new_len=None,
-                      stream=None):
+                      workspace=None, stream=None):
     """attn_cache_select on torch device tensors (include/attn_evict.h): which places of every sequence and key head are kept.
 
     weights fp32 [B,H_kv,width], kv_len and keep int32 [B]: of a sequence's kv_len places the `keep` ones with the largest weights
     stay, tokens below number `sinks` and the last `recent` ones before all others.  stamps int32 like weights with seen int32 [B]
     (attn_cache_weigh): the tokens' numbers, otherwise the places are.  max_moves: the lists' width, at least the smaller of
     keep and kv_len - keep of every sequence (one for which it is not drops nothing).  dst, src int32 [B,H_kv,max_moves] and
-    new_len int32 [B] are allocated when not given.  Asynchronous on `stream`.  Returns (dst, src, new_len): the
+    new_len int32 [B] are allocated when not given; workspace: a contiguous GPU tensor of at least
+    attn_cache_select_workspace_bytes(B, H_kv, width) bytes (the same).  Asynchronous on `stream`.  Returns (dst, src, new_len): the
     moves for attn_cache_move, padded with -1, and the lengths that they leave.
     """
-    r = (_marshal_module or _native()).select(weights, kv_len, keep, max_moves, stamps, seen, sinks, recent, dst, src, new_len, stream)
+    r = (_marshal_module or _native()).select(weights, kv_len, keep, max_moves, stamps, seen, sinks, recent, dst, src, new_len,
+                                              workspace, stream)
     if r is not None:
         return _finish(r)
     import torch
@@ -882,11 +890,17 @@ def attn_cache_select(weights, kv_len, keep, max_moves, stamps=None, seen=None, 
     _check_array(dst, torch.int32, (B, H_kv, max_moves), "dst", device)
     _check_array(src, torch.int32, (B, H_kv, max_moves), "src", device)
     _check_array(new_len, torch.int32, (B,), "new_len", device)
+    need = attn_cache_select_workspace_bytes(B, H_kv, width)
+    if workspace is None and need > 0:
+        workspace = _allocate(lambda: torch.empty((need,), dtype=torch.uint8, device=device), device, stream, returned=False)
+    if workspace is not None:
+        _check_array(workspace, workspace.dtype, workspace.shape, "workspace", device)
     if stream is None:
         stream = torch.cuda.current_stream(device)
     with torch.cuda.device(device):
         rc = _lib.attn_cache_select(weights.data_ptr(), _address(stamps), _address(seen), kv_len.data_ptr(), keep.data_ptr(),
-                                    dst.data_ptr(), src.data_ptr(), new_len.data_ptr(), int(sinks), int(recent), B, H_kv, width,
+                                    dst.data_ptr(), src.data_ptr(), new_len.data_ptr(), int(sinks), int(recent), _address(workspace),
+                                    0 if workspace is None else workspace.numel() * workspace.element_size(), B, H_kv, width,
                                     int(max_moves), stream.cuda_stream)
     if rc != ATTN_OK:
         raise AttnError(rc)

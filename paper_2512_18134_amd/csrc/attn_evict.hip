@@ -1,9 +1,11 @@
 // attn_evict.hip -- which places of the paged cache to keep, and moving them together: kernels and entry points
 // (include/attn_evict.h).
 //
-// Select: a workgroup to a sequence and key head.  The keep-th largest weight is found digit by digit (11, 11 and 10 bits of the
-// order-preserving integer of a float) from counts in LDS, which no order of additions can change; then every wave
-// counts what its stretch of places has to give and take, and after one sum over the waves writes its part of the lists.
+// Select: the keep-th largest weight is found digit by digit (11, 11 and 10 bits of the order-preserving integer of a float) from counts
+// in LDS, which no order of additions can change; the outcome is left as bits, from which the places' numbers in the lists are
+// counted.  Up to kSelectWhole places a workgroup has a list, its ranks in registers from the first reading on.  Longer ones
+// are shared out to workgroups, in four launches: a digit's counts of every part, which the next launch adds up.  (One workgroup is bound
+// by its vector unit, some 25 instructions for each place and digit: 131072 places in 150 us.)
 //
 // Move: a copy of rows; 16 bytes to a lane.  Dropped places before the new end are filled from kept ones behind it, so that as
 // little as possible moves and nothing depends on an order: a longer list is as many independent copies.  Short lists,
@@ -25,6 +27,11 @@ struct SelectParams {
     const int *stamps, *seen, *kv_len, *keep;
     int *dst, *src, *new_len;
     int sinks, recent, B, H_kv, width, moves;
+    // lists in parts: the counts of the digits [lists][parts][kBins] each, then what is known of a list and of its parts
+    int parts, part_places;             // of a list at most, of a part (a multiple of kPartChunk)
+    int *counts[3];
+    int2 *known;                        // [lists]: leading bits of the keep-th largest rank, how many that have them are kept
+    int *kept;                          // [lists][parts]: kept ones that are known so far
 };
 
 // Floats in the order of unsigned integers: NaN below everything, the zeros alike.
@@ -37,219 +44,377 @@ constexpr uint32_t kAlways = 0xffffffffu;                   // above the rank of
 
 typedef __attribute__((ext_vector_type(4))) int i32x4;
 
-// THREADS of a workgroup; HELD: ranks stay in registers from the first reading on, in so many vectors of four to a thread (a list of up to
-// THREADS * 4 * HELD places), 0: every pass reads anew, which the L2 serves.
-template <int THREADS, int HELD>
-struct SelectTiling {
-    static constexpr int DIGIT = THREADS == 256 ? 11 : 12;  // bits of the first digit; the second one has half of the rest
-    static constexpr int BINS = 1 << DIGIT, WAVES = THREADS / 64;
-    static constexpr int STRIDE = THREADS * 4;              // places of a vector of all threads
-    static constexpr int SEGMENT = HELD ? STRIDE * HELD : 131072;     // places whose outcome lies in LDS at once, bit by bit
+constexpr int kBins = 2048;
+constexpr int digit_bits(int pass) { return pass == 2 ? 10 : 11; }
+constexpr int digit_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
+
+constexpr int kHeld = 8;                // vectors of four ranks that a thread holds
+constexpr int kSelectThreads = 256, kSelectWhole = kSelectThreads * 4 * kHeld;
+constexpr int kPartThreads = 512, kPartChunk = kPartThreads * 4 * kHeld, kMostParts = 64;
+
+// What a workgroup shares.
+template <int THREADS>
+struct SelectShared {
+    static constexpr int PLACES = THREADS * 4 * kHeld;
+    __attribute__((aligned(16))) int count[kBins];
+    // of every 256 places four words: bit l of word k is place 4 l + k, kept in any case and as one of the last rank
+    unsigned long long above[PLACES / 64], equal[PLACES / 64];
+    int of_wave[3][THREADS / 64];
+    int found[2];
 };
 
-template <int THREADS, int HELD>
-__global__ __launch_bounds__(THREADS) void attn_select_kernel(const SelectParams p)
-{
-    typedef SelectTiling<THREADS, HELD> T;
-    constexpr int WAVES = T::WAVES;
-    __shared__ __attribute__((aligned(16))) int count[T::BINS];
-    // of every 256 places four words: bit l of word k is place 4 l + k, kept in any case and as one of the last rank
-    __shared__ unsigned long long above[T::SEGMENT / 64], equal[T::SEGMENT / 64];
-    __shared__ int of_wave[3][WAVES];
-    __shared__ int found[2];                                // digit, how many are to be kept of its elements
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int b = quotient((int)blockIdx.x, p.H_kv), h = blockIdx.x - b * p.H_kv;
-    const int kv = min(max(p.kv_len[b], 0), p.width), keep = min(kv, max(p.keep[b], 0));
-    const size_t row = (size_t)b * p.H_kv + h;
-    int *const dst = p.dst + row * p.moves, *const src = p.src + row * p.moves;
-    const bool whole = min(keep, kv - keep) > p.moves;      // more moves than the lists may hold
-    if (h == 0 && tid == 0)
-        p.new_len[b] = whole ? kv : keep;
-    int at_dst = 0, at_src = 0;
-    if (!whole && keep > 0 && keep < kv) {
+// One list, or a part of it, as the threads of a workgroup see it.
+template <int THREADS>
+struct SelectList {
+    static constexpr int WAVES = THREADS / 64, STRIDE = THREADS * 4;
+    typedef SelectShared<THREADS> Shared;
+    const SelectParams &p;
+    Shared &sh;
+    const int tid, lane, wave;
+    int b, h, kv, keep;
+    bool whole;                         // nothing is dropped
+    size_t row;
+    u32x4 held[kHeld];
+
+    __device__ __forceinline__ SelectList(const SelectParams &p_, Shared &sh_, int list)
+        : p(p_), sh(sh_), tid(threadIdx.x), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6))
+    {
+        b = quotient(list, p.H_kv), h = list - b * p.H_kv;
+        kv = min(max(p.kv_len[b], 0), p.width), keep = min(kv, max(p.keep[b], 0));
+        row = (size_t)b * p.H_kv + h;
+        // (more moves than the lists may hold, or none)
+        whole = min(keep, kv - keep) > p.moves || keep == 0 || keep == kv;
+    }
+    __device__ __forceinline__ int new_len() const { return min(keep, kv - keep) > p.moves ? kv : keep; }
+
+    // ranks of the places [lo, hi), no more than PLACES from lo & ~3 on
+    __device__ __forceinline__ void read(int lo, int hi)
+    {
         const float *const weights = p.weights + row * p.width;
         const int *const stamps = p.stamps ? p.stamps + row * p.width : nullptr;
         const long long late = (long long)(p.stamps ? p.seen[b] : kv) - p.recent;
-        // four ranks from place j on (a multiple of four; the rows end on one)
-        auto read = [&](int j) -> u32x4 {
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const int j = (lo & ~3) + i * STRIDE + 4 * tid;
+            if (j >= hi)                                    // (rows are a multiple of four long)
+                continue;
             const f32x4 w = *reinterpret_cast<const f32x4 *>(weights + j);
             i32x4 number = {j, j + 1, j + 2, j + 3};
             if (stamps)
                 number = *reinterpret_cast<const i32x4 *>(stamps + j);
-            u32x4 r;
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                r[k] = number[k] < p.sinks || number[k] >= late ? kAlways : rank_of(w[k]);
-            return r;
-        };
-        u32x4 held[HELD ? HELD : 1];
-        if constexpr (HELD != 0) {
-#pragma unroll
-            for (int i = 0; i < HELD; ++i)
-                if (i * T::STRIDE < kv) {
-                    const int j = i * T::STRIDE + 4 * tid;
-                    if (j < kv)
-                        held[i] = read(j);
-                }
-        }
-        // f(first place of the lane's four, their ranks) for the places from `from` to `upto`; lanes behind kv take part
-        auto each = [&](int from, int upto, auto f) {
-            if constexpr (HELD != 0) {
-#pragma unroll
-                for (int i = 0; i < HELD; ++i)
-                    if (i * T::STRIDE < kv)
-                        f(i * T::STRIDE + 4 * tid, held[i]);
-            } else {
-                constexpr int U = 4;
-                for (int j0 = from + 4 * tid; j0 - 4 * tid < upto; j0 += U * T::STRIDE) {
-                    u32x4 r[U];
-#pragma unroll
-                    for (int u = 0; u < U; ++u)
-                        r[u] = read(min(j0 + u * T::STRIDE, (kv - 1) & ~3));
-#pragma unroll
-                    for (int u = 0; u < U; ++u)
-                        if (j0 - 4 * tid + u * T::STRIDE < upto)
-                            f(j0 + u * T::STRIDE, r[u]);
-                }
-            }
-        };
-        // ---- the keep-th largest rank, digit by digit: its leading bits, and how many of those that have them are kept
-        uint32_t top = 0;
-        int left = keep, shift = 32;
-#pragma unroll 1
-        for (int pass = 0; pass < 3; ++pass) {
-            const int bits = pass == 0 ? T::DIGIT : pass == 1 ? (33 - T::DIGIT) / 2 : (32 - T::DIGIT) / 2;
-            const uint32_t known = pass == 0 ? 0u : ~0u << shift;
-            shift -= bits;
-            for (int i = tid; i < T::BINS / 4; i += THREADS)
-                reinterpret_cast<i32x4 *>(count)[i] = i32x4{0, 0, 0, 0};
-            __syncthreads();
-            each(0, kv, [&](int j, u32x4 r) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const bool mine = j + k < kv && (r[k] & known) == top;
-                    const int digit = r[k] >> shift & ((1 << bits) - 1);
-                    // the first lane counts for all that have its digit: one value may be everywhere
-                    const unsigned long long with = __ballot(mine);
-                    if (with == 0)
-                        continue;
-                    const int lead = __ffsll(with) - 1;
-                    const bool same = mine && digit == __builtin_amdgcn_readlane(digit, lead);
-                    const unsigned long long all = __ballot(same);
-                    if (mine && (!same || lane == lead))
-                        atomicAdd(&count[digit], same ? __popcll(all) : 1);
-                }
-            });
-            __syncthreads();
-            // from the largest digit down, PER neighbouring ones to a thread
-            constexpr int PER = T::BINS / THREADS;
-            const int first = T::BINS - (tid + 1) * PER;
-            int mine = 0;
-#pragma unroll
-            for (int i = 0; i < PER; ++i)
-                mine += count[first + i];
-            const int upto = wave_prefix(mine);
-            if (lane == 63)
-                of_wave[0][wave] = upto;
-            __syncthreads();
-            int before = upto - mine;
-            for (int w = 0; w < wave; ++w)
-                before += of_wave[0][w];
-            if (before < left && left <= before + mine) {
-                int digit = first + PER - 1;
-                while (before + count[digit] < left)
-                    before += count[digit--];
-                found[0] = digit, found[1] = left - before;
-            }
-            __syncthreads();
-            top |= (uint32_t)found[0] << shift;
-            left = found[1];
-            __syncthreads();                                // (before anything of it is written again)
-        }
-        // ---- kept: above `top`, and the first `left` of those that equal it; a segment at a time
-        for (int seg = 0; seg < kv; seg += T::SEGMENT) {
-            const int n = min(kv - seg, T::SEGMENT), blocks = (n + 255) / 256;
-            each(seg, seg + n, [&](int j, u32x4 r) {
-                const int at = (j - seg) / 256 * 4;         // (a wave's 256 places are a block)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const unsigned long long more = __ballot(j + k < kv && r[k] > top), same = __ballot(j + k < kv && r[k] == top);
-                    if (lane == k && at < 4 * blocks)
-                        above[at + k] = more, equal[at + k] = same;
-                }
-            });
-            __syncthreads();
-            // a wave has a stretch of blocks
-            const int stretch = (blocks + WAVES - 1) / WAVES;
-            const int first = min(wave * stretch, blocks), behind = min(first + stretch, blocks);
-            auto join = [&](int x, int k, int &all) {       // of the waves before this one, and of all
-                if (lane == 0)
-                    of_wave[k][wave] = x;
-                __syncthreads();
-                int s = 0;
-                all = 0;
-                for (int w = 0; w < WAVES; ++w) {
-                    s += w < wave ? of_wave[k][w] : 0;
-                    all += of_wave[k][w];
-                }
-                return s;
-            };
-            int same = 0, all_same, all_holes, all_movers;
-            for (int i = 4 * first + lane; i - lane < 4 * behind; i += 64)
-                same += wave_sum(i < 4 * behind ? __popcll(equal[i]) : 0);
-            int e = join(same, 0, all_same);
-            // what is kept of the last rank joins the others; free places before the end and kept ones behind it are counted
-            int holes = 0, movers = 0;
-            auto lower = [&](unsigned long long x) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(x >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)x, 0u)); };
-            for (int i = first; i < behind; ++i) {
-                unsigned long long m[4], q[4];
-                int rank = e;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    m[k] = above[4 * i + k], q[k] = equal[4 * i + k];
-                    rank += lower(q[k]);
-                    e += __popcll(q[k]);
-                }
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const bool mine = q[k] >> lane & 1;
-                    m[k] |= __ballot(mine && rank < left);
-                    rank += mine;
-                    if (lane == k)
-                        above[4 * i + k] = m[k];
-                    const int j = seg + 256 * i + 4 * lane + k;
-                    const bool kept = m[k] >> lane & 1;
-                    holes += __popcll(__ballot(!kept && j < keep));
-                    movers += __popcll(__ballot(kept && j >= keep));
-                }
-            }
-            int d = at_dst + join(holes, 1, all_holes), s = at_src + join(movers, 2, all_movers);
-            for (int i = first; i < behind; ++i) {
-                const int j = seg + 256 * i + 4 * lane;
-                bool hole[4], mover[4];
-                int to = d, from = s;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const bool kept = above[4 * i + k] >> lane & 1;
-                    hole[k] = !kept && j + k < keep, mover[k] = kept && j + k >= keep;
-                    const unsigned long long x = __ballot(hole[k]), y = __ballot(mover[k]);
-                    to += lower(x), from += lower(y);
-                    d += __popcll(x), s += __popcll(y);
-                }
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (hole[k])
-                        dst[to++] = j + k;
-                    if (mover[k])
-                        src[from++] = j + k;
-                }
-            }
-            at_dst += all_holes, at_src += all_movers, left -= min(left, all_same);
-            __syncthreads();                                // the segment's words have been read
+                held[i][k] = number[k] < p.sinks || number[k] >= late ? kAlways : rank_of(w[k]);
         }
     }
-    for (int i = at_dst + tid; i < p.moves; i += THREADS)
-        dst[i] = src[i] = -1;
+    // f(first place of the lane's four, their ranks), lanes behind hi take part
+    template <typename F>
+    __device__ __forceinline__ void each(int lo, int hi, F f)
+    {
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            if ((lo & ~3) + i * STRIDE < hi)
+                f((lo & ~3) + i * STRIDE + 4 * tid, held[i]);
+    }
+    __device__ __forceinline__ void clear()
+    {
+        for (int i = tid; i < kBins / 4; i += THREADS)
+            reinterpret_cast<i32x4 *>(sh.count)[i] = i32x4{0, 0, 0, 0};
+        __syncthreads();
+    }
+    // counts of a digit among the ranks of [lo, hi) whose bits above it are `top`
+    __device__ __forceinline__ void tally(int pass, uint32_t top, int lo, int hi)
+    {
+        const int shift = digit_shift(pass), bits = digit_bits(pass);
+        const uint32_t known = pass == 0 ? 0u : ~0u << (shift + bits);
+        each(lo, hi, [&](int j, u32x4 r) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const bool mine = j + k >= lo && j + k < hi && (r[k] & known) == top;
+                const int digit = r[k] >> shift & ((1 << bits) - 1);
+                // the first lane counts for all that have its digit: one value may be everywhere
+                const unsigned long long with = __ballot(mine);
+                if (with == 0)
+                    continue;
+                const int lead = __ffsll(with) - 1;
+                const bool same = mine && digit == __builtin_amdgcn_readlane(digit, lead);
+                const unsigned long long all = __ballot(same);
+                if (mine && (!same || lane == lead))
+                    atomicAdd(&sh.count[digit], same ? __popcll(all) : 1);
+            }
+        });
+    }
+    // x of the waves before this one, and of all
+    __device__ __forceinline__ int join(int x, int k, int &all)
+    {
+        if (lane == 0)
+            sh.of_wave[k][wave] = x;
+        __syncthreads();
+        int s = 0;
+        all = 0;
+        for (int w = 0; w < WAVES; ++w) {
+            s += w < wave ? sh.of_wave[k][w] : 0;
+            all += sh.of_wave[k][w];
+        }
+        return s;
+    }
+    // the digit in which the left-th largest lies, by the counts; left: how many of its elements are kept
+    __device__ __forceinline__ int find(int &left)
+    {
+        constexpr int PER = kBins / THREADS;                // from the largest digit down, neighbouring ones to a thread
+        __syncthreads();
+        const int first = kBins - (tid + 1) * PER;
+        int mine = 0, all;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            mine += sh.count[first + i];
+        const int upto = wave_prefix(mine);
+        int before = upto - mine + join(__builtin_amdgcn_readlane(upto, 63), 0, all);
+        if (before < left && left <= before + mine) {
+            int digit = first + PER - 1;
+            while (before + sh.count[digit] < left)
+                before += sh.count[digit--];
+            sh.found[0] = digit, sh.found[1] = left - before;
+        }
+        __syncthreads();
+        const int digit = sh.found[0];
+        left = sh.found[1];
+        __syncthreads();                                    // (before anything of it is written again)
+        return digit;
+    }
+    // The lists' elements of the places [lo, hi): kept are the ranks above top and of those that equal it the first `left`.
+    // at_dst, at_src: elements of the places before; all three go on to what follows.
+    __device__ __forceinline__ void emit(int lo, int hi, uint32_t top, int &left, int &at_dst, int &at_src)
+    {
+        int *const dst = p.dst + row * p.moves, *const src = p.src + row * p.moves;
+        const int seg = lo & ~3, blocks = (hi - seg + 255) / 256;
+        each(lo, hi, [&](int j, u32x4 r) {
+            const int at = (j - seg) / 256 * 4;             // (a wave's 256 places are a block)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const bool there = j + k >= lo && j + k < hi;
+                const unsigned long long more = __ballot(there && r[k] > top), same = __ballot(there && r[k] == top);
+                if (lane == k && at < 4 * blocks)
+                    sh.above[at + k] = more, sh.equal[at + k] = same;
+            }
+        });
+        __syncthreads();
+        // a wave has a stretch of blocks
+        const int stretch = (blocks + WAVES - 1) / WAVES;
+        const int first = min(wave * stretch, blocks), behind = min(first + stretch, blocks);
+        int same = 0, all_same, all_holes, all_movers;
+        for (int i = 4 * first + lane; i - lane < 4 * behind; i += 64)
+            same += wave_sum(i < 4 * behind ? __popcll(sh.equal[i]) : 0);
+        int e = join(same, 0, all_same);
+        // what is kept of the last rank joins the others; free places before the end and kept ones behind it are counted
+        int holes = 0, movers = 0;
+        auto lower = [&](unsigned long long x) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(x >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)x, 0u)); };
+        for (int i = first; i < behind; ++i) {
+            unsigned long long m[4], q[4];
+            int rank = e;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                m[k] = sh.above[4 * i + k], q[k] = sh.equal[4 * i + k];
+                rank += lower(q[k]);
+                e += __popcll(q[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const bool mine = q[k] >> lane & 1;
+                m[k] |= __ballot(mine && rank < left);
+                rank += mine;
+                if (lane == k)
+                    sh.above[4 * i + k] = m[k];
+                const int j = seg + 256 * i + 4 * lane + k;
+                const bool kept = m[k] >> lane & 1;
+                holes += __popcll(__ballot(!kept && j >= lo && j < min(hi, keep)));
+                movers += __popcll(__ballot(kept && j >= keep));
+            }
+        }
+        int d = at_dst + join(holes, 1, all_holes), s = at_src + join(movers, 2, all_movers);
+        for (int i = first; i < behind; ++i) {
+            const int j = seg + 256 * i + 4 * lane;
+            bool hole[4], mover[4];
+            int to = d, from = s;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const bool kept = sh.above[4 * i + k] >> lane & 1;
+                hole[k] = !kept && j + k >= lo && j + k < min(hi, keep), mover[k] = kept && j + k >= keep;
+                const unsigned long long x = __ballot(hole[k]), y = __ballot(mover[k]);
+                to += lower(x), from += lower(y);
+                d += __popcll(x), s += __popcll(y);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (hole[k])
+                    dst[to++] = j + k;
+                if (mover[k])
+                    src[from++] = j + k;
+            }
+        }
+        at_dst += all_holes, at_src += all_movers, left -= min(left, all_same);
+        __syncthreads();                                    // the words have been read
+    }
+    // the elements of the lists from n on
+    __device__ __forceinline__ void fill(int n, int part, int parts)
+    {
+        int *const dst = p.dst + row * p.moves, *const src = p.src + row * p.moves;
+        for (long long i = (long long)n + part * THREADS + tid; i < p.moves; i += (long long)parts * THREADS)
+            dst[i] = src[i] = -1;
+    }
+};
+
+// A list to a workgroup.
+__global__ __launch_bounds__(kSelectThreads) void attn_select_kernel(const SelectParams p)
+{
+    __shared__ SelectShared<kSelectThreads> sh;
+    SelectList<kSelectThreads> l(p, sh, blockIdx.x);
+    if (l.h == 0 && l.tid == 0)
+        p.new_len[l.b] = l.new_len();
+    int at_dst = 0, at_src = 0;
+    if (!l.whole) {
+        l.read(0, l.kv);
+        uint32_t top = 0;
+        int left = l.keep;
+#pragma unroll 1
+        for (int pass = 0; pass < 3; ++pass) {
+            l.clear();
+            l.tally(pass, top, 0, l.kv);
+            top |= (uint32_t)l.find(left) << digit_shift(pass);
+        }
+        l.emit(0, l.kv, top, left, at_dst, at_src);
+    }
+    l.fill(at_dst, 0, 1);
+}
+
+// The parts of a list: [0, keep) in stretches of part_places, then [keep, kv) in stretches that begin at a multiple of four.
+struct SelectPart {
+    int below, all;                     // parts before keep, and of the list
+    __device__ __forceinline__ SelectPart(const SelectParams &p, int kv, int keep)
+    {
+        below = (keep + p.part_places - 1) / p.part_places;
+        all = below + (kv - (keep & ~3) + p.part_places - 1) / p.part_places;
+    }
+    __device__ __forceinline__ int lo(const SelectParams &p, int keep, int i) const
+    {
+        return i < below ? i * p.part_places : max(keep, (keep & ~3) + (i - below) * p.part_places);
+    }
+    __device__ __forceinline__ int hi(const SelectParams &p, int kv, int keep, int i) const
+    {
+        return i < below ? min((i + 1) * p.part_places, keep) : min((keep & ~3) + (i - below + 1) * p.part_places, kv);
+    }
+};
+
+// One of four launches over the parts of the lists.  Launch 0 counts the first digit; 1 and 2 add up the parts' counts of the digit
+// before and count the next one; 3 adds up the last ones and writes the lists.
+template <int PASS>
+__global__ __launch_bounds__(kPartThreads) void attn_select_part_kernel(const SelectParams p)
+{
+    __shared__ SelectShared<kPartThreads> sh;
+    const int list = quotient((int)blockIdx.x, p.parts), part = blockIdx.x - list * p.parts;
+    SelectList<kPartThreads> l(p, sh, list);
+    if (l.whole) {
+        if (PASS == 3) {
+            if (l.h == 0 && part == 0 && l.tid == 0)
+                p.new_len[l.b] = l.new_len();
+            l.fill(0, part, p.parts);
+        }
+        return;
+    }
+    const SelectPart parts(p, l.kv, l.keep);
+    if (part >= parts.all)
+        return;
+    const int lo = parts.lo(p, l.keep, part), hi = parts.hi(p, l.kv, l.keep, part);
+    uint32_t top = 0;
+    int left = l.keep;
+    int *const kept = p.kept + (size_t)list * p.parts;
+    if constexpr (PASS > 0) {
+        if (PASS > 1) {
+            const int2 known = p.known[(size_t)(PASS - 2) * gridDim.x / p.parts + list];
+            top = (uint32_t)known.x, left = known.y;
+        }
+        const int *const counts = p.counts[PASS - 1] + (size_t)list * p.parts * kBins;
+        for (int i = l.tid; i < kBins / 4; i += kPartThreads) {
+            i32x4 sum = {0, 0, 0, 0};
+            for (int k = 0; k < parts.all; ++k)
+                sum += *reinterpret_cast<const i32x4 *>(counts + (size_t)k * kBins + 4 * i);
+            reinterpret_cast<i32x4 *>(sh.count)[i] = sum;
+        }
+        const int digit = l.find(left);
+        top |= (uint32_t)digit << digit_shift(PASS - 1);
+        if (PASS < 3) {
+            if (part == 0 && l.tid == 0)
+                p.known[(size_t)(PASS - 1) * gridDim.x / p.parts + list] = int2{(int)top, left};
+            // this part's ranks above the digit are kept
+            int more = 0, all;
+            for (int i = l.tid; i < kBins; i += kPartThreads)
+                more += i > digit ? counts[(size_t)part * kBins + i] : 0;
+            l.join(wave_sum(more), 1, all);
+            if (l.tid == 0)
+                kept[part] = (PASS > 1 ? kept[part] : 0) + all;
+        } else {
+            // kept ones of every part: so far, above the last digit, and of those that equal it as many as the parts before leave
+            int *const of_part = reinterpret_cast<int *>(sh.above), *const same = of_part + kMostParts + 2;
+            for (int k = l.wave; k < parts.all; k += kPartThreads / 64) {
+                int more = 0;
+                for (int i = l.lane; i < kBins; i += 64)
+                    more += i > digit ? counts[(size_t)k * kBins + i] : 0;
+                more = wave_sum(more);
+                if (l.lane == 0)
+                    of_part[k] = kept[k] + more, same[k] = counts[(size_t)k * kBins + digit];
+            }
+            __syncthreads();
+            int at_dst = 0, at_src = 0, all = 0, of_last = left;
+            for (int k = 0; k < parts.all; ++k) {
+                const int taken = min(of_last, same[k]), n = of_part[k] + taken;
+                const int holes = k < parts.below ? parts.hi(p, l.kv, l.keep, k) - parts.lo(p, l.keep, k) - n : 0;
+                if (k < part)
+                    at_dst += holes, at_src += k < parts.below ? 0 : n, left -= taken;
+                of_last -= taken, all += holes;
+            }
+            __syncthreads();                                // (the words are written again)
+            if (l.h == 0 && part == 0 && l.tid == 0)
+                p.new_len[l.b] = l.new_len();
+            for (int from = lo; from < hi;) {
+                const int upto = min((from & ~3) + kPartChunk, hi);
+                l.read(from, upto);
+                l.emit(from, upto, top, left, at_dst, at_src);
+                from = upto;
+            }
+            l.fill(all, part, parts.all);
+            return;
+        }
+        __syncthreads();                                    // the sums have been read
+    }
+    l.clear();
+    for (int from = lo; from < hi;) {
+        const int upto = min((from & ~3) + kPartChunk, hi);
+        l.read(from, upto);
+        l.tally(PASS, top, from, upto);
+        from = upto;
+    }
+    __syncthreads();
+    int *const mine = p.counts[PASS < 3 ? PASS : 0] + ((size_t)list * p.parts + part) * kBins;
+    for (int i = l.tid; i < kBins / 4; i += kPartThreads)
+        reinterpret_cast<i32x4 *>(mine)[i] = reinterpret_cast<const i32x4 *>(sh.count)[i];
+}
+
+// Sizes of a call: parts of a list, places of a part, bytes of workspace.
+struct SelectSizes {
+    int parts, part_places;
+    long long bytes;
+};
+inline SelectSizes select_sizes(int B, int H_kv, int width)
+{
+    SelectSizes s = {1, kPartChunk, 0};
+    if (width > kSelectWhole) {
+        const long long chunks = ((long long)width + kPartChunk - 1) / kPartChunk;
+        s.part_places = (int)((chunks + kMostParts - 1) / kMostParts * kPartChunk);
+        s.parts = (int)(((long long)width + s.part_places - 1) / s.part_places) + 2;      // (both stretches may end in a short one)
+        s.bytes = (long long)B * H_kv * ((3LL * kBins + 1) * s.parts * 4 + 2 * (long long)sizeof(int2));
+        s.bytes = (s.bytes + 15) / 16 * 16;
+    }
+    return s;
 }
 
 struct MoveParams {
@@ -273,7 +438,7 @@ constexpr int kMoveTogether = 128;      // elements of a list that are read befo
 
 // One list, or 64 elements of a longer one, of a sequence and key head; blockIdx.y: keys or values.  RB: bytes of a row.
 template <int RB>
-__global__ __launch_bounds__(256) void attn_move_kernel(const MoveParams p, int parts)
+__global__ __launch_bounds__(256, RB == 512 ? 4 : 6) void attn_move_kernel(const MoveParams p, int parts)
 {
     constexpr int LPR = RB / 16, RPP = 256 / LPR, N = kMoveTogether / RPP;    // lanes of a row, rows of a pass, passes
     const int w = blockIdx.y, tid = threadIdx.x;
@@ -355,9 +520,16 @@ int launch_move(const attn::MoveParams &p, hipStream_t st)
 
 }  // namespace
 
+extern "C" long long attn_cache_select_workspace_bytes(int B, int H_kv, int width)
+{
+    if (B < 1 || H_kv < 1 || width < 1 || width % 16 || width > (1 << 30) || (long long)B * H_kv >= 1 << 22)
+        return -1;
+    return attn::select_sizes(B, H_kv, width).bytes;
+}
+
 extern "C" int attn_cache_select(const float *weights, const int *stamps, const int *seen, const int *kv_len, const int *keep,
-                                 int *dst, int *src, int *new_len, int sinks, int recent, int B, int H_kv, int width,
-                                 int moves_width, void *stream)
+                                 int *dst, int *src, int *new_len, int sinks, int recent, void *workspace, long long workspace_bytes,
+                                 int B, int H_kv, int width, int moves_width, void *stream)
 {
     if (!weights || !kv_len || !keep || !dst || !src || !new_len || !stamps != !seen)
         return ATTN_ERR_NULL;
@@ -370,21 +542,37 @@ extern "C" int attn_cache_select(const float *weights, const int *stamps, const 
     for (const int *p : {kv_len, keep, seen})
         if (p && (uintptr_t)new_len < (uintptr_t)(p + B) && (uintptr_t)p < (uintptr_t)(new_len + B))
             return ATTN_ERR_SHAPE;
+    const attn::SelectSizes s = attn::select_sizes(B, H_kv, width);
+    const long long lists = (long long)B * H_kv, groups = lists * s.parts;
+    if (groups > attn::most_workgroups(attn::kPartThreads) || lists > attn::most_workgroups(attn::kSelectThreads))
+        return ATTN_ERR_SHAPE;
+    if (s.bytes && !workspace)
+        return ATTN_ERR_NULL;
     if (misaligned(weights, 16) || misaligned(stamps, 16) || misaligned(seen, 4) || misaligned(kv_len, 4) || misaligned(keep, 4) ||
-        misaligned(dst, 4) || misaligned(src, 4) || misaligned(new_len, 4))
+        misaligned(dst, 4) || misaligned(src, 4) || misaligned(new_len, 4) || (s.bytes && misaligned(workspace, 16)))
         return ATTN_ERR_ALIGN;
+    if (workspace_bytes < s.bytes)
+        return ATTN_ERR_WORKSPACE;
     attn::SelectParams p;
     p.weights = weights, p.stamps = stamps, p.seen = seen, p.kv_len = kv_len, p.keep = keep;
     p.dst = dst, p.src = src, p.new_len = new_len;
     p.sinks = sinks, p.recent = recent, p.B = B, p.H_kv = H_kv, p.width = width, p.moves = moves_width;
+    p.parts = s.parts, p.part_places = s.part_places;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const dim3 grid((unsigned)(B * H_kv));
-    if (width <= attn::SelectTiling<256, 8>::SEGMENT)
-        hipLaunchKernelGGL((attn::attn_select_kernel<256, 8>), grid, dim3(256), 0, st, p);
-    else if (width <= attn::SelectTiling<1024, 8>::SEGMENT)
-        hipLaunchKernelGGL((attn::attn_select_kernel<1024, 8>), grid, dim3(1024), 0, st, p);
-    else
-        hipLaunchKernelGGL((attn::attn_select_kernel<1024, 0>), grid, dim3(1024), 0, st, p);
+    if (s.bytes == 0) {
+        hipLaunchKernelGGL(attn::attn_select_kernel, dim3((unsigned)lists), dim3(attn::kSelectThreads), 0, st, p);
+        return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH;
+    }
+    int *const ws = static_cast<int *>(workspace);
+    for (int i = 0; i < 3; ++i)
+        p.counts[i] = ws + i * groups * attn::kBins;
+    p.known = reinterpret_cast<int2 *>(ws + 3 * groups * attn::kBins);
+    p.kept = reinterpret_cast<int *>(p.known + 2 * lists);
+    const dim3 grid((unsigned)groups), block(attn::kPartThreads);
+    hipLaunchKernelGGL((attn::attn_select_part_kernel<0>), grid, block, 0, st, p);
+    hipLaunchKernelGGL((attn::attn_select_part_kernel<1>), grid, block, 0, st, p);
+    hipLaunchKernelGGL((attn::attn_select_part_kernel<2>), grid, block, 0, st, p);
+    hipLaunchKernelGGL((attn::attn_select_part_kernel<3>), grid, block, 0, st, p);
     return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH;
 }
 

@@ -559,14 +559,16 @@ typedef int (*TreeFn)(const void *, const long long *, void *, float *, const vo
 typedef int (*WeighFn)(const void *, const long long *, const float *, const void *, const unsigned char *, const int *, const int *,
                        const int *, int, const float *, float *, int *, const int *, float, int, int, int, int, int, int, int, int,
                        int, int, float, void *);
-typedef int (*SelectFn)(const float *, const int *, const int *, const int *, const int *, int *, int *, int *, int, int, int, int,
-                        int, int, void *);
+typedef int (*SelectFn)(const float *, const int *, const int *, const int *, const int *, int *, int *, int *, int, int, void *,
+                        long long, int, int, int, int, void *);
+typedef long long (*SelectWsFn)(int, int, int);
 typedef int (*MoveFn)(void *, void *, unsigned char *, unsigned char *, const int *, const int *, const int *, int, float *, int *,
                       int, int, int, int, int, int, int, int, void *);
 
 TreeFn g_tree[2];
 WeighFn g_weigh[2];
 SelectFn g_select;
+SelectWsFn g_select_ws;
 MoveFn g_move;
 
 // tree(type, q, k_pages, v_pages, page_table, start, kv_len, mask, k_scale, v_scale, o, lse, workspace, scale, max_q, stream)
@@ -695,15 +697,15 @@ bool int_output(PyObject *given, at::IntArrayRef shape, const at::Tensor &like, 
     return true;
 }
 
-// select(weights, kv_len, keep, max_moves, stamps, seen, sinks, recent, dst, src, new_len, stream) -> (dst, src, new_len)
+// select(weights, kv_len, keep, max_moves, stamps, seen, sinks, recent, dst, src, new_len, workspace, stream) -> (dst, src, new_len)
 PyObject *py_select(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
-    const at::Tensor *w = n == 12 ? plain(a[0], at::kFloat, 3) : nullptr;
+    const at::Tensor *w = n == 13 ? plain(a[0], at::kFloat, 3) : nullptr;
     int moves, sinks, recent;
     void *stream;
-    if (!w || !g_select || !int_of(a[3], moves) || !int_of(a[6], sinks) || !int_of(a[7], recent) || moves < 1 ||
-        !stream_of(a[11], w->device(), any_none(a + 8, 3), stream))
+    if (!w || !g_select || !g_select_ws || !int_of(a[3], moves) || !int_of(a[6], sinks) || !int_of(a[7], recent) || moves < 1 ||
+        !stream_of(a[12], w->device(), any_none(a + 8, 4), stream))
         Py_RETURN_NONE;
     const int64_t B = w->size(0), H = w->size(1), width = w->size(2);
     if (B < 1 || H < 1 || width < 1 || B > INT_MAX || H > INT_MAX || width > INT_MAX)
@@ -711,14 +713,28 @@ PyObject *py_select(PyObject *, PyObject *const *a, Py_ssize_t n)
     const int64_t seqs[1] = {B}, lists[3] = {B, H, moves};
     const c10::Device dev = w->device();
     int *kv_len, *keep, *stamps, *seen;
-    at::Tensor dst, src, len;
+    at::Tensor dst, src, len, ws;
+    const long long need = g_select_ws((int)B, (int)H, (int)width);
+    if (need < 0)
+        Py_RETURN_NONE;
+    if (a[11] != Py_None) {
+        if (!THPVariable_CheckExact(a[11]))
+            Py_RETURN_NONE;
+        ws = THPVariable_Unpack(a[11]);
+        if (!plain(a[11], ws.scalar_type(), 0) || ws.device() != dev)
+            Py_RETURN_NONE;
+    }
     if (!array_or_none(a[1], at::kInt, seqs, dev, false, kv_len) || !array_or_none(a[2], at::kInt, seqs, dev, false, keep) ||
         !array_or_none(a[4], at::kInt, w->sizes(), dev, true, stamps) || !array_or_none(a[5], at::kInt, seqs, dev, true, seen) ||
         !stamps != !seen || !int_output(a[8], lists, *w, dst) || !int_output(a[9], lists, *w, src) || !int_output(a[10], seqs, *w, len))
         Py_RETURN_NONE;
+    if (!ws.defined() && need > 0)
+        ws = allocate([&] { return at::empty({need}, w->options().dtype(at::kByte)); });
+    void *const ws_at = ws.defined() ? ws.data_ptr() : nullptr;
+    const long long ws_bytes = ws.defined() ? (long long)ws.nbytes() : 0;
     const int rc = launch(dev, [&] {
         return g_select((const float *)w->data_ptr(), stamps, seen, kv_len, keep, (int *)dst.data_ptr(), (int *)src.data_ptr(),
-                        (int *)len.data_ptr(), sinks, recent, (int)B, (int)H, (int)width, moves, stream);
+                        (int *)len.data_ptr(), sinks, recent, ws_at, ws_bytes, (int)B, (int)H, (int)width, moves, stream);
     });
     return rc ? PyLong_FromLong(rc) : pack({&dst, &src, &len});
     END_HANDLE_TH_ERRORS
@@ -762,15 +778,16 @@ PyObject *py_move(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// set_eviction_entries(addresses of paged_tree and cache_weigh, bf16 and fp16 of each, cache_select and cache_move)
+// set_eviction_entries(addresses of paged_tree and cache_weigh, bf16 and fp16 of each, cache_select, cache_move and the workspace size of
+// the last but one)
 PyObject *py_set_eviction_entries(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    void *p[6];
-    if (n != 6) {
-        PyErr_SetString(PyExc_TypeError, "set_eviction_entries takes six addresses");
+    void *p[7];
+    if (n != 7) {
+        PyErr_SetString(PyExc_TypeError, "set_eviction_entries takes seven addresses");
         return nullptr;
     }
-    for (int i = 0; i < 6; ++i)
+    for (int i = 0; i < 7; ++i)
         p[i] = PyLong_AsVoidPtr(a[i]);
     if (PyErr_Occurred())
         return nullptr;
@@ -780,6 +797,7 @@ PyObject *py_set_eviction_entries(PyObject *, PyObject *const *a, Py_ssize_t n)
     }
     g_select = (SelectFn)p[4];
     g_move = (MoveFn)p[5];
+    g_select_ws = (SelectWsFn)p[6];
     Py_RETURN_NONE;
 }
 

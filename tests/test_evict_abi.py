@@ -9,7 +9,7 @@ WEIGH = [("q", OK), ("strides", arr([512, 64])), ("lse", OK), ("k_pages", OK), (
          ("kind", 1), ("weights", OK), ("out", OK), ("stamps", OK), ("seen", OK), ("decay", 1.0), ("max_q", 1), ("T", 3), ("B", 2),
          ("H_q", 4), ("H_kv", 2), ("D", 64), ("n_pages", 9), ("page_size", 16), ("width", 4), ("causal", 1), ("scale", 0.125), ("stream", 0)]
 SELECT = [("weights", OK), ("stamps", OK), ("seen", OK), ("kv_len", OK), ("keep", OK), ("dst", OK), ("src", OK), ("new_len", FAR),
-          ("sinks", 0), ("recent", 0), ("B", 2), ("H_kv", 2), ("width", 64), ("moves", 8), ("stream", 0)]
+          ("sinks", 0), ("recent", 0), ("ws", OK), ("ws_bytes", 1 << 50), ("B", 2), ("H_kv", 2), ("width", 64), ("moves", 8), ("stream", 0)]
 MOVE = [("k_pages", OK), ("v_pages", OK), ("k_scale", OK), ("v_scale", OK), ("table", OK), ("dst", OK), ("src", OK), ("kind", 1),
         ("weights", OK), ("stamps", OK), ("heads", 2), ("moves", 8), ("B", 2), ("H_kv", 2), ("D", 64), ("n_pages", 9), ("page_size", 16),
         ("width", 4), ("stream", 0)]
@@ -70,6 +70,14 @@ def test_select_refusals(b):  # noqa: F811
     for n in ("seen", "kv_len", "keep", "dst", "src"):
         assert f(**{n: OK + 2}) == b.ATTN_ERR_ALIGN
     assert f(new_len=FAR + 2) == b.ATTN_ERR_ALIGN
+    need = b.attn_cache_select_workspace_bytes
+    assert need(2, 2, 8192) == 0 and f(ws=None, ws_bytes=0, dst=OK + 2) == b.ATTN_ERR_ALIGN
+    assert need(2, 2, 8208) > 0 and need(2, 2, 8208) % 16 == 0
+    assert f(width=8208, ws=None) == b.ATTN_ERR_NULL and f(width=8208, ws=OK + 8) == b.ATTN_ERR_ALIGN
+    assert f(width=8208, ws_bytes=need(2, 2, 8208) - 1) == b.ATTN_ERR_WORKSPACE
+    for bad in ((0, 2, 64), (2, 0, 64), (2, 2, 0), (2, 2, 24), (2, 2, (1 << 30) + 16), (1 << 21, 2, 64)):
+        assert need(*bad) == -1
+    assert f(B=1 << 20, width=1 << 17) == b.ATTN_ERR_SHAPE                        # 2^24 workgroups of 512 threads
 
 
 def test_move_refusals(b):  # noqa: F811

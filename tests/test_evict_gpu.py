@@ -73,6 +73,38 @@ def test_select_of_long_sequences():
     run_select(M, w, i32([131072, 100001]), i32([8192, 65000]), 40000, sinks=4, recent=1000)
 
 
+@pytest.mark.parametrize("kind", ["spread", "few", "special"])
+@pytest.mark.parametrize("width, kvs, keeps", [
+    (8208, [8208, 8193, 5000, 8208], [100, 8192, 4999, 8207]), (16400, [16400, 16385, 16384, 20], [8001, 16384, 1, 7]),
+    (50000, [50000, 49153, 33000, 50000], [32768, 16383, 16385, 3])])
+def test_select_of_lists_in_parts(width, kvs, keeps, kind):
+    """Ends at, before and behind the borders of the parts, which begin anew at the new length."""
+    from paper_2512_18134_amd import binding as M
+    gen = torch.Generator().manual_seed(width)
+    w = torch.randn((4, 1, width), generator=gen).mul(2).exp() * 1e-3
+    if kind == "few":
+        w = torch.randint(0, 3, w.shape, generator=gen).float()
+    elif kind == "special":
+        for x in (math.inf, math.nan, -1.0, 0.0):
+            w[torch.rand(w.shape, generator=gen) < 0.2] = x
+    moves = max(min(k, kv - k) for k, kv in zip(keeps, kvs))
+    run_select(M, w, i32(kvs), i32(keeps), moves, sinks=3, recent=50)
+    stamps = torch.stack([torch.randperm(width + 9, generator=gen)[:width] for _ in range(4)]).view(4, 1, width).to(torch.int32)
+    run_select(M, w, i32(kvs), i32(keeps), moves // 2, stamps, i32([width + 9] * 4), sinks=100, recent=1000)
+
+
+def test_select_in_a_given_workspace_that_holds_something_else():
+    from paper_2512_18134_amd import binding as M
+    gen = torch.Generator().manual_seed(8)
+    w = torch.rand((2, 2, 20000), generator=gen)
+    need = M.attn_cache_select_workspace_bytes(2, 2, 20000)
+    ws = torch.full((need,), 0xff, dtype=torch.uint8, device="cuda")
+    for _ in range(2):
+        got = M.attn_cache_select(w.cuda(), i32([20000, 9000]).cuda(), i32([500, 8000]).cuda(), 1000, workspace=ws)
+        for g, want in zip(got, E.select(w, i32([20000, 9000]), i32([500, 8000]), 1000)):
+            assert torch.equal(g.cpu(), want)
+
+
 def dirty(c):
     """Every place holds something of its own."""
     for i in range(2):
