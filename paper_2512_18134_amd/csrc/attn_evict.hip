@@ -2,8 +2,8 @@
 // (include/attn_evict.h).
 //
 // Select: the keep-th largest weight is found digit by digit (11, 11 and 10 bits of the order-preserving integer of a float) from counts
-// in LDS, which no order of additions can change; the outcome is left as bits, from which the places' numbers in the lists are
-// counted.  Up to kSelectWhole places a workgroup has a list, its ranks in registers from the first reading on.  Longer ones
+// in LDS, which no order of additions can change; what a wave has
+// of free and of kept places is then counted, and the lists are written in the places' order.  Up to kSelectWhole places a workgroup has a list, its ranks in registers from the first reading on.  Longer ones
 // are shared out to workgroups, in four launches: a digit's counts of every part, which the next launch adds up.  (One workgroup is bound
 // by its vector unit, some 25 instructions for each place and digit: 131072 places in 150 us.)
 //
@@ -34,11 +34,12 @@ struct SelectParams {
     int *kept;                          // [lists][parts]: kept ones that are known so far
 };
 
-// Floats in the order of unsigned integers: NaN below everything, the zeros alike.
-__device__ __forceinline__ uint32_t rank_of(float x)
+// Floats, by their bits, in the order of unsigned integers: NaN below everything, the zeros alike.
+__device__ __forceinline__ uint32_t rank_of(uint32_t x)
 {
-    const uint32_t bits = __builtin_bit_cast(uint32_t, x + 0.f);
-    return x != x ? 0u : bits >> 31 ? ~bits : bits | 0x80000000u;
+    const float f = __builtin_bit_cast(float, x) + 0.f;
+    const uint32_t bits = __builtin_bit_cast(uint32_t, f);
+    return f != f ? 0u : bits ^ ((uint32_t)((int)bits >> 31) | 0x80000000u);
 }
 constexpr uint32_t kAlways = 0xffffffffu;                   // above the rank of +infinity
 
@@ -50,16 +51,16 @@ constexpr int digit_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0
 
 constexpr int kHeld = 8;                // vectors of four ranks that a thread holds
 constexpr int kSelectThreads = 256, kSelectWhole = kSelectThreads * 4 * kHeld;
+static_assert(kBins == 4 * 512, "a thread of a part has four bins");
 constexpr int kPartThreads = 512, kPartChunk = kPartThreads * 4 * kHeld, kMostParts = 64;
 
 // What a workgroup shares.
 template <int THREADS>
 struct SelectShared {
-    static constexpr int PLACES = THREADS * 4 * kHeld;
     __attribute__((aligned(16))) int count[kBins];
-    // of every 256 places four words: bit l of word k is place 4 l + k, kept in any case and as one of the last rank
-    unsigned long long above[PLACES / 64], equal[PLACES / 64];
-    int of_wave[3][THREADS / 64];
+    int of_wave[2][THREADS / 64];
+    int of_vector[3][kHeld * THREADS / 64];                // of a wave's part of a vector: equal ranks, free places, kept ones behind
+    int of_part[2][kMostParts + 2];
     int found[2];
 };
 
@@ -87,24 +88,45 @@ struct SelectList {
     }
     __device__ __forceinline__ int new_len() const { return min(keep, kv - keep) > p.moves ? kv : keep; }
 
-    // ranks of the places [lo, hi), no more than PLACES from lo & ~3 on
-    __device__ __forceinline__ void read(int lo, int hi)
+    // Ranks of the places [lo, hi), no more than a vector of four for each of the kHeld turns from lo & ~3 on: asked for (all on their way
+    // before the first is looked at; behind hi the last ones once more), and made.  seen: the sequence's, if there are stamps
+    i32x4 number[kHeld];
+    int seen;
+    __device__ __forceinline__ void ask(int lo, int hi)
     {
         const float *const weights = p.weights + row * p.width;
-        const int *const stamps = p.stamps ? p.stamps + row * p.width : nullptr;
-        const long long late = (long long)(p.stamps ? p.seen[b] : kv) - p.recent;
+        const int base = (lo & ~3) + 4 * tid, last = (hi - 1) & ~3;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            if ((lo & ~3) + i * STRIDE < hi)
+                held[i] = *reinterpret_cast<const u32x4 *>(weights + min(base + i * STRIDE, last));
+        if (p.stamps) {
+            const int *const stamps = p.stamps + row * p.width;
+            seen = p.seen[b];
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i)
+                if ((lo & ~3) + i * STRIDE < hi)
+                    number[i] = *reinterpret_cast<const i32x4 *>(stamps + min(base + i * STRIDE, last));
+        }
+    }
+    __device__ __forceinline__ void make(int lo)
+    {
+        const long long late = (long long)(p.stamps ? seen : kv) - p.recent;
 #pragma unroll
         for (int i = 0; i < kHeld; ++i) {
-            const int j = (lo & ~3) + i * STRIDE + 4 * tid;
-            if (j >= hi)                                    // (rows are a multiple of four long)
-                continue;
-            const f32x4 w = *reinterpret_cast<const f32x4 *>(weights + j);
-            i32x4 number = {j, j + 1, j + 2, j + 3};
-            if (stamps)
-                number = *reinterpret_cast<const i32x4 *>(stamps + j);
+            const int j = (lo & ~3) + 4 * tid + i * STRIDE, of_wave = __builtin_amdgcn_readfirstlane(j);   // first place of the wave
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                held[i][k] = number[k] < p.sinks || number[k] >= late ? kAlways : rank_of(w[k]);
+                held[i][k] = rank_of(held[i][k]);
+            if (p.stamps) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    held[i][k] = number[i][k] < p.sinks || number[i][k] >= late ? kAlways : held[i][k];
+            } else if (of_wave < p.sinks || of_wave + 255 >= late) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    held[i][k] = j + k < p.sinks || j + k >= late ? kAlways : held[i][k];
+            }
         }
     }
     // f(first place of the lane's four, their ranks), lanes behind hi take part
@@ -131,16 +153,9 @@ struct SelectList {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const bool mine = j + k >= lo && j + k < hi && (r[k] & known) == top;
-                const int digit = r[k] >> shift & ((1 << bits) - 1);
-                // the first lane counts for all that have its digit: one value may be everywhere
-                const unsigned long long with = __ballot(mine);
-                if (with == 0)
-                    continue;
-                const int lead = __ffsll(with) - 1;
-                const bool same = mine && digit == __builtin_amdgcn_readlane(digit, lead);
-                const unsigned long long all = __ballot(same);
-                if (mine && (!same || lane == lead))
-                    atomicAdd(&sh.count[digit], same ? __popcll(all) : 1);
+                // (one value everywhere: 64 additions to one place, some 7 us of a part of 16384)
+                if (mine)
+                    atomicAdd(&sh.count[r[k] >> shift & ((1 << bits) - 1)], 1);
             }
         });
     }
@@ -182,78 +197,83 @@ struct SelectList {
         __syncthreads();                                    // (before anything of it is written again)
         return digit;
     }
-    // The lists' elements of the places [lo, hi): kept are the ranks above top and of those that equal it the first `left`.
-    // at_dst, at_src: elements of the places before; all three go on to what follows.
+    // The lists' elements of the places [lo, hi), whose ranks are held: kept are the ranks above top, and of those that equal it the first
+    // `left`.  at_dst, at_src: elements of the places before; all three go on to what follows.  What a wave's part of a vector holds is
+    // counted, summed in the order of the places, and written.
     __device__ __forceinline__ void emit(int lo, int hi, uint32_t top, int &left, int &at_dst, int &at_src)
     {
+        constexpr int N = kHeld * WAVES;
+        static_assert(N <= 64, "a lane to a wave's part of a vector");
         int *const dst = p.dst + row * p.moves, *const src = p.src + row * p.moves;
-        const int seg = lo & ~3, blocks = (hi - seg + 255) / 256;
-        each(lo, hi, [&](int j, u32x4 r) {
-            const int at = (j - seg) / 256 * 4;             // (a wave's 256 places are a block)
+        auto lower = [](unsigned long long x) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(x >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)x, 0u)); };
+        // x of the parts before part i of this wave (lane i * WAVES + wave has it), and of all
+        auto sums = [&](int k, int &all) {
+            const int x = lane < N ? sh.of_vector[k][lane] : 0, upto = wave_prefix(x);
+            all = __builtin_amdgcn_readlane(upto, 63);
+            return upto - x;
+        };
+        int n_same[kHeld], all_same;
+        each(lo, hi, [&, i = 0](int j, u32x4 r) mutable {
+            int n = 0;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const bool there = j + k >= lo && j + k < hi;
-                const unsigned long long more = __ballot(there && r[k] > top), same = __ballot(there && r[k] == top);
-                if (lane == k && at < 4 * blocks)
-                    sh.above[at + k] = more, sh.equal[at + k] = same;
-            }
+            for (int k = 0; k < 4; ++k)
+                n += __popcll(__ballot(j + k >= lo && j + k < hi && r[k] == top));
+            n_same[i++] = n;
         });
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            if (lane == 0)
+                sh.of_vector[0][i * WAVES + wave] = (lo & ~3) + i * STRIDE < hi ? n_same[i] : 0;
         __syncthreads();
-        // a wave has a stretch of blocks
-        const int stretch = (blocks + WAVES - 1) / WAVES;
-        const int first = min(wave * stretch, blocks), behind = min(first + stretch, blocks);
-        int same = 0, all_same, all_holes, all_movers;
-        for (int i = 4 * first + lane; i - lane < 4 * behind; i += 64)
-            same += wave_sum(i < 4 * behind ? __popcll(sh.equal[i]) : 0);
-        int e = join(same, 0, all_same);
-        // what is kept of the last rank joins the others; free places before the end and kept ones behind it are counted
-        int holes = 0, movers = 0;
-        auto lower = [&](unsigned long long x) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(x >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)x, 0u)); };
-        for (int i = first; i < behind; ++i) {
-            unsigned long long m[4], q[4];
-            int rank = e;
+        const int before_same = sums(0, all_same);
+        uint32_t hole = 0, mover = 0;                       // bit 4 i + k
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                m[k] = sh.above[4 * i + k], q[k] = sh.equal[4 * i + k];
-                rank += lower(q[k]);
-                e += __popcll(q[k]);
-            }
+        for (int i = 0; i < kHeld; ++i) {
+            int holes = 0, movers = 0;
+            if ((lo & ~3) + i * STRIDE < hi) {
+                const int j = (lo & ~3) + i * STRIDE + 4 * tid;
+                bool same[4];
+                int rank = __builtin_amdgcn_readlane(before_same, i * WAVES + wave);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const bool mine = q[k] >> lane & 1;
-                m[k] |= __ballot(mine && rank < left);
-                rank += mine;
-                if (lane == k)
-                    sh.above[4 * i + k] = m[k];
-                const int j = seg + 256 * i + 4 * lane + k;
-                const bool kept = m[k] >> lane & 1;
-                holes += __popcll(__ballot(!kept && j >= lo && j < min(hi, keep)));
-                movers += __popcll(__ballot(kept && j >= keep));
+                for (int k = 0; k < 4; ++k) {
+                    same[k] = j + k >= lo && j + k < hi && held[i][k] == top;
+                    rank += lower(__ballot(same[k]));
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const bool there = j + k >= lo && j + k < hi;
+                    const bool kept = there && (held[i][k] > top || (same[k] && rank < left));
+                    rank += same[k];
+                    const bool x = there && !kept && j + k < keep, y = kept && j + k >= keep;
+                    hole |= (uint32_t)x << (4 * i + k), mover |= (uint32_t)y << (4 * i + k);
+                    holes += __popcll(__ballot(x)), movers += __popcll(__ballot(y));
+                }
             }
+            if (lane == 0)
+                sh.of_vector[1][i * WAVES + wave] = holes, sh.of_vector[2][i * WAVES + wave] = movers;
         }
-        int d = at_dst + join(holes, 1, all_holes), s = at_src + join(movers, 2, all_movers);
-        for (int i = first; i < behind; ++i) {
-            const int j = seg + 256 * i + 4 * lane;
-            bool hole[4], mover[4];
-            int to = d, from = s;
+        __syncthreads();
+        int all_holes, all_movers;
+        const int before_holes = sums(1, all_holes), before_movers = sums(2, all_movers);
+        auto write = [&](int *list, uint32_t which, int before) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const bool kept = sh.above[4 * i + k] >> lane & 1;
-                hole[k] = !kept && j + k >= lo && j + k < min(hi, keep), mover[k] = kept && j + k >= keep;
-                const unsigned long long x = __ballot(hole[k]), y = __ballot(mover[k]);
-                to += lower(x), from += lower(y);
-                d += __popcll(x), s += __popcll(y);
-            }
+            for (int i = 0; i < kHeld; ++i) {
+                if (__ballot(which >> (4 * i) & 15) == 0)
+                    continue;
+                int at = __builtin_amdgcn_readlane(before, i * WAVES + wave);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (hole[k])
-                    dst[to++] = j + k;
-                if (mover[k])
-                    src[from++] = j + k;
+                for (int k = 0; k < 4; ++k)
+                    at += lower(__ballot(which >> (4 * i + k) & 1));
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (which >> (4 * i + k) & 1)
+                        list[at++] = (lo & ~3) + i * STRIDE + 4 * tid + k;
             }
-        }
+        };
+        write(dst, hole, at_dst + before_holes);
+        write(src, mover, at_src + before_movers);
         at_dst += all_holes, at_src += all_movers, left -= min(left, all_same);
-        __syncthreads();                                    // the words have been read
+        __syncthreads();                                    // the counts have been read
     }
     // the elements of the lists from n on
     __device__ __forceinline__ void fill(int n, int part, int parts)
@@ -273,7 +293,8 @@ __global__ __launch_bounds__(kSelectThreads) void attn_select_kernel(const Selec
         p.new_len[l.b] = l.new_len();
     int at_dst = 0, at_src = 0;
     if (!l.whole) {
-        l.read(0, l.kv);
+        l.ask(0, l.kv);
+        l.make(0);
         uint32_t top = 0;
         int left = l.keep;
 #pragma unroll 1
@@ -308,7 +329,7 @@ struct SelectPart {
 // One of four launches over the parts of the lists.  Launch 0 counts the first digit; 1 and 2 add up the parts' counts of the digit
 // before and count the next one; 3 adds up the last ones and writes the lists.
 template <int PASS>
-__global__ __launch_bounds__(kPartThreads) void attn_select_part_kernel(const SelectParams p)
+__global__ __launch_bounds__(kPartThreads, 4) void attn_select_part_kernel(const SelectParams p)
 {
     __shared__ SelectShared<kPartThreads> sh;
     const int list = quotient((int)blockIdx.x, p.parts), part = blockIdx.x - list * p.parts;
@@ -328,6 +349,18 @@ __global__ __launch_bounds__(kPartThreads) void attn_select_part_kernel(const Se
     uint32_t top = 0;
     int left = l.keep;
     int *const kept = p.kept + (size_t)list * p.parts;
+    l.ask(lo, min((lo & ~3) + kPartChunk, hi));             // (on their way while the counts are added up)
+    // f(from, upto) with the ranks of those places, a chunk at a time
+    auto chunks = [&](auto f) {
+        for (int from = lo; from < hi;) {
+            const int upto = min((from & ~3) + kPartChunk, hi);
+            if (from != lo)
+                l.ask(from, upto);
+            l.make(from);
+            f(from, upto);
+            from = upto;
+        }
+    };
     if constexpr (PASS > 0) {
         if (PASS > 1) {
             const int2 known = p.known[(size_t)(PASS - 2) * gridDim.x / p.parts + list];
@@ -336,8 +369,15 @@ __global__ __launch_bounds__(kPartThreads) void attn_select_part_kernel(const Se
         const int *const counts = p.counts[PASS - 1] + (size_t)list * p.parts * kBins;
         for (int i = l.tid; i < kBins / 4; i += kPartThreads) {
             i32x4 sum = {0, 0, 0, 0};
-            for (int k = 0; k < parts.all; ++k)
-                sum += *reinterpret_cast<const i32x4 *>(counts + (size_t)k * kBins + 4 * i);
+            for (int k0 = 0; k0 < parts.all; k0 += 8) {     // eight rows on their way
+                i32x4 x[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    x[k] = *reinterpret_cast<const i32x4 *>(counts + (size_t)min(k0 + k, parts.all - 1) * kBins + 4 * i);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    sum += k0 + k < parts.all ? x[k] : i32x4{0, 0, 0, 0};
+            }
             reinterpret_cast<i32x4 *>(sh.count)[i] = sum;
         }
         const int digit = l.find(left);
@@ -347,18 +387,28 @@ __global__ __launch_bounds__(kPartThreads) void attn_select_part_kernel(const Se
                 p.known[(size_t)(PASS - 1) * gridDim.x / p.parts + list] = int2{(int)top, left};
             // this part's ranks above the digit are kept
             int more = 0, all;
-            for (int i = l.tid; i < kBins; i += kPartThreads)
-                more += i > digit ? counts[(size_t)part * kBins + i] : 0;
+            const i32x4 own = *reinterpret_cast<const i32x4 *>(counts + (size_t)part * kBins + 4 * l.tid);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                more += 4 * l.tid + j > digit ? own[j] : 0;
             l.join(wave_sum(more), 1, all);
             if (l.tid == 0)
                 kept[part] = (PASS > 1 ? kept[part] : 0) + all;
         } else {
             // kept ones of every part: so far, above the last digit, and of those that equal it as many as the parts before leave
-            int *const of_part = reinterpret_cast<int *>(sh.above), *const same = of_part + kMostParts + 2;
+            int *const of_part = sh.of_part[0], *const same = sh.of_part[1];
             for (int k = l.wave; k < parts.all; k += kPartThreads / 64) {
+                constexpr int N = (1 << digit_bits(2)) / 256;
+                i32x4 x[N];
                 int more = 0;
-                for (int i = l.lane; i < kBins; i += 64)
-                    more += i > digit ? counts[(size_t)k * kBins + i] : 0;
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    x[i] = *reinterpret_cast<const i32x4 *>(counts + (size_t)k * kBins + 256 * i + 4 * l.lane);
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        more += 256 * i + 4 * l.lane + j > digit ? x[i][j] : 0;
                 more = wave_sum(more);
                 if (l.lane == 0)
                     of_part[k] = kept[k] + more, same[k] = counts[(size_t)k * kBins + digit];
@@ -372,27 +422,16 @@ __global__ __launch_bounds__(kPartThreads) void attn_select_part_kernel(const Se
                     at_dst += holes, at_src += k < parts.below ? 0 : n, left -= taken;
                 of_last -= taken, all += holes;
             }
-            __syncthreads();                                // (the words are written again)
             if (l.h == 0 && part == 0 && l.tid == 0)
                 p.new_len[l.b] = l.new_len();
-            for (int from = lo; from < hi;) {
-                const int upto = min((from & ~3) + kPartChunk, hi);
-                l.read(from, upto);
-                l.emit(from, upto, top, left, at_dst, at_src);
-                from = upto;
-            }
+            chunks([&](int from, int upto) { l.emit(from, upto, top, left, at_dst, at_src); });
             l.fill(all, part, parts.all);
             return;
         }
         __syncthreads();                                    // the sums have been read
     }
     l.clear();
-    for (int from = lo; from < hi;) {
-        const int upto = min((from & ~3) + kPartChunk, hi);
-        l.read(from, upto);
-        l.tally(PASS, top, from, upto);
-        from = upto;
-    }
+    chunks([&](int from, int upto) { l.tally(PASS, top, from, upto); });
     __syncthreads();
     int *const mine = p.counts[PASS < 3 ? PASS : 0] + ((size_t)list * p.parts + part) * kBins;
     for (int i = l.tid; i < kBins / 4; i += kPartThreads)
