@@ -240,15 +240,16 @@ __global__ __launch_bounds__(256) void attn_weigh_rows_kernel(const WeighParams 
 }
 
 // Many rows: a workgroup has 256 keys (128 at D = 256), each wave its part of them in registers as A operands of v_mfma_f32_32x32x16,
-// and the rows pass through LDS in stages that all waves read.  A batch with few blocks of so many keys is cut finer: the
-// waves of a workgroup then have the same keys and take a stage's 32-row tiles in turn.
+// and the rows pass through LDS in stages that all waves read.  A batch with few blocks of 256 keys is cut finer: two waves of a workgroup
+// then have the same keys, and half of a stage's rows each.
 template <int D>
 struct WeighTiling {
     static constexpr int ROWB = D * 2, SUB = D == 256 ? 2 : 4;     // 32-row tiles of a stage
     static constexpr int ROWS = 32 * SUB, STAGE = ROWS * ROWB;
     static constexpr int KB = D == 256 ? 1 : 2;                    // 32-key blocks of a wave
     static constexpr int KEYS = 4 * 32 * KB;                       // of a workgroup
-    static constexpr int LDS_BYTES = 2 * STAGE;
+    static constexpr int SHARE = SUB / 2;                          // waves that share keys where the batch has few blocks
+    static constexpr int LDS_BYTES = 2 * (STAGE + ROWS * 4);
 };
 constexpr int kWeighTileGroups = 512;   // workgroups of a launch: two to a compute unit
 
@@ -265,11 +266,12 @@ __global__ __launch_bounds__(256, 2) void attn_weigh_tiles_kernel(const WeighPar
     const int page_mask = (1 << p.c.page_log2) - 1;
     WeighUnits units;
     units.begin(p.c, __builtin_ctz(T::KEYS));
-    const bool split = p.c.B <= 64 && (long long)units.all * p.c.H_kv < kWeighTileGroups;
+    const bool split = T::SHARE > 1 && p.c.B <= 64 && (long long)units.all * p.c.H_kv < kWeighTileGroups;
     if (split)
-        units.begin(p.c, __builtin_ctz(T::KEYS / SUB));
-    const int my_keys = (split ? wave / SUB : wave) * 32 * KB, my_tile = split ? wave % SUB : -1;
-    const uint32_t k0 = (uint32_t)(lq * ROWB + ((g ^ swz<D>(lq)) * 16));       // chunk g of row lq; chunk 2 s + g: k0 ^ 32 s
+        units.begin(p.c, __builtin_ctz(T::KEYS / T::SHARE));
+    const int my_keys = (split ? wave / T::SHARE : wave) * 32 * KB;
+    const int tile0 = split ? wave % T::SHARE * 2 : 0, tile1 = split ? tile0 + 2 : SUB;    // of a stage
+    uint32_t k0 = (uint32_t)(lq * ROWB + ((g ^ swz<D>(lq)) * 16));       // chunk g of row lq; chunk 2 s + g: k0 ^ 32 s
     const uint32_t st = (uint32_t)p.q_st * 2, sh = (uint32_t)p.q_sh * 2;       // (the host keeps offsets of a call's rows to 32 bits)
 
     for (long long unit = blockIdx.x;; unit += gridDim.x) {
@@ -289,42 +291,34 @@ __global__ __launch_bounds__(256, 2) void attn_weigh_tiles_kernel(const WeighPar
                                                           (uint32_t)__builtin_amdgcn_readfirstlane((int)at));
         asm volatile("s_nop 4" : "+s"(rows));               // five wait states between the vector unit's write of a scalar and a load
         uint32_t off[LOADS];
-        int rem[LOADS];                                     // head of the row in its group
-        const int step_rem = T::ROWS % p.G;
-        const uint32_t step = (uint32_t)(T::ROWS / p.G) * st + (uint32_t)step_rem * sh, wrap = st - (uint32_t)p.G * sh;
+        const uint32_t step = (uint32_t)(T::ROWS / p.G) * st;
+        const bool even = T::ROWS % p.G == 0;               // a stage's rows are whole tokens: the next one's lie a step on
         auto bring = [&](int i) {
             if (i >= stages)
                 return;
             const int first = from + i * T::ROWS;
+            int ln = lane;                                  // (places made anew: kept across stages they take registers)
+            asm volatile("" : "+v"(ln));
 #pragma unroll
             for (int l = 0; l < LOADS; ++l) {
-                const int r = (wave * LOADS + l) * RPL + lane / CPR, ch = lane % CPR;
-                if (i == 0 || first + T::ROWS > n_rows) {
+                const int r = (wave * LOADS + l) * RPL + ln / CPR, ch = ln % CPR;
+                if (i == 0 || !even || first + T::ROWS > n_rows) {
                     const int row = min(first + r, n_rows - 1), token = p.token_of(row);
-                    rem[l] = row - token * p.G;
-                    off[l] = (uint32_t)token * st + (uint32_t)rem[l] * sh + (uint32_t)(((ch & ~15) | ((ch & 15) ^ swz<D>(r))) * 16);
+                    off[l] = (uint32_t)token * st + (uint32_t)(row - token * p.G) * sh +
+                             (uint32_t)(((ch & ~15) | ((ch & 15) ^ swz<D>(r))) * 16);
                 } else {
                     off[l] += step;
-                    if (step_rem) {
-                        rem[l] += step_rem;
-                        off[l] += rem[l] >= p.G ? wrap : 0;
-                        rem[l] -= rem[l] >= p.G ? p.G : 0;
-                    }
                 }
                 dma16(lds0 + (i & 1) * T::STAGE + (wave * LOADS + l) * 1024, rows, off[l]);
             }
         };
-        // what a row's scores are lowered by (base 2): infinity where it sees nothing or there is no row
-        float shift[SUB], next[SUB];
+        // what a row's scores are lowered by (base 2), infinity where it sees nothing or there is no row: a thread has a row of the stage
+        float *const shifts = reinterpret_cast<float *>(smem + 2 * T::STAGE);
+        float lse = -INFINITY;
         auto ask = [&](int i) {
-#pragma unroll
-            for (int t = 0; t < SUB; ++t) {
-                if (split && t != my_tile)
-                    continue;
-                const int r = from + i * T::ROWS + 32 * t + lq, row = min(r, n_rows - 1), token = p.token_of(row);
-                const float x = p.lse[(size_t)(row0 + token) * p.H_q + h * p.G + row - token * p.G];
-                next[t] = r < n_rows ? x : -INFINITY;
-            }
+            const int r = from + i * T::ROWS + (int)threadIdx.x, row = min(r, n_rows - 1), token = p.token_of(row);
+            if (threadIdx.x < T::ROWS && i < stages)
+                lse = r < n_rows ? p.lse[(size_t)(row0 + token) * p.H_q + h * p.G + row - token * p.G] : -INFINITY;
         };
         __syncthreads();                                    // the last unit's rows have been read
         if (stages > 0) {
@@ -355,58 +349,81 @@ __global__ __launch_bounds__(256, 2) void attn_weigh_tiles_kernel(const WeighPar
             }
         }
 
-        f32x16 w[KB];
+        float w[KB][16];
 #pragma unroll
         for (int t = 0; t < KB; ++t)
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 w[t][r] = 0.f;
+        // Scores of tile t of stage i into `now`; between the products the weights of the tile before are taken, whose scores lie in
+        // `then` and are lowered by `down`: the matrix pipe and the vector unit have the same to do, and neither waits for the other.
+        float down = -INFINITY;
+        auto scores = [&](int i, int t, f32x16 (&now)[KB], f32x16 (&then)[KB]) {
+            const uint32_t base = lds0 + (i & 1) * T::STAGE + t * 32 * ROWB;
+            asm volatile("" : "+v"(k0));                    // (its later chunks' offsets made anew: kept they take registers)
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    now[kb][r] = 0.f;
+            constexpr int AHEAD = 3;                        // operands on their way
+            u32x4 q[AHEAD + 1];
+            auto operand = [&](int ks) { return *(ATTN_LDS_PTR(const u32x4))(uintptr_t)((k0 ^ (32 * ks)) + base); };
+#pragma unroll
+            for (int ks = 0; ks < AHEAD; ++ks)
+                q[ks] = operand(ks);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                if (ks + AHEAD < KS)
+                    q[(ks + AHEAD) % (AHEAD + 1)] = operand(ks + AHEAD);
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+                    now[kb] = mfma32<E>(a[kb][ks], q[ks % (AHEAD + 1)], now[kb]);
+                constexpr int PER = 16 * KB / KS;
+#pragma unroll
+                for (int x = ks * PER; x < (ks + 1) * PER; ++x) {
+                    w[x / 16][x % 16] += __builtin_amdgcn_exp2f(fmaf(then[x / 16][x % 16], p.c_log2, down));
+                    asm volatile("" : "+v"(w[x / 16][x % 16]));              // (here, not behind the products)
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            down = shifts[(i & 1) * T::ROWS + 32 * t + lq];
+            const int first = from + i * T::ROWS + 32 * t;
+            if (p.causal && first_pos + p.token_of(min(first, n_rows - 1)) < j0 + 32 * KB - 1) {     // some row does not see some key
+                // (against constants: positions kept in registers would take 32)
+                const int limit = first_pos + p.token_of(min(first + lq, n_rows - 1)) - j0 - 4 * g;
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        now[kb][r] = 32 * kb + acc_row(r, 0) > limit ? -INFINITY : now[kb][r];
+            }
+        };
+        f32x16 s0[KB], s1[KB];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                s1[kb][r] = 0.f;                            // (lowered by infinity)
 #pragma clang loop unroll(disable)
         for (int i = 0; i < stages; ++i) {
             wait_vmcnt<0>();
-#pragma unroll
-            for (int t = 0; t < SUB; ++t)
-                shift[t] = next[t] == -INFINITY ? -INFINITY : -next[t] * 1.44269504088896340736f;
+            if (threadIdx.x < T::ROWS)
+                shifts[(i & 1) * T::ROWS + threadIdx.x] = lse == -INFINITY ? -INFINITY : -lse * 1.44269504088896340736f;
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");     // stage i is complete, stage i - 1 has been read
             bring(i + 1);
-            if (i + 1 < stages)
-                ask(i + 1);
-#pragma unroll
-            for (int t = 0; t < SUB; ++t) {
-                if (split && t != my_tile)
-                    continue;
-                const uint32_t base = lds0 + (i & 1) * T::STAGE + t * 32 * ROWB;
-                f32x16 s[KB];
-#pragma unroll
-                for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        s[kb][r] = 0.f;
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    const u32x4 q = *(ATTN_LDS_PTR(const u32x4))(uintptr_t)((k0 ^ (32 * ks)) + base);
-#pragma unroll
-                    for (int kb = 0; kb < KB; ++kb)
-                        s[kb] = mfma32<E>(a[kb][ks], q, s[kb]);
-                }
-                const int first = from + i * T::ROWS + 32 * t;
-                const bool cut = p.causal && first_pos + p.token_of(min(first, n_rows - 1)) < j0 + 32 * KB - 1;
-                if (cut) {                                  // some row does not see some key
-                    const int last = first_pos + p.token_of(min(first + lq, n_rows - 1));
-#pragma unroll
-                    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (j0 + 32 * kb + acc_row(r, g) > last)
-                                s[kb][r] = -INFINITY;
-                }
-#pragma unroll
-                for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        w[kb][r] += __builtin_amdgcn_exp2f(fmaf(s[kb][r], p.c_log2, shift[t]));
+            ask(i + 1);
+#pragma clang loop unroll(disable)
+            for (int t = tile0; t < tile1; t += 2) {
+                scores(i, t, s0, s1);
+                scores(i, t + 1, s1, s0);
             }
         }
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                w[kb][r] += __builtin_amdgcn_exp2f(fmaf(s1[kb][r], p.c_log2, down));
 
         // ---- one sum for every key: over the 32 rows of a tile, and in a split unit over its waves
         float y[KB];                                        // of key acc_row(lq % 16, g)
@@ -426,12 +443,12 @@ __global__ __launch_bounds__(256, 2) void attn_weigh_tiles_kernel(const WeighPar
             for (int kb = 0; kb < KB; ++kb)
                 part[(wave * KB + kb) * 64 + lane] = y[kb];
             __syncthreads();
-            if (my_tile != 0)
+            if (tile0 != 0)
                 continue;
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
                 y[kb] = 0.f;
-                for (int v = wave; v < wave + SUB; ++v)
+                for (int v = wave; v < wave + T::SHARE; ++v)
                     y[kb] += part[(v * KB + kb) * 64 + lane];
             }
         }
@@ -469,7 +486,7 @@ int launch(const WeighParams &p, int max_q, hipStream_t st)
     const long long reach = 2 * ((long long)p.c.T * p.q_st + (long long)p.G * p.q_sh + D);  // bytes of a head's rows
     const bool tiles = rows > kRowsMost && reach < 1LL << 32;
     // no more workgroups than units that the table can hold
-    const long long keys = tiles ? attn::WeighTiling<D>::KEYS / attn::WeighTiling<D>::SUB : 4 * attn::kWeighKeys;
+    const long long keys = tiles ? attn::WeighTiling<D>::KEYS / attn::WeighTiling<D>::SHARE : 4 * attn::kWeighKeys;
     const long long blocks = (((long long)p.c.table_width << p.c.page_log2) + keys - 1) / keys;
     const long long seqs = p.c.B < p.c.T ? p.c.B : p.c.T;
     const int held = tiles ? attn::kWeighTileGroups : attn::persistent_slots(reinterpret_cast<const void *>(attn::attn_weigh_rows_kernel<D, E, E4M3>), 256, 0, 1);
