@@ -247,7 +247,7 @@ int launch(TreeParams &p, int max_q, const Workspace &w, hipStream_t st)
     const long long rows = (long long)(max_q < p.c.T ? max_q : p.c.T) * p.G;
     const long long tiles16 = (long long)p.c.T * p.G / 16 + (p.c.B < p.c.T ? p.c.B : p.c.T);
     const long long head_bytes = ((long long)p.c.table_width << p.c.page_log2) * D * (E4M3 ? 2 : 4);
-    const bool few = rows <= 16 || tiles16 * p.c.H_kv * head_bytes <= kFewBytes;
+    const bool few = rows <= 16 || tiles16 * p.c.H_kv <= kFewBytes / head_bytes;
     if constexpr (D != 256)
         if (few && tiles16 * p.c.H_kv <= kTarget / 2 && head_bytes <= kWholeBytes)
             return launch_rows<D, 1, E, E4M3, true, kWaves>(p, 0x7fffffff, st);
