@@ -92,7 +92,7 @@ int attn_cache_select(const float *weights, const int *stamps, const int *seen, 
                       int *dst, int *src, int *new_len, int sinks, int recent, void *workspace, long long workspace_bytes,
                       int B, int H_kv, int width, int moves_width, void *stream);
 
-/* Bytes of workspace attn_cache_select needs (0 up to 8192 places, a few KB for each 16384 places of a list beyond); -1 on
+/* Bytes of workspace attn_cache_select needs (0 up to 16384 places, some 25 KB for each 16384 places of a list beyond); -1 on
  * invalid arguments. */
 long long attn_cache_select_workspace_bytes(int B, int H_kv, int width);
 

@@ -50,7 +50,7 @@ constexpr int digit_bits(int pass) { return pass == 2 ? 10 : 11; }
 constexpr int digit_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
 
 constexpr int kHeld = 8;                // vectors of four ranks that a thread holds
-constexpr int kSelectThreads = 256, kSelectWhole = kSelectThreads * 4 * kHeld;
+constexpr int kSelectThreads = 512, kSelectWhole = kSelectThreads * 4 * kHeld;     // (256 for lists of up to half of that)
 static_assert(kBins == 4 * 512, "a thread of a part has four bins");
 constexpr int kPartThreads = 512, kPartChunk = kPartThreads * 4 * kHeld, kMostParts = 64;
 
@@ -226,25 +226,36 @@ struct SelectList {
                 sh.of_vector[0][i * WAVES + wave] = (lo & ~3) + i * STRIDE < hi ? n_same[i] : 0;
         __syncthreads();
         const int before_same = sums(0, all_same);
+        // (all of the last rank, or none: no order among them)
+        const bool some = left > 0 && left < all_same;
         uint32_t hole = 0, mover = 0;                       // bit 4 i + k
 #pragma unroll
         for (int i = 0; i < kHeld; ++i) {
             int holes = 0, movers = 0;
             if ((lo & ~3) + i * STRIDE < hi) {
                 const int j = (lo & ~3) + i * STRIDE + 4 * tid;
-                bool same[4];
-                int rank = __builtin_amdgcn_readlane(before_same, i * WAVES + wave);
+                bool kept[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    same[k] = j + k >= lo && j + k < hi && held[i][k] == top;
-                    rank += lower(__ballot(same[k]));
+                for (int k = 0; k < 4; ++k)
+                    kept[k] = held[i][k] > top || (held[i][k] == top && left > 0);
+                if (some) {
+                    int rank = __builtin_amdgcn_readlane(before_same, i * WAVES + wave);
+                    bool same[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        same[k] = j + k >= lo && j + k < hi && held[i][k] == top;
+                        rank += lower(__ballot(same[k]));
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        kept[k] = same[k] ? rank < left : kept[k];
+                        rank += same[k];
+                    }
                 }
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const bool there = j + k >= lo && j + k < hi;
-                    const bool kept = there && (held[i][k] > top || (same[k] && rank < left));
-                    rank += same[k];
-                    const bool x = there && !kept && j + k < keep, y = kept && j + k >= keep;
+                    const bool there = j + k >= lo && j + k < hi, below = j + k < keep;
+                    const bool x = there && below && !kept[k], y = there && !below && kept[k];
                     hole |= (uint32_t)x << (4 * i + k), mover |= (uint32_t)y << (4 * i + k);
                     holes += __popcll(__ballot(x)), movers += __popcll(__ballot(y));
                 }
@@ -285,10 +296,11 @@ struct SelectList {
 };
 
 // A list to a workgroup.
-__global__ __launch_bounds__(kSelectThreads) void attn_select_kernel(const SelectParams p)
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void attn_select_kernel(const SelectParams p)
 {
-    __shared__ SelectShared<kSelectThreads> sh;
-    SelectList<kSelectThreads> l(p, sh, blockIdx.x);
+    __shared__ SelectShared<THREADS> sh;
+    SelectList<THREADS> l(p, sh, blockIdx.x);
     if (l.h == 0 && l.tid == 0)
         p.new_len[l.b] = l.new_len();
     int at_dst = 0, at_src = 0;
@@ -599,7 +611,11 @@ extern "C" int attn_cache_select(const float *weights, const int *stamps, const 
     p.parts = s.parts, p.part_places = s.part_places;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (s.bytes == 0) {
-        hipLaunchKernelGGL(attn::attn_select_kernel, dim3((unsigned)lists), dim3(attn::kSelectThreads), 0, st, p);
+        constexpr int half = attn::kSelectThreads / 2;
+        if (width <= attn::kSelectWhole / 2)
+            hipLaunchKernelGGL((attn::attn_select_kernel<half>), dim3((unsigned)lists), dim3(half), 0, st, p);
+        else
+            hipLaunchKernelGGL((attn::attn_select_kernel<attn::kSelectThreads>), dim3((unsigned)lists), dim3(attn::kSelectThreads), 0, st, p);
         return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH;
     }
     int *const ws = static_cast<int *>(workspace);

@@ -32,7 +32,7 @@ def registers(text):
     return found
 
 
-@pytest.mark.parametrize("source, kernels", [("attn_tree", 40), ("attn_weigh", 24), ("attn_evict", 9)])
+@pytest.mark.parametrize("source, kernels", [("attn_tree", 40), ("attn_weigh", 24), ("attn_evict", 10)])
 def test_no_scratch_no_spills_and_room_for_the_workgroups(source, kernels, tmp_path):
     text = listing(source, tmp_path)
     found = metadata(text)

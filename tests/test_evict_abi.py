@@ -71,10 +71,10 @@ def test_select_refusals(b):  # noqa: F811
         assert f(**{n: OK + 2}) == b.ATTN_ERR_ALIGN
     assert f(new_len=FAR + 2) == b.ATTN_ERR_ALIGN
     need = b.attn_cache_select_workspace_bytes
-    assert need(2, 2, 8192) == 0 and f(ws=None, ws_bytes=0, dst=OK + 2) == b.ATTN_ERR_ALIGN
-    assert need(2, 2, 8208) > 0 and need(2, 2, 8208) % 16 == 0
-    assert f(width=8208, ws=None) == b.ATTN_ERR_NULL and f(width=8208, ws=OK + 8) == b.ATTN_ERR_ALIGN
-    assert f(width=8208, ws_bytes=need(2, 2, 8208) - 1) == b.ATTN_ERR_WORKSPACE
+    assert need(2, 2, 16384) == 0 and f(ws=None, ws_bytes=0, dst=OK + 2) == b.ATTN_ERR_ALIGN
+    assert need(2, 2, 16400) > 0 and need(2, 2, 16400) % 16 == 0
+    assert f(width=16400, ws=None) == b.ATTN_ERR_NULL and f(width=16400, ws=OK + 8) == b.ATTN_ERR_ALIGN
+    assert f(width=16400, ws_bytes=need(2, 2, 16400) - 1) == b.ATTN_ERR_WORKSPACE
     for bad in ((0, 2, 64), (2, 0, 64), (2, 2, 0), (2, 2, 24), (2, 2, (1 << 30) + 16), (1 << 21, 2, 64)):
         assert need(*bad) == -1
     assert f(B=1 << 20, width=1 << 17) == b.ATTN_ERR_SHAPE                        # 2^24 workgroups of 512 threads

@@ -75,7 +75,7 @@ def test_select_of_long_sequences():
 
 @pytest.mark.parametrize("kind", ["spread", "few", "special"])
 @pytest.mark.parametrize("width, kvs, keeps", [
-    (8208, [8208, 8193, 5000, 8208], [100, 8192, 4999, 8207]), (16400, [16400, 16385, 16384, 20], [8001, 16384, 1, 7]),
+    (8208, [8208, 8193, 5000, 8208], [100, 8192, 4999, 8207]), (16384, [16384, 9000, 16383, 12289], [5000, 8999, 16382, 1]), (16400, [16400, 16385, 16384, 20], [8001, 16384, 1, 7]),
     (50000, [50000, 49153, 33000, 50000], [32768, 16383, 16385, 3])])
 def test_select_of_lists_in_parts(width, kvs, keeps, kind):
     """Ends at, before and behind the borders of the parts, which begin anew at the new length."""
