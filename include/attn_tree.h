@@ -26,8 +26,10 @@ extern "C" {
  *
  * The mask is device memory like start and kv_len: its values may change between the replays of a captured graph.
  *
- * All other arguments, the workspace (attn_paged_fwd_workspace_bytes), results, limits, ownership and errors are those of
- * attn_paged_fwd; ATTN_ERR_NULL, ATTN_ERR_SHAPE and ATTN_ERR_ALIGN stand for the mask's arguments too.  Every row reads every
+ * workspace_bytes at least attn_paged_tree_workspace_bytes(T, B, H_q, H_kv, D), else ATTN_ERR_WORKSPACE; calls that follow each other may
+ * share one, also with attn_paged_fwd (the larger of the two sizes).
+ *
+ * All other arguments, results, limits, ownership and errors are those of attn_paged_fwd; ATTN_ERR_NULL, ATTN_ERR_SHAPE and ATTN_ERR_ALIGN stand for the mask's arguments too.  Every row reads every
  * key that its sequence has, so no row is cheaper for what its mask hides.
  */
 int attn_paged_tree(const void *q, const long long *strides, void *o, float *lse,
@@ -42,6 +44,10 @@ int attn_paged_tree_f16(const void *q, const long long *strides, void *o, float 
                         const unsigned long long *mask, int mask_words, void *workspace, long long workspace_bytes, int max_q,
                         int T, int B, int H_q, int H_kv, int D, int n_pages, int page_size, int table_width,
                         float scale, void *stream);
+
+/* Bytes of workspace attn_paged_tree (either element type) needs; -1 on invalid arguments.  By rows (T * H_q / H_kv) at D = 128: 9 MB up to 16
+ * of them, 72 up to 128, 144 beyond, and 16 bytes for every token. */
+long long attn_paged_tree_workspace_bytes(int T, int B, int H_q, int H_kv, int D);
 
 #ifdef __cplusplus
 }

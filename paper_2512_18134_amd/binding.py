@@ -125,7 +125,8 @@ def _native():
                                      for suffix in ("", "_f16")), address(_lib.attn_paged_fwd_workspace_bytes))
         module.set_eviction_entries(*(address(getattr(_lib, name)) for name in
                                       ("attn_paged_tree", "attn_paged_tree_f16", "attn_cache_weigh", "attn_cache_weigh_f16",
-                                       "attn_cache_select", "attn_cache_move", "attn_cache_select_workspace_bytes")))
+                                       "attn_cache_select", "attn_cache_move", "attn_cache_select_workspace_bytes",
+                                       "attn_paged_tree_workspace_bytes")))
         _marshal_module = module
     return _marshal_module
 
@@ -673,12 +674,12 @@ def attn_paged_fwd_f16(q, k_pages, v_pages, page_table, start, kv_len, k_scale=N
 def _marshal_paged(entry, dt, q, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale, o, lse, workspace, causal, scale,
                    max_q, stream):
     return _paged(entry, dt, q, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale, o, lse, workspace, (), (int(bool(causal)),),
-                  scale, max_q, stream)
+                  scale, max_q, stream, attn_paged_fwd_workspace_bytes)
 
 
 def _paged(entry, dt, q, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale, o, lse, workspace, mask, causal, scale, max_q,
-           stream):
-    """mask, causal: the C entry point's arguments behind kind and behind table_width."""
+           stream, workspace_bytes):
+    """mask, causal: the C entry point's arguments behind kind and behind table_width; workspace_bytes: the function that says how many."""
     import torch
 
     _check_rows(q, dt, 3, "q", q.device)
@@ -687,7 +688,7 @@ def _paged(entry, dt, q, k_pages, v_pages, page_table, start, kv_len, k_scale, v
                                                                      v_scale, q.device)
     if D != D_cache or H_kv < 1 or H_q % H_kv:
         raise ValueError("q's heads do not fit the cache's")
-    need = attn_paged_fwd_workspace_bytes(T, B, H_q, H_kv, D)
+    need = workspace_bytes(T, B, H_q, H_kv, D)
     o = _allocate(lambda: torch.empty((T, H_q, D), dtype=dt, device=q.device), q.device, stream) if o is None else o
     if lse is None:
         lse = _allocate(lambda: torch.empty((T, H_q), dtype=torch.float32, device=q.device), q.device, stream)
@@ -720,13 +721,21 @@ for _suffix in ("", "_f16"):
                                                            + [_float, _pointer])
 
 
+_lib.attn_paged_tree_workspace_bytes.restype = _int64
+_lib.attn_paged_tree_workspace_bytes.argtypes = [_int] * 5
+
+
+def attn_paged_tree_workspace_bytes(T, B, H_q, H_kv, D):
+    return int(_lib.attn_paged_tree_workspace_bytes(T, B, H_q, H_kv, D))
+
+
 def attn_paged_tree(q, k_pages, v_pages, page_table, start, kv_len, mask, k_scale=None, v_scale=None, o=None, lse=None,
                     workspace=None, scale=None, max_q=None, stream=None):
     """attn_paged_tree on torch device tensors (include/attn_tree.h): drafted tokens' queries against the cache, with a mask among them.
 
     mask int64 [T,words]: bit m % 64 of word m // 64 of row t says that row t sees row start[b] + m of its own sequence (bit 63 is
-    the sign); what lies in the cache before a sequence's new tokens is seen by all of them.  Everything else is as in
-    attn_paged_fwd.  Asynchronous on `stream`.  Returns (o, lse).
+    the sign); what lies in the cache before a sequence's new tokens is seen by all of them.  workspace: at least
+    attn_paged_tree_workspace_bytes(...) bytes.  Everything else is as in attn_paged_fwd.  Asynchronous on `stream`.  Returns (o, lse).
     """
     r = (_marshal_module or _native()).tree(0, q, k_pages, v_pages, page_table, start, kv_len, mask, k_scale, v_scale, o, lse, workspace,
                                             scale, max_q, stream)
@@ -758,7 +767,7 @@ def _marshal_tree(entry, dt, q, k_pages, v_pages, page_table, start, kv_len, mas
         raise TypeError("mask must be an int64 tensor [T, words]")
     _check_array(mask, torch.int64, (q.shape[0], mask.shape[1]), "mask", q.device)
     return _paged(entry, dt, q, k_pages, v_pages, page_table, start, kv_len, k_scale, v_scale, o, lse, workspace, (mask.data_ptr(), mask.shape[1]),
-                  (), scale, max_q, stream)
+                  (), scale, max_q, stream, attn_paged_tree_workspace_bytes)
 
 
 # ---------------------------------------------------------------------------------------------------------------------

@@ -80,6 +80,17 @@ inline Workspace workspace_of(int T, int B, int G, int D)
     return w;
 }
 
+// A call of trees has one kernel at a time: kSlots partial results of the tallest tiles that its rows can ask for.
+inline int tree_rows(int D, long long rows) { return rows <= 16 ? 16 : D == 256 || rows <= 128 ? 128 : 256; }
+inline Workspace tree_workspace_of(int T, int B, int G, int D)
+{
+    Workspace w = {};
+    w.merge = (long long)kSlots * tree_rows(D, (long long)T * G) * (D + 1) * 4;
+    w.cut[0] = w.cut[1] = w.merge + (long long)T * (long long)sizeof(MergeNote);
+    w.bytes = w.cut[0] + (B > kOwnCut ? (B + 1LL) * (long long)sizeof(int2) : 0);
+    return w;
+}
+
 inline bool misaligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
 // The cut of a batch of many sequences, before the kernel that takes its units.
@@ -253,7 +264,7 @@ int launch(TreeParams &p, int max_q, const Workspace &w, hipStream_t st)
             return launch_rows<D, 1, E, E4M3, true, kWaves>(p, 0x7fffffff, st);
     // the kernel has the workspace for itself
     PagedParams::Parts &parts = p.parts[few ? 0 : 1];
-    parts.BM = few ? 16 : D == 256 || rows <= 128 ? 128 : 256;
+    parts.BM = few ? 16 : tree_rows(D, rows);
     const long long fit = w.merge / ((long long)parts.BM * (D + 1) * 4);
     parts.slots = (int)(fit < kSlots ? fit : kSlots);
     parts.o = p.parts[0].o;
@@ -315,7 +326,7 @@ int paged_call(const void *q, const long long *strides, void *o, float *lse, con
         return ATTN_ERR_ALIGN;
     if (!(scale > 0.f) || !(scale < INFINITY))
         return ATTN_ERR_SCALE;
-    const Workspace w = workspace_of(T, B, H_q / H_kv, D);
+    const Workspace w = TREE ? tree_workspace_of(T, B, H_q / H_kv, D) : workspace_of(T, B, H_q / H_kv, D);
     if (workspace_bytes < w.bytes)
         return ATTN_ERR_WORKSPACE;
     ParamsOf<TREE> p;

@@ -5,6 +5,14 @@
 #include "attn_paged_launch.h"
 #include "attn_tree.h"
 
+extern "C" long long attn_paged_tree_workspace_bytes(int T, int B, int H_q, int H_kv, int D)
+{
+    if (T < 1 || B < 1 || H_q < 1 || H_kv < 1 || H_q % H_kv || (D != 64 && D != 128 && D != 256) ||
+        (long long)T * H_q > 0x3fffffffLL || B > attn::kMostSequences)
+        return -1;
+    return attn::tree_workspace_of(T, B, H_q / H_kv, D).bytes;
+}
+
 #define ATTN_TREE_ENTRY(name, E)                                                                                                \
     extern "C" int name(const void *q, const long long *strides, void *o, float *lse, const void *k_pages, const void *v_pages, \
                         const unsigned char *k_scale, const unsigned char *v_scale, const int *page_table, const int *start,    \

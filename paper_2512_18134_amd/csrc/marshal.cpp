@@ -569,6 +569,7 @@ TreeFn g_tree[2];
 WeighFn g_weigh[2];
 SelectFn g_select;
 SelectWsFn g_select_ws;
+PagedWsFn g_tree_ws;
 MoveFn g_move;
 
 // tree(type, q, k_pages, v_pages, page_table, start, kv_len, mask, k_scale, v_scale, o, lse, workspace, scale, max_q, stream)
@@ -581,7 +582,7 @@ PyObject *py_tree(PyObject *, PyObject *const *a, Py_ssize_t n)
     void *stream;
     float scale;
     at::Tensor o, lse, ws;
-    if (n != 16 || !g_tree[type] || !g_paged_ws || !cache_of(a + 2, a[8], a[9], kElem[type], c) || !scale_of(a[13], c.D, scale))
+    if (n != 16 || !g_tree[type] || !g_tree_ws || !cache_of(a + 2, a[8], a[9], kElem[type], c) || !scale_of(a[13], c.D, scale))
         Py_RETURN_NONE;
     const at::Tensor *q = rows_of(a[1], kElem[type], 3), *mask = plain(a[7], at::kLong, 2);
     if (!q || !mask || q->device() != c.k->device() || mask->device() != q->device() || q->size(2) != c.D || q->size(1) % c.H_kv ||
@@ -592,7 +593,7 @@ PyObject *py_tree(PyObject *, PyObject *const *a, Py_ssize_t n)
     int max_q = T;
     if (a[14] != Py_None && !int_of(a[14], max_q))
         Py_RETURN_NONE;
-    const long long need = g_paged_ws(T, c.B, H_q, c.H_kv, c.D);
+    const long long need = g_tree_ws(T, c.B, H_q, c.H_kv, c.D);
     if (need < 1)
         Py_RETURN_NONE;
     if (a[12] != Py_None) {
@@ -778,16 +779,16 @@ PyObject *py_move(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// set_eviction_entries(addresses of paged_tree and cache_weigh, bf16 and fp16 of each, cache_select, cache_move and the workspace size of
-// the last but one)
+// set_eviction_entries(addresses of paged_tree and cache_weigh, bf16 and fp16 of each, cache_select, cache_move and the workspace sizes of
+// cache_select and paged_tree)
 PyObject *py_set_eviction_entries(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    void *p[7];
-    if (n != 7) {
-        PyErr_SetString(PyExc_TypeError, "set_eviction_entries takes seven addresses");
+    void *p[8];
+    if (n != 8) {
+        PyErr_SetString(PyExc_TypeError, "set_eviction_entries takes eight addresses");
         return nullptr;
     }
-    for (int i = 0; i < 7; ++i)
+    for (int i = 0; i < 8; ++i)
         p[i] = PyLong_AsVoidPtr(a[i]);
     if (PyErr_Occurred())
         return nullptr;
@@ -798,6 +799,7 @@ PyObject *py_set_eviction_entries(PyObject *, PyObject *const *a, Py_ssize_t n)
     g_select = (SelectFn)p[4];
     g_move = (MoveFn)p[5];
     g_select_ws = (SelectWsFn)p[6];
+    g_tree_ws = (PagedWsFn)p[7];
     Py_RETURN_NONE;
 }
 

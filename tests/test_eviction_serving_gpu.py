@@ -163,7 +163,7 @@ def test_a_captured_step_is_replayed_as_lengths_and_masks_change():
         out = {"o": torch.empty((T_rows, H * G, D), dtype=torch.bfloat16, device="cuda"), "lse": torch.empty((T_rows, H * G), device="cuda"),
                "dst": torch.empty((B, H, 16), dtype=torch.int32, device="cuda"), "src": torch.empty((B, H, 16), dtype=torch.int32, device="cuda"),
                "new_len": torch.empty(B, dtype=torch.int32, device="cuda")}
-        ws = torch.empty(M.attn_paged_fwd_workspace_bytes(T_rows, B, H * G, H, D), dtype=torch.uint8, device="cuda")
+        ws = torch.empty(M.attn_paged_tree_workspace_bytes(T_rows, B, H * G, H, D), dtype=torch.uint8, device="cuda")
         ws2 = torch.empty(max(16, M.attn_cache_select_workspace_bytes(B, H, p.L)), dtype=torch.uint8, device="cuda")
 
         def step(s, o, ws, ws2):

@@ -33,8 +33,11 @@ def test_tree_refusals(b, suffix):  # noqa: F811
     assert f(mask=OK + 4) == b.ATTN_ERR_ALIGN
     for s in (0.0, -1.0, float("nan"), float("inf")):
         assert f(scale=s) == b.ATTN_ERR_SCALE
-    need = b.attn_paged_fwd_workspace_bytes(3, 2, 4, 2, 64)
-    assert f(ws_bytes=need - 1) == b.ATTN_ERR_WORKSPACE
+    need = b.attn_paged_tree_workspace_bytes(3, 2, 4, 2, 64)
+    assert need > 0 and f(ws_bytes=need - 1) == b.ATTN_ERR_WORKSPACE
+    for bad in ((0, 1, 4, 2, 64), (3, 0, 4, 2, 64), (3, 2, 5, 2, 64), (3, 2, 4, 0, 64), (3, 2, 4, 2, 96), (1 << 30, 1, 4, 2, 64),
+                (3, (1 << 30) + 1, 4, 2, 64)):
+        assert b.attn_paged_tree_workspace_bytes(*bad) == -1
     for B in ((1 << 30) + 1, 2 ** 31 - 64, 2 ** 31 - 1):
         assert f(B=B, start=OK + 2) == b.ATTN_ERR_SHAPE
     many = dict(T=1 << 22, B=1 << 22, H_q=8, H_kv=8, strides=arr([512, 64]))

@@ -21,7 +21,7 @@ def attend(M, c, G, sets, n_words=None, max_q=None, q=None, fill=-1):
     args, scales = c.on_gpu()
     o = torch.full(q.shape, float("nan"), dtype=q.dtype, device="cuda")
     lse = torch.full(q.shape[:2], float("nan"), device="cuda")
-    ws = torch.full((M.attn_paged_fwd_workspace_bytes(c.T, len(c.kv_len), q.shape[1], c.H_kv, c.D) // 4,), float("nan"), device="cuda")
+    ws = torch.full((M.attn_paged_tree_workspace_bytes(c.T, len(c.kv_len), q.shape[1], c.H_kv, c.D) // 4,), float("nan"), device="cuda")
     got = fn(M, "attn_paged_tree", c.dt)(q.cuda(), *args, mask.cuda(), **scales, o=o, lse=lse, workspace=ws, max_q=max_q)
     assert got[0] is o and got[1] is lse
     torch.cuda.synchronize()
