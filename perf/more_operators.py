@@ -349,7 +349,9 @@ def _run_own(s):
     from paper_2512_18134_amd import binding
     case = s["case"]
     if case["op"] == "select":
-        dst, src, new_len = binding.attn_cache_select(s["weights"], s["kv_len"], s["keep"], _most_moves(case), stamps=s["stamps"],
+        if "moves" not in s:                              # a number of the program's plan, not of a call
+            s["moves"] = _most_moves(case)
+        dst, src, new_len = binding.attn_cache_select(s["weights"], s["kv_len"], s["keep"], s["moves"], stamps=s["stamps"],
                                                       seen=s["seen"], sinks=case["sinks"], recent=case["recent"])
         return {"dst": dst, "src": src, "new_len": new_len}
     if case["op"] == "tree":
