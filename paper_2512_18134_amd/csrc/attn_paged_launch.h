@@ -248,10 +248,13 @@ int launch(PagedParams &p, int max_q, hipStream_t st)
     return rc == ATTN_OK ? launch_merge<D, E, false>(p, merge, st) : rc;
 }
 
-// Trees of drafted tokens: few rows of many heads, or some hundreds.  One kernel takes all sequences of a call: 16-row tiles of the row
-// kernel where no sequence has more, or where K and V are so small that reading them for every such tile takes no time (kFewBytes); otherwise
-// the tile kernel, whose waves share a tile of keys, with 32 or 64 rows to a wave.  A wave without rows brings its share of
-// the keys and has nothing else to do, so that a sequence of few rows costs the tile kernel no more than its stream.
+// Trees of drafted tokens: few rows of many heads, or some hundreds.  One kernel takes all sequences of a call:
+//   * the row kernel by 16 rows where no sequence has more, or where K and V are so small that reading them for every such tile
+//     takes no time (kFewBytes)
+//   * the row kernel by 32 or 64 rows where no sequence has more: 16 sequences of 8 drafts at 8000, 16 heads over 4, D = 128, 57.5 us
+//     and in e4m3 32.2, by the tile kernel 63.7 and 43.4; at D = 256 65.9 and 82.3 in e4m3, 114.6 and 110.4 in 16 bits
+//   * otherwise the tile kernel, whose waves share a tile of keys, with 32 or 64 rows to a wave.  A wave without rows brings its share
+//     of the keys and has nothing else to do, so that a sequence of few rows costs it no more than its stream
 template <int D, typename E, bool E4M3>
 int launch(TreeParams &p, int max_q, const Workspace &w, hipStream_t st)
 {
@@ -262,23 +265,29 @@ int launch(TreeParams &p, int max_q, const Workspace &w, hipStream_t st)
     if constexpr (D != 256)
         if (few && tiles16 * p.c.H_kv <= kTarget / 2 && head_bytes <= kWholeBytes)
             return launch_rows<D, 1, E, E4M3, true, kWaves>(p, 0x7fffffff, st);
+    constexpr int kMid = D != 256 ? 64 : E4M3 ? 32 : 0;
+    const bool mid = !few && rows <= kMid, by_rows = few || mid;
     // the kernel has the workspace for itself
-    PagedParams::Parts &parts = p.parts[few ? 0 : 1];
-    parts.BM = few ? 16 : tree_rows(D, rows);
+    PagedParams::Parts &parts = p.parts[by_rows ? 0 : 1];
+    parts.BM = few ? 16 : mid ? 16 * row_tiles(D, rows) : tree_rows(D, rows);
     const long long fit = w.merge / ((long long)parts.BM * (D + 1) * 4);
     parts.slots = (int)(fit < kSlots ? fit : kSlots);
     parts.o = p.parts[0].o;
     parts.lse = parts.o + (long long)parts.slots * parts.BM * D;
-    const Merge merge = merge_of<D>(p, !few, few ? kRowsMinRange : kTilesMinRange);
+    const Merge merge = merge_of<D>(p, !by_rows, by_rows ? kRowsMinRange : kTilesMinRange);
     if (merge.blocks > most_workgroups(256))
         return ATTN_ERR_SHAPE;
-    int rc;
+    int rc = ATTN_ERR_LAUNCH;
     if (few)
         rc = launch_rows<D, 1, E, E4M3, true>(p, 0x7fffffff, st);
-    else if (parts.BM == 128)
-        rc = launch_tiles<D, E, E4M3, true, 1>(p, 0, st);
-    else
-        rc = launch_tiles<D, E, E4M3, true>(p, 0, st);
+    if constexpr (kMid >= 32)
+        if (mid && parts.BM == 32)
+            rc = launch_rows<D, 2, E, E4M3, true>(p, 0x7fffffff, st);
+    if constexpr (kMid >= 64)
+        if (mid && parts.BM == 64)
+            rc = launch_rows<D, 4, E, E4M3, true>(p, 0x7fffffff, st);
+    if (!by_rows)
+        rc = parts.BM == 128 ? launch_tiles<D, E, E4M3, true, 1>(p, 0, st) : launch_tiles<D, E, E4M3, true>(p, 0, st);
     return rc == ATTN_OK ? launch_merge<D, E, true>(p, merge, st) : rc;
 }
 

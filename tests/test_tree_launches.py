@@ -19,7 +19,7 @@ def test_one_kernel_with_room_for_its_workgroups(tmp_path, monkeypatch):
     from paper_2512_18134_amd import binding as lib
     assert L.RUN.count("    else:\n") == 1
     monkeypatch.setattr(L, "RUN", L.RUN.replace("    else:\n", TREE_ARGS))
-    sizes = [(D, n, G, B, width, dt, e4m3) for D in (64, 128, 256) for n, G in ((1, 1), (5, 3), (5, 4), (16, 4), (33, 4), (64, 8))
+    sizes = [(D, n, G, B, width, dt, e4m3) for D in (64, 128, 256) for n, G in ((1, 1), (5, 3), (5, 4), (16, 4), (24, 4), (33, 4), (64, 8))
              for B, width in ((1, 32), (1, 64), (1, 8192), (40, 8192)) for dt in ("bf16", "f16") for e4m3 in (False, True)]
     calls = [tree(lib, n * B, B, 2 * G, 2, D, 16, width, n, dt, e4m3) for D, n, G, B, width, dt, e4m3 in sizes]
     seen = set()
@@ -33,8 +33,8 @@ def test_one_kernel_with_room_for_its_workgroups(tmp_path, monkeypatch):
             assert x["slots"] >= x["target"] + 64, (D, n, G, B, width, name)
             assert len(lines) == 2 or width * 16 <= 256    # the merge
         if name[0] == "attn_paged_tiles_kernel":
-            assert n * G > 16
+            assert n * G > (64 if D < 256 else 32 if e4m3 else 16)
             assert x["target"] == 256 * (3 if D < 256 and n * G <= 128 else 2)
         seen.add(x["kernel"])
-    # by 16 rows (four and eight waves; D = 256 has no eight), and tiles of 128 and 256 rows (D = 256: of 128)
-    assert len(seen) == 4 * (2 * 4 + 2)
+    # by 16 rows (four and eight waves), 32 and 64, and tiles of 128 and 256 rows; D = 256: no eight waves, 32 rows in e4m3 alone, tiles of 128
+    assert len(seen) == 2 * (2 * 2 * 6 + (2 + 3))
