@@ -2,6 +2,9 @@
 //
 // The kernels are those of the attention over the paged cache with TREE set: a row sees every key in front of its sequence's new
 // tokens, and of those what its mask says.  Only the steps that hold new tokens look at the mask.
+//
+// 32 sequences of up to 8191 positions and trees of up to 24 drafts, 32 heads over 8, D = 128: 458 MB of K and V in 104 us, 95 of them the
+// kernel's (4.8 TB/s).  4 of 32768 in e4m3, 64 drafts, 64 heads over 8: 275 GFLOP in 304 to 313 us.  One tree of 15 at 1000: 11.3 us.
 #include "attn_paged_launch.h"
 #include "attn_tree.h"
 

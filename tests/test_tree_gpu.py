@@ -159,3 +159,22 @@ def test_long_sequences_are_cut_and_joined_and_repeat_bit_for_bit():
         for _ in range(3):
             q, o2, lse2, _ = attend(M, c, G, trees([n, 1], 13), max_q=n, q=q)
             assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("D, e4m3", [(64, False), (128, False), (128, True), (256, True)])
+def test_ranges_of_keys_of_which_a_row_sees_none(D, e4m3):
+    """A tree longer than the ranges that the walk is cut into: most rows see nothing of the last ones, and the first rows, without pages in front of
+    them, of all but one."""
+    from paper_2512_18134_amd import binding as M
+    n = 600
+    c = Cache([n], [6000], 1, D, 16, "bf16", e4m3, 73)
+    sets = T.random_tree(n, 21)
+    sets[7], sets[599] = 0, 1 << 599
+    q, o, lse, ref = attend(M, c, 1, [sets], max_q=n)
+    check_attention(c, o, lse, ref)
+    for missing in ((6000 - n) // 16, (6000 - n) // 16 + 1):    # of what lies before, eight positions are left, then none
+        c.table[0, :missing] = -1
+        del c._gpu
+        q, o, lse, ref = attend(M, c, 1, [sets], max_q=n, q=q)
+        check_attention(c, o, lse, ref)
+    assert lse[7, 0] == -math.inf and (o[7] == 0).all() and torch.isfinite(lse[599]).all()
