@@ -43,7 +43,9 @@ extern "C" {
  *
  *   q, strides, k_pages, k_scale, page_table, start, kv_len, kind, T .. table_width, max_q, causal, scale
  *                 as in attn_paged_fwd (attn_cache.h), whose limits hold
- *   lse           device pointer, fp32, contiguous [T][H_q]: what attn_paged_fwd (or attn_paged_tree) has left for these rows
+ *   lse           device pointer, fp32, contiguous [T][H_q]: what attention has left for these rows.  The rows of a tree of
+ *                 drafts (attn_tree.h) are weighed once their accepted path has moved together: its rows' q and lse, kv_len
+ *                 with them; causally each then sees what its mask showed it
  *   weights, weights_out   device pointers, 16-byte aligned, contiguous; the same array, or two that do not overlap
  *                 (ATTN_ERR_SHAPE).  B * H_kv * table_width * page_size at most 2^40
  *   stamps, seen  device pointers, both or neither (ATTN_ERR_NULL); stamps 16-byte aligned

@@ -5,7 +5,7 @@
 // in LDS, which no order of additions can change; what a wave has of free and of kept places is then counted, and the lists are written in
 // the places' order.  Up to kSelectWhole places a workgroup has a list, its ranks in registers from the first reading on: 512 lists of
 // 2176 places in 12 us.  Longer ones are shared out to workgroups, in four launches: a digit's counts of every part, which the next launch
-// adds up.  32 lists of 131072 places in 55 us (a workgroup to a list: 150, bound by its vector unit).
+// adds up.  32 lists of 131072 places in 52 us (a workgroup to a list: 150, bound by its vector unit).
 //
 // Move: a copy of rows; 16 bytes to a lane.  Dropped places before the new end are filled from kept ones behind it, so that as
 // little as possible moves and nothing depends on an order: a longer list is as many independent copies.  Short lists,
@@ -200,8 +200,8 @@ struct SelectList {
     }
     // The lists' elements of the places [lo, hi), whose ranks are held: kept are the ranks above top, and of those that equal it the first
     // `left`.  at_dst, at_src: elements of the places before; all three go on to what follows.  What a wave's part of a vector holds is
-    // counted, summed in the order of the places, and written.
-    __device__ __forceinline__ void emit(int lo, int hi, uint32_t top, int &left, int &at_dst, int &at_src)
+    // counted, summed in the order of the places, and written.  all_same: how many equal it, -1 if that is to be counted.
+    __device__ __forceinline__ void emit(int lo, int hi, uint32_t top, int all_same, int &left, int &at_dst, int &at_src)
     {
         constexpr int N = kHeld * WAVES;
         static_assert(N <= 64, "a lane to a wave's part of a vector");
@@ -213,20 +213,24 @@ struct SelectList {
             all = __builtin_amdgcn_readlane(upto, 63);
             return upto - x;
         };
-        int n_same[kHeld], all_same;
-        each(lo, hi, [&, i = 0](int j, u32x4 r) mutable {
-            int n = 0;
+        const bool takes = lo < keep, gives = hi > keep;    // (a part of a list has one of the two)
+        int before_same = 0;
+        if (all_same < 0 || (left > 0 && left < all_same)) {
+            int n_same[kHeld] = {};
+            each(lo, hi, [&, i = 0](int j, u32x4 r) mutable {
+                int n = 0;
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                n += __popcll(__ballot(j + k >= lo && j + k < hi && r[k] == top));
-            n_same[i++] = n;
-        });
+                for (int k = 0; k < 4; ++k)
+                    n += __popcll(__ballot(j + k >= lo && j + k < hi && r[k] == top));
+                n_same[i++] = n;
+            });
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i)
-            if (lane == 0)
-                sh.of_vector[0][i * WAVES + wave] = (lo & ~3) + i * STRIDE < hi ? n_same[i] : 0;
-        __syncthreads();
-        const int before_same = sums(0, all_same);
+            for (int i = 0; i < kHeld; ++i)
+                if (lane == 0)
+                    sh.of_vector[0][i * WAVES + wave] = n_same[i];
+            __syncthreads();
+            before_same = sums(0, all_same);
+        }
         // (all of the last rank, or none: no order among them)
         const bool some = left > 0 && left < all_same;
         uint32_t hole = 0, mover = 0;                       // bit 4 i + k
@@ -255,10 +259,17 @@ struct SelectList {
                 }
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const bool there = j + k >= lo && j + k < hi, below = j + k < keep;
-                    const bool x = there && below && !kept[k], y = there && !below && kept[k];
-                    hole |= (uint32_t)x << (4 * i + k), mover |= (uint32_t)y << (4 * i + k);
-                    holes += __popcll(__ballot(x)), movers += __popcll(__ballot(y));
+                    const bool there = j + k >= lo && j + k < hi;
+                    if (takes) {
+                        const bool x = there && !kept[k] && (!gives || j + k < keep);
+                        hole |= (uint32_t)x << (4 * i + k);
+                        holes += __popcll(__ballot(x));
+                    }
+                    if (gives) {
+                        const bool y = there && kept[k] && (!takes || j + k >= keep);
+                        mover |= (uint32_t)y << (4 * i + k);
+                        movers += __popcll(__ballot(y));
+                    }
                 }
             }
             if (lane == 0)
@@ -282,8 +293,10 @@ struct SelectList {
                         list[at++] = (lo & ~3) + i * STRIDE + 4 * tid + k;
             }
         };
-        write(dst, hole, at_dst + before_holes);
-        write(src, mover, at_src + before_movers);
+        if (takes)
+            write(dst, hole, at_dst + before_holes);
+        if (gives)
+            write(src, mover, at_src + before_movers);
         at_dst += all_holes, at_src += all_movers, left -= min(left, all_same);
         __syncthreads();                                    // the counts have been read
     }
@@ -316,7 +329,7 @@ __global__ __launch_bounds__(THREADS) void attn_select_kernel(const SelectParams
             l.tally(pass, top, 0, l.kv);
             top |= (uint32_t)l.find(left) << digit_shift(pass);
         }
-        l.emit(0, l.kv, top, left, at_dst, at_src);
+        l.emit(0, l.kv, top, -1, left, at_dst, at_src);
     }
     l.fill(at_dst, 0, 1);
 }
@@ -437,7 +450,9 @@ __global__ __launch_bounds__(kPartThreads, 4) void attn_select_part_kernel(const
             }
             if (l.h == 0 && part == 0 && l.tid == 0)
                 p.new_len[l.b] = l.new_len();
-            chunks([&](int from, int upto) { l.emit(from, upto, top, left, at_dst, at_src); });
+            const int equal = hi - (lo & ~3) <= kPartChunk ? same[part] : -1;
+            __syncthreads();
+            chunks([&](int from, int upto) { l.emit(from, upto, top, equal, left, at_dst, at_src); });
             l.fill(all, part, parts.all);
             return;
         }
