@@ -244,7 +244,9 @@ __global__ __launch_bounds__(256) void attn_weigh_rows_kernel(const WeighParams 
 
 // Many rows: a workgroup has 256 keys (128 at D = 256), each wave its part of them in registers as A operands of v_mfma_f32_32x32x16,
 // and the rows pass through LDS in stages that all waves read.  A batch with few blocks of 256 keys is cut finer: two waves of a workgroup
-// then have the same keys, and half of a stage's rows each.
+// then have the same keys, and half of a stage's rows each.  RING stages are there at once, all but one of them on their way: two, and two
+// workgroups to a compute unit, or four where the batch has no more units than compute units, whose stages would each wait for memory
+// otherwise (2048 rows at 16384 keys, 8 heads over 2, D = 256: two 193 us, four 178).
 template <int D>
 struct WeighTiling {
     static constexpr int ROWB = D * 2, SUB = D == 256 ? 2 : 4;     // 32-row tiles of a stage
@@ -252,11 +254,12 @@ struct WeighTiling {
     static constexpr int KB = D == 256 ? 1 : 2;                    // 32-key blocks of a wave
     static constexpr int KEYS = 4 * 32 * KB;                       // of a workgroup
     static constexpr int SHARE = SUB / 2;                          // waves that share keys where the batch has few blocks
-    static constexpr int LDS_BYTES = 2 * (STAGE + ROWS * 4);
+    static constexpr int LSE = 4 * 64 * 4;                         // bytes of the rows' lse of a stage: 64 rows of each wave, some of the next one's
+    static constexpr int lds_bytes(int ring) { return ring * (STAGE + LSE); }
 };
 constexpr int kWeighTileGroups = 512;   // workgroups of a launch: two to a compute unit
 
-template <int D, typename E, bool E4M3>
+template <int D, typename E, bool E4M3, int RING>
 __global__ __launch_bounds__(256, 2) void attn_weigh_tiles_kernel(const WeighParams p)
 {
     typedef WeighTiling<D> T;
@@ -287,12 +290,16 @@ __global__ __launch_bounds__(256, 2) void attn_weigh_tiles_kernel(const WeighPar
         const int from = p.causal ? (int)min((long long)max(key0 - first_pos, 0) * p.G, (long long)n_rows) : 0;
         const int stages = (n_rows - from + T::ROWS - 1) / T::ROWS;
 
-        // ---- rows: memory -> LDS, stage i into its half.  A load takes RPL rows; lane -> (row, 16-byte chunk), the swizzle of a
-        // tile's rows is applied on the global side.  Rows behind the last repeat it
-        const uint64_t at = (uint64_t)(uintptr_t)p.q + 2 * ((long long)row0 * p.q_st + (long long)h * p.G * p.q_sh);
-        const void *rows = reinterpret_cast<const void *>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32 |
-                                                          (uint32_t)__builtin_amdgcn_readfirstlane((int)at));
-        asm volatile("s_nop 4" : "+s"(rows));               // five wait states between the vector unit's write of a scalar and a load
+        // ---- rows and their lse: memory -> LDS, stage i into its part of the ring.  A load takes RPL rows; lane -> (row, 16-byte chunk), the
+        // swizzle of a tile's rows is applied on the global side.  Rows behind the last repeat it
+        auto scalar = [](const void *at) {
+            const uint64_t x = (uint64_t)(uintptr_t)at;
+            return reinterpret_cast<const void *>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 |
+                                                  (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+        };
+        const void *rows = scalar(static_cast<const typename E::t *>(p.q) + ((long long)row0 * p.q_st + (long long)h * p.G * p.q_sh));
+        const void *lses = scalar(p.lse + ((size_t)row0 * p.H_q + h * p.G));
+        asm volatile("s_nop 4" : "+s"(rows), "+s"(lses));   // five wait states between the vector unit's write of a scalar and a load
         uint32_t off[LOADS];
         const uint32_t step = (uint32_t)(T::ROWS / p.G) * st;
         const bool even = T::ROWS % p.G == 0;               // a stage's rows are whole tokens: the next one's lie a step on
@@ -312,22 +319,16 @@ __global__ __launch_bounds__(256, 2) void attn_weigh_tiles_kernel(const WeighPar
                 } else {
                     off[l] += step;
                 }
-                dma16(lds0 + (i & 1) * T::STAGE + (wave * LOADS + l) * 1024, rows, off[l]);
+                dma16(lds0 + i % RING * T::STAGE + (wave * LOADS + l) * 1024, rows, off[l]);
             }
+            const int row = min(first + 64 * wave + ln, n_rows - 1), token = p.token_of(row);
+            dma4(lds0 + RING * T::STAGE + i % RING * T::LSE + wave * 256, lses, (uint32_t)(token * p.H_q + row - token * p.G) * 4);
         };
-        // what a row's scores are lowered by (base 2), infinity where it sees nothing or there is no row: a thread has a row of the stage
-        float *const shifts = reinterpret_cast<float *>(smem + 2 * T::STAGE);
-        float lse = -INFINITY;
-        auto ask = [&](int i) {
-            const int r = from + i * T::ROWS + (int)threadIdx.x, row = min(r, n_rows - 1), token = p.token_of(row);
-            if (threadIdx.x < T::ROWS && i < stages)
-                lse = r < n_rows ? p.lse[(size_t)(row0 + token) * p.H_q + h * p.G + row - token * p.G] : -INFINITY;
-        };
+        const float *const raw = reinterpret_cast<const float *>(smem + RING * T::STAGE);
         __syncthreads();                                    // the last unit's rows have been read
-        if (stages > 0) {
-            bring(0);
-            ask(0);
-        }
+#pragma unroll
+        for (int i = 0; i < RING - 1; ++i)
+            bring(i);
 
         // ---- keys: lane l has key l % 32 of a block, elements 16 s + 8 g on of step s
         u32x4 a[KB][KS];
@@ -351,6 +352,13 @@ __global__ __launch_bounds__(256, 2) void attn_weigh_tiles_kernel(const WeighPar
                     a[t][s] = *reinterpret_cast<const u32x4 *>(k + 32 * s + 16 * g);
             }
         }
+        // (waited for here: at their first use the wait would be part of the loop, and one for the rows on their way as well; D = 64,
+        // 2048 rows at 16384 keys, 16 heads over 4: 115 us, 118 without)
+#pragma unroll
+        for (int t = 0; t < KB; ++t)
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+                asm volatile("" : "+v"(a[t][s]));
 
         float w[KB][16];
 #pragma unroll
@@ -362,7 +370,7 @@ __global__ __launch_bounds__(256, 2) void attn_weigh_tiles_kernel(const WeighPar
         // `then` and are lowered by `down`: the matrix pipe and the vector unit have the same to do, and neither waits for the other.
         float down = -INFINITY;
         auto scores = [&](int i, int t, f32x16 (&now)[KB], f32x16 (&then)[KB]) {
-            const uint32_t base = lds0 + (i & 1) * T::STAGE + t * 32 * ROWB;
+            const uint32_t base = lds0 + i % RING * T::STAGE + t * 32 * ROWB;
             asm volatile("" : "+v"(k0));                    // (its later chunks' offsets made anew: kept they take registers)
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
@@ -383,15 +391,26 @@ __global__ __launch_bounds__(256, 2) void attn_weigh_tiles_kernel(const WeighPar
                 for (int kb = 0; kb < KB; ++kb)
                     now[kb] = mfma32<E>(a[kb][ks], q[ks % (AHEAD + 1)], now[kb]);
                 constexpr int PER = 16 * KB / KS;
+                // (side by side, so that no exponential is waited for; and here, not behind the products)
+                float e[PER];
 #pragma unroll
-                for (int x = ks * PER; x < (ks + 1) * PER; ++x) {
-                    w[x / 16][x % 16] += __builtin_amdgcn_exp2f(fmaf(then[x / 16][x % 16], p.c_log2, down));
-                    asm volatile("" : "+v"(w[x / 16][x % 16]));              // (here, not behind the products)
-                }
+                for (int x = 0; x < PER; ++x)
+                    e[x] = fmaf(then[(ks * PER + x) / 16][(ks * PER + x) % 16], p.c_log2, down);
+#pragma unroll
+                for (int x = 0; x < PER; ++x)
+                    e[x] = __builtin_amdgcn_exp2f(e[x]);
+#pragma unroll
+                for (int x = 0; x < PER; ++x)
+                    w[(ks * PER + x) / 16][(ks * PER + x) % 16] += e[x];
+#pragma unroll
+                for (int x = 0; x < PER; ++x)
+                    asm volatile("" : "+v"(w[(ks * PER + x) / 16][(ks * PER + x) % 16]));
                 __builtin_amdgcn_sched_barrier(0);
             }
-            down = shifts[(i & 1) * T::ROWS + 32 * t + lq];
+            // what a row's scores are lowered by (base 2): infinity where it sees nothing or there is no row
             const int first = from + i * T::ROWS + 32 * t;
+            const float lse = raw[i % RING * (T::LSE / 4) + 32 * t + lq];
+            down = first + lq < n_rows && lse != -INFINITY ? -lse * 1.44269504088896340736f : -INFINITY;
             if (p.causal && first_pos + p.token_of(min(first, n_rows - 1)) < j0 + 32 * KB - 1) {     // some row does not see some key
                 // (against constants: positions kept in registers would take 32)
                 const int limit = first_pos + p.token_of(min(first + lq, n_rows - 1)) - j0 - 4 * g;
@@ -410,12 +429,12 @@ __global__ __launch_bounds__(256, 2) void attn_weigh_tiles_kernel(const WeighPar
                 s1[kb][r] = 0.f;                            // (lowered by infinity)
 #pragma clang loop unroll(disable)
         for (int i = 0; i < stages; ++i) {
-            wait_vmcnt<0>();
-            if (threadIdx.x < T::ROWS)
-                shifts[(i & 1) * T::ROWS + threadIdx.x] = lse == -INFINITY ? -INFINITY : -lse * 1.44269504088896340736f;
+            if (RING > 2 && i + RING - 2 < stages)
+                wait_vmcnt<(RING - 2) * (LOADS + 1)>();     // of stage i nothing is on its way, of those behind it all may be
+            else
+                wait_vmcnt<0>();                            // (the last ones: there are fewer behind)
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");     // stage i is complete, stage i - 1 has been read
-            bring(i + 1);
-            ask(i + 1);
+            bring(i + RING - 1);
 #pragma clang loop unroll(disable)
             for (int t = tile0, upto = min(tile1, (n_rows - from - i * T::ROWS + 31) / 32); t < upto; t += 2) {
                 scores(i, t, s0, s1);
@@ -496,13 +515,17 @@ int launch(const WeighParams &p, int max_q, hipStream_t st)
     const int held = tiles ? attn::kWeighTileGroups : attn::persistent_slots(reinterpret_cast<const void *>(attn::attn_weigh_rows_kernel<D, E, E4M3>), 256, 0, 1);
     const long long most = held > 0 ? held : attn::kWeighGroups, per_seq = blocks < most ? blocks * p.c.H_kv : most;
     const long long grid = per_seq < most / seqs ? per_seq * seqs : most;
-    if (tiles) {
-        constexpr int lds = attn::WeighTiling<D>::LDS_BYTES;
-        if (!attn::allow_lds(reinterpret_cast<const void *>(attn::attn_weigh_tiles_kernel<D, E, E4M3>), lds))
-            return ATTN_ERR_LAUNCH;
-        hipLaunchKernelGGL((attn::attn_weigh_tiles_kernel<D, E, E4M3>), dim3((unsigned)grid), dim3(256), lds, st, p);
-    } else {
+    if (!tiles) {
         hipLaunchKernelGGL((attn::attn_weigh_rows_kernel<D, E, E4M3>), dim3((unsigned)grid), dim3(256), 0, st, p);
+    } else {
+        // (D = 64: four stages leave room for two workgroups)
+        const bool deep = D == 64 || grid <= attn::kWeighTileGroups / 2;
+        constexpr int two = D == 64 ? 4 : 2;
+        auto *const kern = deep ? attn::attn_weigh_tiles_kernel<D, E, E4M3, 4> : attn::attn_weigh_tiles_kernel<D, E, E4M3, two>;
+        const int lds = attn::WeighTiling<D>::lds_bytes(deep ? 4 : two);
+        if (!attn::allow_lds(reinterpret_cast<const void *>(kern), lds))
+            return ATTN_ERR_LAUNCH;
+        hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), lds, st, p);
     }
     return hipGetLastError() == hipSuccess ? ATTN_OK : ATTN_ERR_LAUNCH;
 }
