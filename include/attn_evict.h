@@ -115,7 +115,9 @@ long long attn_cache_select_workspace_bytes(int B, int H_kv, int width);
  * (ATTN_ERR_SHAPE).
  *
  * An accepted path m_0 < m_1 < ... of the n_b drafted tokens of a sequence: dst = kv_len - n_b + 0, 1, ..., src = kv_len - n_b + m_0,
- * m_1, ... with list_heads 1; the new kv_len is kv_len - n_b + the path's length.
+ * m_1, ... with list_heads 1; the new kv_len is kv_len - n_b + the path's length.  Its places overlap, so a call takes at most 128
+ * tokens of it (moves_width): a longer path in one call leaves it to the order of the workgroups what is read.  Calls of up to 128
+ * elements each, in ascending order on one stream, move a path of any length: m_i >= i, so none writes what a later one reads.
  */
 int attn_cache_move(void *k_pages, void *v_pages, unsigned char *k_scale, unsigned char *v_scale, const int *page_table,
                     const int *dst, const int *src, int kind, float *weights, int *stamps,

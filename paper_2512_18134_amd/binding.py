@@ -922,7 +922,8 @@ def attn_cache_move(k_pages, v_pages, page_table, dst, src, k_scale=None, v_scal
 
     dst, src int32 [B,H_kv,moves], or [B,1,moves] for all heads alike; elements outside the table move nothing.  In lists of more than
     128 elements no place may be both source and destination.  An accepted path of a tree of n drafted tokens, token
-    numbers path [B,1,m] ascending: dst = kv_len - n + arange(m), src = kv_len - n + path.
+    numbers path [B,1,m] ascending: dst = kv_len - n + arange(m), src = kv_len - n + path, at most 128 elements of it a call; a
+    longer path in several calls, in ascending order on one stream.
     Asynchronous on `stream`.  Returns (k_pages, v_pages).
     """
     r = (_marshal_module or _native()).move(k_pages, v_pages, page_table, dst, src, k_scale, v_scale, weights, stamps, stream)
