@@ -285,6 +285,7 @@ def prepare(case, seed):
         s["weights"] = _weights(case, gen)
         s["stamps"], s["seen"] = _stamps(s, gen) if case["stamps"] else (None, None)
         s["keep"] = torch.tensor(_keeps(case), dtype=torch.int32, device=_DEVICE)
+        s["moves"] = _most_moves(case)                    # a number of the program's plan, not of a call
         return s
 
     # a pool in which the sequences' pages lie in no order; the table is padded with -1
@@ -317,7 +318,8 @@ def prepare(case, seed):
     elif case["keep"]:
         s["keep"] = torch.tensor(_keeps(case), dtype=torch.int32, device=_DEVICE)
         weights = _weights(case, gen)
-        s["dst"], s["src"], _ = _select_plain({"case": case, "weights": weights, "stamps": None, "kv_len": s["kv_len"], "keep": s["keep"]})
+        s["dst"], s["src"], _ = _select_plain({"case": case, "weights": weights, "stamps": None, "kv_len": s["kv_len"], "keep": s["keep"],
+                                             "moves": _most_moves(case)})
         s["weights"], s["stamps"] = (weights, _stamps(s, gen)[0]) if case["stamps"] else (None, None)
     else:
         # the accepted path of each tree: its first token is the first drafted one, the others lie behind the path's end
@@ -349,8 +351,6 @@ def _run_own(s):
     from paper_2512_18134_amd import binding
     case = s["case"]
     if case["op"] == "select":
-        if "moves" not in s:                              # a number of the program's plan, not of a call
-            s["moves"] = _most_moves(case)
         dst, src, new_len = binding.attn_cache_select(s["weights"], s["kv_len"], s["keep"], s["moves"], stamps=s["stamps"],
                                                       seen=s["seen"], sinks=case["sinks"], recent=case["recent"])
         return {"dst": dst, "src": src, "new_len": new_len}
@@ -474,7 +474,7 @@ def _select_plain(s):
     w = torch.where(j < kv, torch.where(always, float("inf"), w), -1.0)
     order = w.sort(dim=-1, descending=True, stable=True).indices
     kept = torch.zeros_like(w, dtype=torch.bool).scatter_(2, order, (j < keep).expand_as(w).contiguous())
-    M = _most_moves(case)
+    M = s["moves"]
     lists = torch.full((2,) + w.shape[:2] + (M + 1,), -1, dtype=torch.int64, device=w.device)
     for i, chosen in enumerate(((j < keep) & ~kept, (j >= keep) & kept)):
         at = torch.where(chosen, chosen.cumsum(dim=-1) - 1, M).clamp(max=M)
