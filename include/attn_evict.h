@@ -94,8 +94,9 @@ int attn_cache_select(const float *weights, const int *stamps, const int *seen, 
                       int *dst, int *src, int *new_len, int sinks, int recent, void *workspace, long long workspace_bytes,
                       int B, int H_kv, int width, int moves_width, void *stream);
 
-/* Bytes of workspace attn_cache_select needs (0 up to 16384 places, some 25 KB for each 16384 places of a list beyond); -1 on
- * invalid arguments. */
+/* Bytes of workspace attn_cache_select needs; -1 on invalid arguments.  0 for a width of up to 16384 places.  Beyond, 24580 bytes for every part
+ * of a list and 16 for the list, which has ceil(width / part) + 2 of them: parts of 16384 places up to 2^20, and of as many times that beyond
+ * as leave no more than 66.  98 KB a list of 16400 places, 246 KB of 131072, 1.6 MB at most. */
 long long attn_cache_select_workspace_bytes(int B, int H_kv, int width);
 
 /*

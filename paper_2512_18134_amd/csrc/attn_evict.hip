@@ -503,7 +503,7 @@ struct MoveParams {
 
 constexpr int kMoveTogether = 128;      // elements of a list that are read before any is written
 
-// One list, or 64 elements of a longer one, of a sequence and key head; blockIdx.y: keys or values.  RB: bytes of a row.
+// One list, or kMoveTogether elements of a longer one, of a sequence and key head; blockIdx.y: keys or values.  RB: bytes of a row.
 template <int RB>
 __global__ __launch_bounds__(256, RB == 512 ? 4 : 6) void attn_move_kernel(const MoveParams p, int parts)
 {

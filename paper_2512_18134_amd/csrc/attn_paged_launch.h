@@ -13,8 +13,9 @@
 
 namespace attn {
 
-// Workgroups that the chip holds at once: on each of 256 compute units two of the e4m3 tile kernel, one of the 16-bit one, and of
-// the row kernel what its tiling promises the compiler.  (16 sequences of four drafted tokens and 512 .. 4100
+// Workgroups that the chip holds at once: on each of 256 compute units two of the tile kernel for e4m3 chunks and for trees (three for trees of
+// up to 128 rows at D < 256: PagedTilesTiling::PER_CU), one of the scheduled one for 16-bit chunks, and of the row kernel what its tiling
+// promises the compiler.  (16 sequences of four drafted tokens and 512 .. 4100
 // positions, D = 256: 26.0 us cut for 512, 22.0 for 256.)
 constexpr int kTarget = 512;
 template <int D, int MT>

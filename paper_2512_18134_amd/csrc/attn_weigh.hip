@@ -2,8 +2,9 @@
 // (include/attn_evict.h).
 //
 // S = K Q^T once more, without a second product: exp(S - lse) summed over a position's column of queries.  Every position belongs
-// to one wave, which walks the rows that see it: sums stay in its registers, in a fixed order, and nothing is joined in
-// memory.  For few rows the kernel is a stream of keys; for many the matrix pipe and the exponentials bound it.
+// to one wave, which walks the rows that see it (in small batches of many rows to two waves of a workgroup, which add their halves in LDS):
+// sums stay in registers, in a fixed order, and nothing is joined in memory.  For few rows the kernel is a stream of keys; for many the
+// matrix pipe and the exponentials bound it.
 //
 // 64 sequences of up to 8191 positions, one token each, 32 heads over 8, D = 128: 455 MB of keys in 98.5 us (4.8 TB/s with the weights).  2048
 // tokens at the end of 16384: 258 GFLOP in 259 to 277 us, 930 to 996 TFLOP/s, at the power limit.
