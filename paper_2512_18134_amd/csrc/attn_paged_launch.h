@@ -35,7 +35,11 @@ constexpr int kRowsMinRange = 2, kTilesMinRange = 4;
 // keys 13.6 whole, 9.9 cut.
 constexpr long long kWholeBytes = 1 << 18;
 constexpr int kWaves = 8;
-// Bytes of K and V, counted for every 16-row tile that reads them, up to which a tree's rows are taken 16 at a time.
+// Bytes of K and V, counted for every 16-row tile that reads them, up to which a tree's rows are taken 16 at a time; K and V as many as the table
+// can hold.  32 heads over 8, D = 128, us by 16 rows and by what is chosen otherwise: 15 drafts at 1000 in e4m3 (8 MB) 11.7 and 17.0, in 16 bits
+// (16 MB) 11.9 and 17.6, at 2000 (33 MB) 12.6 and 16.4; beyond the bound 40 at 1000 (45 MB) 14.8 and 47.7, 15 at 4000 (66 MB) 17.2 and 21.4,
+// four of 15 at 1000 (78 MB) 16.5 and 22.4; 16 of 8 at 8000, 16 heads over 4 (786 MB) 83.6 and 58.1.  8 of 6 at 300, 8 heads over 2, D = 256 (12 MB)
+// 13.6 and 21.9.
 constexpr long long kFewBytes = 32 << 20;
 constexpr int kSlots = 2 * kTarget + 64;
 // words of 64 bits of a row's mask, at most: as many new tokens as a tree of drafts will not have
@@ -252,8 +256,11 @@ int launch(PagedParams &p, int max_q, hipStream_t st)
 // Trees of drafted tokens: few rows of many heads, or some hundreds.  One kernel takes all sequences of a call:
 //   * the row kernel by 16 rows where no sequence has more, or where K and V are so small that reading them for every such tile
 //     takes no time (kFewBytes)
-//   * the row kernel by 32 or 64 rows where no sequence has more: 16 sequences of 8 drafts at 8000, 16 heads over 4, D = 128, 57.5 us
-//     and in e4m3 32.2, by the tile kernel 63.7 and 43.4; at D = 256 65.9 and 82.3 in e4m3, 114.6 and 110.4 in 16 bits
+//   * the row kernel by 32 or 64 rows where no sequence has more: 16 sequences of 8 drafts at 8000, 16 heads over 4, D = 128, 58.1 us
+//     and in e4m3 31.5, by the tile kernel 64.4 and 42.7; of 16 drafts 62.5 and 45.1, by tiles 70.5 and 51.8; D = 64 32.2 and 34.3, 36.3 and
+//     35.7; at D = 256 8 drafts 65.6 and 82.4 in e4m3, 114.6 and 110.4 in 16 bits.  Long sequences of few heads are the tile kernel's: 27 of 8
+//     drafts at 50000, 4 heads over 1, D = 128, 179 us and in e4m3 114, by tiles 133 and 86; of 16 203 and 157, 142 and 102; at D = 64 of 8
+//     78 and 43, 73 and 65, of 16 115 and 119, 76 and 71
 //   * otherwise the tile kernel, whose waves share a tile of keys, with 32 or 64 rows to a wave.  A wave without rows brings its share
 //     of the keys and has nothing else to do, so that a sequence of few rows costs it no more than its stream
 template <int D, typename E, bool E4M3>

@@ -499,8 +499,16 @@ using attn::WeighParams;
 
 bool misaligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
-// Rows of a sequence up to which the row kernel takes a call.  8 sequences of 16384 keys, 4 heads: of 64 rows D = 128 50.2 us by rows and
-// 45.8 by tiles, D = 64 in e4m3 25.5 and 32.8; of 128 79.2 and 47.8, 40.8 and 33.9.
+// Rows of a sequence up to which the row kernel takes a call: one bound for all head sizes, though they cross at rows of their own.  8 sequences of
+// 16384 keys, 4 heads, us by rows and by tiles:
+//     rows                     16            32            48            64            80            96           128
+//     D = 64,  16 bits     19.1  31.2    22.0  30.3    25.8  30.5    29.2  30.3    33.0  35.8    36.9  35.8    43.9  35.7
+//              e4m3        14.3  28.0    18.3  28.5    21.8  28.4    25.7  28.6    29.4  34.2    33.3  33.8    41.3  33.5
+//     D = 128, 16 bits     29.6  41.0    36.0  40.7    43.1  41.2    50.1  41.2    57.4  48.3    64.6  48.2    79.5  48.9
+//              e4m3        23.1  38.5    30.4  38.3    37.0  38.5    43.5  38.7    50.6  44.3    57.5  44.2    71.7  44.8
+//     D = 256, 16 bits     58.4  69.3    70.5  69.3    83.7  71.5    97.4  72.0     112  90.1     125  90.0     154  84.1
+//              e4m3        41.0  57.9    55.3  58.9    69.8  59.0    83.9  58.5    98.7  76.3     113  76.3     142  72.8
+// One sequence of 4000: 16 to 64 rows by rows 6.0 to 9.5 and by tiles 7.4 to 9.4.
 constexpr long long kRowsMost = 64;
 
 template <int D, typename E, bool E4M3>
