@@ -29,8 +29,14 @@ extern "C" {
  * workspace_bytes at least attn_paged_tree_workspace_bytes(T, B, H_q, H_kv, D), else ATTN_ERR_WORKSPACE; calls that follow each other may
  * share one, also with attn_paged_fwd (the larger of the two sizes).
  *
- * All other arguments, results, limits, ownership and errors are those of attn_paged_fwd; ATTN_ERR_NULL, ATTN_ERR_SHAPE and ATTN_ERR_ALIGN stand for the mask's arguments too.  Every row reads every
- * key that its sequence has, so no row is cheaper for what its mask hides.
+ * All other arguments, results, limits, ownership and errors are those of attn_paged_fwd; ATTN_ERR_NULL, ATTN_ERR_SHAPE and ATTN_ERR_ALIGN stand
+ * for the mask's arguments too.  Every row reads every key that its sequence has, so no row is cheaper for what its mask hides.  P enters the
+ * second product in 16 bits as there: against 64 bits o is off by 0.0018 to 0.0023 of its norm (bf16; 0.00025 to 0.00029 fp16), of which
+ * rounding o alone makes 0.0017 (0.00021).
+ *
+ * The host chooses the kernels by sizes alone, K and V as many as the table can hold: one tree of 15 at 1000 (32 heads over 8, D = 128) takes
+ * some 12 us with a table of 1000 positions and 18 with one of 16384 or more, 16 trees of up to 77 at up to 2100 (8 over 2, D = 256, fp16) 30.8
+ * and 32.7.
  */
 int attn_paged_tree(const void *q, const long long *strides, void *o, float *lse,
                     const void *k_pages, const void *v_pages, const unsigned char *k_scale, const unsigned char *v_scale,
