@@ -51,6 +51,9 @@ extern "C" {
  *   stamps, seen  device pointers, both or neither (ATTN_ERR_NULL); stamps 16-byte aligned
  *   decay         finite and >= 0, else ATTN_ERR_SCALE
  *
+ * scale * log2(e) and lse * log2(e) are fp32 numbers, as the scores are: against 64 bits the weights are off by 2.5e-8 to 5.1e-7 of their norm
+ * (the formula in fp32 with the exponential of scale * q.k - lse: 2.5e-8 to 4.3e-7).
+ *
  * NaN and infinities in a row's q or lse make all weights of its sequence and head unspecified, those in a position's k that position's.
  */
 int attn_cache_weigh(const void *q, const long long *strides, const float *lse, const void *k_pages, const unsigned char *k_scale,
@@ -89,12 +92,12 @@ int attn_cache_weigh_f16(const void *q, const long long *strides, const float *l
  *   workspace  device pointer, 16-byte aligned, owned by the caller, overwritten; workspace_bytes at least
  *              attn_cache_select_workspace_bytes(B, H_kv, width), else ATTN_ERR_WORKSPACE; NULL where that is 0.  It holds nothing
  *              between calls; calls that overlap in time need one each
- */
-int attn_cache_select(const float *weights, const int *stamps, const int *seen, const int *kv_len, const int *keep,
-                      int *dst, int *src, int *new_len, int sinks, int recent, void *workspace, long long workspace_bytes,
  *
  * The host does not see kv_len, so the width says which kernels run: 512 lists of 2176 places, each in a row of 2176 or of 16384, take 12.6
  * or 13.0 us, in a row of 32768 or of 131072 102 or 92.
+ */
+int attn_cache_select(const float *weights, const int *stamps, const int *seen, const int *kv_len, const int *keep,
+                      int *dst, int *src, int *new_len, int sinks, int recent, void *workspace, long long workspace_bytes,
                       int B, int H_kv, int width, int moves_width, void *stream);
 
 /* Bytes of workspace attn_cache_select needs; -1 on invalid arguments.  0 for a width of up to 16384 places.  Beyond, 24580 bytes for every part
