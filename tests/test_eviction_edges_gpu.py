@@ -1,6 +1,5 @@
 """Calls of trees, weights and moves that their headers allow and that stand beside the ordinary ones: more query heads to a key head than a tile has
 rows, heads farther apart than rows, weights that are not there yet, one long list for all heads, arrays beside the cache one at a time."""
-
 import pytest
 import torch
 

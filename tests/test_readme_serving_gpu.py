@@ -9,7 +9,6 @@ import pytest
 import torch
 
 import evict_ref as E
-import serving_ref as R
 import tree_ref as T
 from test_paged_gpu import check_attention
 
